@@ -1305,6 +1305,24 @@ int launch_decode_avg(const DeviceState &st, int kind, const WorkerPtrs &wp, int
 
 int dq8::after_launch_of(const char *what, hipStream_t stream) { return after_launch(what, stream); }
 
+int dq8::failed(int code, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(t_err, sizeof(t_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+int dq8::device_tables(int kind, DeviceTables *out)
+{
+    DeviceState *st;
+    const int rc = device_state(&st);
+    if (rc) return rc;
+    *out = {st->tables + (size_t)kind * kTableWords, st->search_words[kind], st->cus};
+    return DQ8_OK;
+}
+
 extern "C" {
 
 const char *dq8_last_error(void) { return t_err; }

@@ -39,6 +39,28 @@ class Dq8Error(RuntimeError):
     pass
 
 
+class _Cache(ctypes.Structure):  # dq8_cache of include/dq8_cache.h
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("pages", ctypes.c_size_t),
+                ("kv_heads", ctypes.c_int), ("page_size", ctypes.c_int), ("dim", ctypes.c_int)]
+
+
+class _Append(ctypes.Structure):  # dq8_append
+    _fields_ = ([("type", ctypes.c_int), ("tokens", ctypes.c_size_t), ("heads", ctypes.c_int)]
+                + [(f, ctypes.c_void_p) for f in ("q", "k", "v", "q_out")]
+                + [("%s_%s_stride" % (f, w), ctypes.c_size_t) for f in ("q", "k", "v", "q_out") for w in ("token", "head")]
+                + [(f, ctypes.c_void_p) for f in ("slots", "positions", "rotation")]
+                + [("n_positions", ctypes.c_size_t), ("half", ctypes.c_int), ("interleaved", ctypes.c_int),
+                   ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_double)])
+
+
+class _Attention(ctypes.Structure):  # dq8_attention
+    _fields_ = ([("type", ctypes.c_int), ("tokens", ctypes.c_size_t), ("heads", ctypes.c_int), ("q", ctypes.c_void_p), ("out", ctypes.c_void_p)]
+                + [("%s_%s_stride" % (f, w), ctypes.c_size_t) for f in ("q", "out") for w in ("token", "head")]
+                + [("batch", ctypes.c_size_t), ("max_pages", ctypes.c_size_t)]
+                + [(f, ctypes.c_void_p) for f in ("pages", "lens", "starts")]
+                + [("max_new", ctypes.c_size_t), ("window", ctypes.c_int), ("softmax_scale", ctypes.c_float)])
+
+
 def lib():
     """The loaded shared library (loaded on first use)."""
     global _lib, _native
@@ -65,6 +87,12 @@ def lib():
                   L.dq8_decode_accumulate_avg_local, L.dq8_decode_avg_encode, L.dq8_absmax_segments, L.dq8_encode_segments,
                   L.dq8_decode_segments, L.dq8_decode_accumulate_avg_segments):
             f.restype = ci
+        L.dq8_cache_append.argtypes = [ci, ctypes.POINTER(_Cache), ctypes.POINTER(_Append), vp]
+        L.dq8_cache_append.restype = ci
+        L.dq8_cache_attention.argtypes = [ci, ctypes.POINTER(_Cache), ctypes.POINTER(_Attention), vp, sz, vp]
+        L.dq8_cache_attention.restype = ci
+        L.dq8_cache_attention_workspace_bytes.argtypes = [ctypes.POINTER(_Cache), ctypes.POINTER(_Attention)]
+        L.dq8_cache_attention_workspace_bytes.restype = sz
         dbl = ctypes.c_double
         L.dq8_model_speedup.argtypes = [ci, dbl, dbl, dbl, ci, dbl, dbl, ctypes.POINTER(dbl)]
         L.dq8_model_penalty.argtypes = [ctypes.POINTER(dbl), ctypes.POINTER(dbl), sz, ctypes.POINTER(dbl)]
@@ -389,6 +417,157 @@ def error_stats(kind, x, block=0, scales=None, scales_given=False, stats=None, m
     _enqueue(lib().dq8_error_stats, x.get_device(), int(kind), x.data_ptr(), n, int(block), scales.data_ptr(),
              SCALES_GIVEN if scales_given else 0, stats.data_ptr(), means.data_ptr())
     return stats, means
+
+
+# types of keys, values and queries (include/dq8_cache.h)
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def cache_buffers(pages, kv_heads, page_size, dim, device="cuda"):
+    """(codes, scales) of an empty paged cache: uint8[2, pages, kv_heads, page_size, dim] and float32[2, pages, kv_heads, page_size],
+    keys before values, every row a zero."""
+    shape = (2, int(pages), int(kv_heads), int(page_size), int(dim))
+    return torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(shape[:-1], dtype=torch.float32, device=device)
+
+
+def _cache(codes, scales):
+    _dev(codes, torch.uint8, "codes")
+    _dev(scales, torch.float32, "scales")
+    if codes.dim() != 5 or codes.shape[0] != 2 or scales.shape != codes.shape[:-1]:
+        raise ValueError("codes must be [2, pages, kv_heads, page_size, dim] and scales the same without the last axis")
+    if scales.device != codes.device:
+        raise ValueError("codes and scales are on different devices")
+    return _Cache(codes.data_ptr(), scales.data_ptr(), codes.shape[1], codes.shape[2], codes.shape[3], codes.shape[4])
+
+
+def _on(device, t, dtype, shape, what):
+    """A contiguous tensor of exactly this type, shape and device."""
+    _dev(t, dtype, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if t.device != device:
+        raise ValueError("%s is on another device than the cache" % what)
+    return t.data_ptr()
+
+
+def _rows(t, what, device, dtype, tokens, heads, dim):
+    """[tokens, heads, dim] with the elements of a row side by side, any other strides: (address, token stride, head stride)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if t.dim() != 3 or (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+        raise ValueError("%s must have shape [tokens, heads, dim] = [%s, %s, %d], got %s"
+                         % (what, "any" if tokens is None else tokens, "any" if heads is None else heads, dim, tuple(t.shape)))
+    if t.stride(2) != 1 and t.numel():
+        raise ValueError("the elements of a row of %s must lie side by side" % what)
+    if t.device != device:
+        raise ValueError("%s is on another device than the cache" % what)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def cache_append(kind, k, v, slots, codes, scales, positions=None, rotation=None, interleaved=False, q=None, q_weight=None,
+                 k_weight=None, eps=1e-6, q_out=None):
+    """Compresses keys and values [tokens, kv_heads, dim] into the cache rows that ``slots`` (int64, slot = page * page_size +
+    place; any other number: padding) name, after the norm (``k_weight``) and the rotation (``rotation`` float32[n, 2, half]: cosines
+    and sines of every position, ``positions`` int64) of the keys.  Queries [tokens, heads, dim] get theirs in the same pass.
+
+    k, v and q may be views whose rows are contiguous (parts of a projection's output).  Returns the queries (``q_out``, a new tensor
+    or q itself), None without q."""
+    c = _cache(codes, scales)
+    dev, dim = codes.device, c.dim
+    if not isinstance(k, torch.Tensor) or k.dtype not in _TYPES:
+        raise TypeError("k must be a float32, bfloat16 or float16 tensor")
+    tokens = k.shape[0] if k.dim() == 3 else None
+    a = _Append()
+    a.type = _TYPES[k.dtype]
+    a.k, a.k_token_stride, a.k_head_stride = _rows(k, "k", dev, k.dtype, tokens, c.kv_heads, dim)
+    a.v, a.v_token_stride, a.v_head_stride = _rows(v, "v", dev, k.dtype, tokens, c.kv_heads, dim)
+    a.tokens = tokens
+    a.slots = _on(dev, slots, torch.int64, (tokens,), "slots")
+    if q is not None:
+        a.q, a.q_token_stride, a.q_head_stride = _rows(q, "q", dev, k.dtype, tokens, None, dim)
+        a.heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        a.q_out, a.q_out_token_stride, a.q_out_head_stride = _rows(q_out, "q_out", dev, k.dtype, tokens, a.heads, dim)
+    elif q_out is not None or q_weight is not None:
+        raise ValueError("q_out and q_weight need q")
+    if rotation is not None:
+        if not isinstance(rotation, torch.Tensor) or rotation.dim() != 3 or rotation.shape[1] != 2:
+            raise ValueError("rotation must be [positions, 2, half]")
+        if positions is None:
+            raise ValueError("rotation needs positions")
+        a.rotation = _on(dev, rotation, torch.float32, rotation.shape, "rotation")
+        a.positions = _on(dev, positions, torch.int64, (tokens,), "positions")
+        a.n_positions, a.half, a.interleaved = rotation.shape[0], rotation.shape[2], bool(interleaved)
+    elif positions is not None:
+        raise ValueError("positions need a rotation")
+    if q_weight is not None:
+        a.q_weight = _on(dev, q_weight, torch.float32, (dim,), "q_weight")
+    if k_weight is not None:
+        a.k_weight = _on(dev, k_weight, torch.float32, (dim,), "k_weight")
+    a.eps = float(eps)
+    _enqueue(lib().dq8_cache_append, codes.get_device(), int(kind), ctypes.byref(c), ctypes.byref(a))
+    return q_out
+
+
+def _attention(q, codes, scales, pages, lens, starts, max_new, softmax_scale, window, out):
+    c = _cache(codes, scales)
+    dev, dim = codes.device, c.dim
+    if not isinstance(q, torch.Tensor) or q.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("q must be a bfloat16 or float16 tensor")
+    a = _Attention()
+    a.type = _TYPES[q.dtype]
+    a.q, a.q_token_stride, a.q_head_stride = _rows(q, "q", dev, q.dtype, None, None, dim)
+    a.tokens, a.heads = q.shape[0], q.shape[1]
+    if not isinstance(pages, torch.Tensor) or pages.dim() != 2:
+        raise ValueError("pages must be [sequences, pages of the longest]")
+    a.batch, a.max_pages = pages.shape
+    a.pages = _on(dev, pages, torch.int32, pages.shape, "pages")
+    a.lens = _on(dev, lens, torch.int32, (a.batch,), "lens")
+    if starts is not None:
+        a.starts = _on(dev, starts, torch.int32, (a.batch + 1,), "starts")
+    a.max_new = 0 if max_new is None else int(max_new)
+    a.window = int(window)
+    a.softmax_scale = dim ** -0.5 if softmax_scale is None else float(softmax_scale)
+    if out is not None:
+        a.out, a.out_token_stride, a.out_head_stride = _rows(out, "out", dev, q.dtype, a.tokens, a.heads, dim)
+    return c, a
+
+
+def cache_attention_workspace(q, codes, scales, pages, lens, starts=None, max_new=None):
+    """Bytes of scratch memory that cache_attention can use for these arguments."""
+    c, a = _attention(q, codes, scales, pages, lens, starts, max_new, None, 0, None)
+    with torch.cuda.device(codes.device):
+        return int(lib().dq8_cache_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(a)))
+
+
+def cache_attention(kind, q, codes, scales, pages, lens, starts=None, max_new=None, softmax_scale=None, window=0, out=None, workspace=None):
+    """Causal attention of new tokens q [tokens, heads, dim] (bfloat16 or float16) over the cached keys and values of their
+    sequences, several query heads per cached head.
+
+    pages int32 [sequences, n]: the page numbers of each sequence in order; lens int32 [sequences]: its cached tokens, the new ones
+    among them.  starts int32 [sequences + 1]: where each sequence's new tokens begin in q; None: every sequence has as many.
+    max_new: the largest number of new tokens of a sequence, where the host knows it.  window > 0: a query sees that many tokens at most.
+    workspace: a uint8 tensor of cache_attention_workspace() bytes; None: taken from torch's allocator, and not while the stream is
+    captured into a graph (hand one in there: without it few sequences are slow)."""
+    c, a = _attention(q, codes, scales, pages, lens, starts, max_new, softmax_scale, window, out)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=codes.device)
+        a.out, a.out_token_stride, a.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
+    if workspace is None:
+        with torch.cuda.device(codes.device):
+            if not torch.cuda.is_current_stream_capturing():
+                workspace = torch.empty(int(lib().dq8_cache_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(a))), dtype=torch.uint8,
+                                        device=codes.device)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
+        if workspace.device != codes.device:
+            raise ValueError("workspace is on another device than the cache")
+    _enqueue(lib().dq8_cache_attention, codes.get_device(), int(kind), ctypes.byref(c), ctypes.byref(a),
+             workspace.data_ptr() if workspace is not None and workspace.numel() else None, 0 if workspace is None else workspace.numel())
+    return out
 
 
 def model_speedup(n_gpus, total_ms, fc_ms, conv_penalty_ms, sub_batches, parallel_fc_ms, fc_penalty_ms):
