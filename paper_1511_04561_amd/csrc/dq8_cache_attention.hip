@@ -32,12 +32,13 @@ typedef float v4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;          // tokens that a wavefront takes at a time
-constexpr int kAttendWaves = 4;    // of a workgroup
+constexpr int kAttendWaves = 8;    // of a workgroup: they share one table
 constexpr int kAttendWg = kAttendWaves * kWave;
+constexpr uint32_t kLeastTiles = 2;  // of a wavefront's part, where there are as many
 constexpr int kQueryTop = 14;      // a query row's largest element is in [2^14, 2^15) in binary16
-constexpr int kWeightTop = 14;     // the largest value scale so far is in [2^14, 2^15) where it multiplies a weight
+constexpr int kWeightTop = 14;     // a weight times a value scale is below 2^15
 constexpr int kLeastExp = -90;     // of scales and queries that are still brought to those ranges
-constexpr float kNothing = -FLT_MAX;  // the running maximum before anything was seen
+constexpr float kNothing = -FLT_MAX;  // the largest score before anything was seen
 
 struct AttendArgs {
     const void *q;
@@ -51,9 +52,11 @@ struct AttendArgs {
     float entry;   // table entries are cb[c] * entry
     float factor;  // log2(e) * softmax_scale / entry
     // workspace (null: no job is split)
-    int4 *records;  // per workgroup: the job that begins there and is finished by others: sequence, job, parts
-    float2 *sums;   // per part: maximum and sum of weights of each query row
-    v4 *parts;      // per part: weighted values, one float4 per lane and block (see Blocks)
+    uint32_t *jobs; // how many there are
+    int4 *records;  // of each: sequence, number in it, the wavefront that begins it, parts (0: one wavefront does all of it)
+    float2 *sums;   // per part: largest score and sum of weights of each query row
+    float *parts;   // per part: weighted values [rows][DP]
+    uint32_t rows;  // query rows of a part, 16 NT or as many as a job has at most
 };
 
 // A sequence's part of the work.
@@ -89,7 +92,12 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, uint32_t b, uint32_
     return s;
 }
 
-__device__ __forceinline__ uint64_t work_of(const AttendArgs &a, const Seq &s) { return (uint64_t)s.q_tiles * a.kv_heads * s.tiles; }
+// Tiles and, in the upper half, jobs of a sequence.
+__device__ __forceinline__ uint64_t work_of(const AttendArgs &a, const Seq &s)
+{
+    const uint32_t jobs = s.q_tiles * a.kv_heads;
+    return (uint64_t)jobs << 32 | jobs * s.tiles;
+}
 
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v, uint32_t lane)
 {
@@ -101,66 +109,77 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v, uint32_t lane)
     return v;
 }
 
-// The tiles of all jobs, in the order of sequences, query groups, heads, tokens, are one line that is cut into equal parts, one per
-// workgroup: whatever the lengths of the sequences, everybody reads as much.  `at`: where this workgroup's part begins.
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// The tiles of all jobs, in the order of sequences, query groups, heads, tokens, are one line that is cut into parts that differ by
+// a tile at most, one per wavefront: whatever the lengths of the sequences, everybody reads as much.  (The host refuses work of
+// 2^31 tiles.)  Every wavefront finds its part by itself: a lane adds up a run of sequences, the runs are scanned, and then the
+// sequences of the run that holds the beginning.
 struct Share {
-    uint64_t total, begin, end;
-    uint32_t groups;  // workgroups that have a part
-    uint32_t b;       // sequence and place in its work of the first tile
-    uint64_t place;
+    uint32_t waves;        // wavefronts that have a part
+    uint32_t per, more;    // tiles of a part; the first `more` parts have one more
+    uint32_t begin, end;   // this wavefront's
+    uint32_t b, place;     // sequence that holds `begin`, and the place in its work
+    uint32_t before, jobs; // jobs of the sequences before it, and of all
+
+    // Wavefronts whose parts lie before or reach over place e > 0.
+    __device__ uint32_t upto(uint32_t e) const
+    {
+        const uint32_t longer = more * (per + 1);
+        return e <= longer ? (e + per) / (per + 1) : more + (e - longer + per - 1) / per;
+    }
 };
 
-__device__ __forceinline__ Share share_of(const AttendArgs &a, uint32_t rows, uint64_t *lds)
+__device__ __forceinline__ Share share_of(const AttendArgs &a, uint32_t rows, uint32_t w)
 {
-    // lds: kAttendWaves + 3 words
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63, run = (a.batch + kWave - 1) / kWave;
+    uint64_t mine = 0;
+    for (uint32_t i = 0; i < run; ++i) {
+        const uint32_t b = lane * run + i;
+        if (b < a.batch) mine += work_of(a, sequence(a, b, rows));
+    }
+    const uint64_t upto = wave_scan(mine, lane), all = lane_of(upto, 63);
+    const uint32_t total = (uint32_t)all;
     Share s;
-    uint64_t total = 0, mine = 0;
-    for (uint32_t b = threadIdx.x; b < a.batch; b += kAttendWg) mine += work_of(a, sequence(a, b, rows));
-    const uint64_t sum = wave_scan(mine, lane);
-    if (lane == 63) lds[wave] = sum;
-    __syncthreads();
-    for (int w = 0; w < kAttendWaves; ++w) total += lds[w];
-    s.total = total;
-    // at least a tile for every wavefront of a workgroup
-    const uint64_t most = (total + kAttendWaves - 1) / kAttendWaves;
-    s.groups = (uint32_t)(gridDim.x < most ? gridDim.x : most);
-    s.b = 0;
-    s.place = 0;
-    if (blockIdx.x >= s.groups) {
-        s.begin = s.end = 0;
-        return s;
-    }
-    s.begin = total * blockIdx.x / s.groups;
-    s.end = total * (blockIdx.x + 1) / s.groups;
-    // the sequence that holds `begin`
-    uint64_t before = 0;
-    for (uint32_t b0 = 0; b0 < a.batch; b0 += kAttendWg) {
-        __syncthreads();
-        const uint32_t b = b0 + threadIdx.x;
-        const uint64_t w = b < a.batch ? work_of(a, sequence(a, b, rows)) : 0;
-        const uint64_t upto = wave_scan(w, lane);
-        if (lane == 63) lds[wave] = upto;
-        __syncthreads();
-        uint64_t base = before;
-        for (uint32_t v = 0; v < wave; ++v) base += lds[v];
-        if (s.begin >= base + upto - w && s.begin < base + upto) {
-            lds[kAttendWaves + 1] = b;
-            lds[kAttendWaves + 2] = s.begin - (base + upto - w);
+    s.jobs = (uint32_t)(all >> 32);
+    const uint32_t most = (total + kLeastTiles - 1) / kLeastTiles;
+    s.waves = gridDim.x * kAttendWaves < most ? gridDim.x * kAttendWaves : most;
+    s.per = s.waves ? total / s.waves : 0;
+    s.more = total - s.per * s.waves;
+    s.b = s.place = s.begin = s.end = s.before = 0;
+    if (w >= s.waves) return s;
+    s.begin = w * s.per + (w < s.more ? w : s.more);
+    s.end = s.begin + s.per + (w < s.more);
+    const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)upto > s.begin));
+    uint64_t before = lane_of(upto - mine, owner);
+    s.b = (uint32_t)owner * run;
+    for (uint32_t i = 0; run > 1 && i < run; i += kWave) {
+        const uint32_t b = (uint32_t)owner * run + i + lane;
+        const uint64_t work = i + lane < run && b < a.batch ? work_of(a, sequence(a, b, rows)) : 0, sum = wave_scan(work, lane);
+        const uint64_t past = __builtin_amdgcn_ballot_w64((uint32_t)(before + sum) > s.begin);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            s.b = (uint32_t)owner * run + i + (uint32_t)l;
+            before += lane_of(sum - work, l);
+            break;
         }
-        for (int v = 0; v < kAttendWaves; ++v) before += lds[v];
-        if (s.begin < before) break;
+        before += lane_of(sum, 63);
     }
-    __syncthreads();
-    s.b = (uint32_t)lds[kAttendWaves + 1];
-    s.place = lds[kAttendWaves + 2];
+    s.b = uniform(s.b);
+    s.place = uniform(s.begin - (uint32_t)before);
+    s.before = uniform((uint32_t)(before >> 32));
     return s;
 }
 
 // Table with entries in binary16, in both halves of a word; see place_lut.
-__device__ __forceinline__ void place_half_table(const uint32_t *tab, float entry, uint32_t *lds)
+__device__ __forceinline__ void place_half_table(float value, float entry, uint32_t *lds)
 {
-    const _Float16 h = (_Float16)(u2f(tab[kCbOff + (threadIdx.x & 255)]) * entry);
+    const _Float16 h = (_Float16)(value * entry);
     uint16_t u;
     __builtin_memcpy(&u, &h, 2);
     place_lut<kAttendWg>(u2f(u | ((uint32_t)u << 16)), reinterpret_cast<float *>(lds));
@@ -178,6 +197,14 @@ __device__ __forceinline__ v8h eight(const uint32_t *lut, uint32_t lo, uint32_t 
 {
     return v8h{half_at<0>(lut, lo, lane4), half_at<1>(lut, lo, lane4), half_at<2>(lut, lo, lane4), half_at<3>(lut, lo, lane4),
                half_at<0>(lut, hi, lane4), half_at<1>(lut, hi, lane4), half_at<2>(lut, hi, lane4), half_at<3>(lut, hi, lane4)};
+}
+
+// Byte J of each of eight words.
+template <int J>
+__device__ __forceinline__ v8h eighth(const uint32_t *lut, const uint32_t (&w)[8], uint32_t lane4)
+{
+    return v8h{half_at<J>(lut, w[0], lane4), half_at<J>(lut, w[1], lane4), half_at<J>(lut, w[2], lane4), half_at<J>(lut, w[3], lane4),
+               half_at<J>(lut, w[4], lane4), half_at<J>(lut, w[5], lane4), half_at<J>(lut, w[6], lane4), half_at<J>(lut, w[7], lane4)};
 }
 
 __device__ __forceinline__ float max_over_groups(float v)
@@ -214,46 +241,6 @@ struct Bytes<16> {
     typedef uint32_t type __attribute__((ext_vector_type(4), aligned(16)));
 };
 
-// What a wavefront loads of a tile: lane l holds of keys the rows l % 16 of both halves of 16 tokens, 16 bytes of every 64, and
-// of values the bytes CPL (l % 16) .. of the eight tokens whose weights it will hold.
-template <int DP>
-struct TileData {
-    static constexpr int kLoads = DP / 64, CPL = DP / 16;
-    u4 k[2][kLoads];
-    typename Bytes<CPL>::type v[8];
-    v4 ks[2], vs[2];
-    uint32_t valid;  // bit h: half h lies on a page of the cache
-};
-
-template <int DP>
-__device__ __forceinline__ void fetch(const AttendArgs &a, const int32_t *table, uint32_t head, uint32_t tile, uint32_t lane, TileData<DP> &d)
-{
-    constexpr int CPL = DP / 16;
-    const uint32_t m = lane & 15, g = lane >> 4;
-    d.valid = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t token = tile * kTile + h * 16;
-        uint32_t index = token >> a.page_shift;
-        index = index < a.max_pages ? index : a.max_pages - 1;  // behind the last page: not seen by anybody
-        const uint32_t page = (uint32_t)__builtin_amdgcn_readfirstlane(table[index]);
-        const bool ok = page < a.n_pages;
-        d.valid |= ok ? 1u << h : 0;
-        const uint64_t row = ((((uint64_t)(ok ? page : 0) * a.kv_heads + head) << a.page_shift) + (token & ((1u << a.page_shift) - 1)));
-        const uint8_t *kc = a.k_codes + (row + m) * a.dim, *vc = a.v_codes + (row + 4 * g) * a.dim;
-#pragma unroll
-        for (int c = 0; c < TileData<DP>::kLoads; ++c) {
-            const uint32_t at = 64 * c + 16 * g;
-            d.k[h][c] = *reinterpret_cast<const u4 *>(kc + (at < a.dim ? at : 0));
-        }
-        const uint32_t at = m * CPL < a.dim ? m * CPL : 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d.v[4 * h + i] = *reinterpret_cast<const typename Bytes<CPL>::type *>(vc + (size_t)i * a.dim + at);
-        d.ks[h] = *reinterpret_cast<const v4 *>(a.k_scales + row + 4 * g);
-        d.vs[h] = *reinterpret_cast<const v4 *>(a.v_scales + row + 4 * g);
-    }
-}
-
 template <int N>
 __device__ __forceinline__ uint32_t word_of(const typename Bytes<N>::type &v, int i)
 {
@@ -263,65 +250,131 @@ __device__ __forceinline__ uint32_t word_of(const typename Bytes<N>::type &v, in
         return v[i];
 }
 
-// Weighted values (as sums of table entries) over the sum of weights; zeros where there was none.
-__device__ __forceinline__ v4 mean_of(const AttendArgs &a, v4 sum, float weights)
+// A load from a uniform address plus a lane's 32-bit byte offset.  The offset is made to look new each time, or its extension to 64 bits is
+// kept for the whole loop and added to the base by the vector unit: two registers and an instruction per load.
+template <typename T>
+__device__ __forceinline__ T load_at(const void *uniform_base, uint32_t byte)
 {
-    return weights == 0.0f ? v4{0, 0, 0, 0} : sum * (1.0f / (weights * a.entry));
+    asm volatile("" : "+v"(byte));
+    return *(const DQ8_GLOBAL T *)(uniform_global(static_cast<const char *>(uniform_base)) + byte);
 }
 
-// Where a query row's output goes: lane's column, block (tile j of 16 elements, group nt of 16 rows).
-template <typename T, int DP>
-__device__ __forceinline__ void store_block(const AttendArgs &a, const Seq &s, uint32_t head, uint32_t row, uint32_t j, v4 value, uint32_t lane)
-{
-    constexpr int CPL = DP / 16;
-    if (row >= s.n * a.group) return;
-    T *to = static_cast<T *>(a.out) + (s.first + row / a.group) * a.o_ts + (head * a.group + row % a.group) * a.o_hs;
+// The page numbers of 64 tiles from `first` on, in the lanes, so that a tile's addresses wait for no load.
+struct Pages {
+    const int32_t *table;
+    uint32_t page[2];  // lane l: of both halves of tile l of the 64
+
+    __device__ void load(const AttendArgs &a, uint32_t first, uint32_t lane)
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t d = CPL * (4 * (lane >> 4) + i) + j;
-        if (d < a.dim) to[d] = (T)value[i];
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t token = (first + lane) * kTile + h * 16, index = token >> a.page_shift;
+            page[h] = (uint32_t)table[index < a.max_pages ? index : a.max_pages - 1];  // behind the last page: not seen by anybody
+        }
+    }
+};
+
+// Where a wavefront is in its tiles: the one that is loaded next.
+struct Walk {
+    uint32_t tile, end, i;  // i: its lane in Pages
+    __device__ bool done() const { return tile >= end; }
+    __device__ void step(const AttendArgs &a, Pages &p, uint32_t lane)
+    {
+        ++tile;
+        if (++i == kWave && tile < end) {
+            p.load(a, tile, lane);
+            i = 0;
+        }
+    }
+};
+
+// What a wavefront loads of a tile: lane l holds of keys the rows l % 16 of both halves of 16 tokens, 16 bytes of every 64, and
+// of values the bytes CPL (l % 16) .. of the eight tokens whose weights it will hold, with the scales of the tokens of its scores.
+template <int DP>
+struct TileData {
+    static constexpr int KL = DP / 64, CPL = DP / 16;
+    u4 k[2][KL];
+    typename Bytes<CPL>::type v[8];
+    v4 ks[2], vs[2];
+    bool valid[2];  // whether the half's page is one of the cache
+};
+
+template <int DP>
+__device__ __forceinline__ void fetch(const AttendArgs &a, const Pages &p, uint32_t head, uint32_t lane, const Walk &w, TileData<DP> &d)
+{
+    constexpr uint32_t CPL = DP / 16;
+    const uint32_t n = lane & 15, g = lane >> 4;
+    const bool behind = w.done();
+    const uint32_t tile = behind ? w.tile - 1 : w.tile, i = behind ? w.i - 1 : w.i;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)p.page[h], (int)i), token = tile * kTile + h * 16;
+        d.valid[h] = page < a.n_pages;
+        const uint64_t row = (((uint64_t)(d.valid[h] ? page : 0) * a.kv_heads + head) << a.page_shift) + (token & ((1u << a.page_shift) - 1));
+        const uint8_t *kc = a.k_codes + row * a.dim, *vc = a.v_codes + row * a.dim;
+#pragma unroll
+        for (int c = 0; c < TileData<DP>::KL; ++c) d.k[h][c] = load_at<u4>(kc, behind ? 0 : n * a.dim + (64 * c + 16 * g < a.dim ? 64 * c + 16 * g : 0));
+        d.ks[h] = load_at<v4>(a.k_scales + row, 16 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) d.v[4 * h + r] = load_at<typename Bytes<CPL>::type>(vc, behind ? 0 : (4 * g + r) * a.dim + (n * CPL < a.dim ? n * CPL : 0));
+        d.vs[h] = load_at<v4>(a.v_scales + row, 16 * g);
     }
 }
 
 // One job's tiles t0 .. t1 - 1: query rows q_tile * 16 NT .. of a sequence against a cached head.  part: where the sums go if the job is
 // not finished here (-1: it is, and the output is stored).
+//
+template <int DP, int NT>
+constexpr bool kQueryInLds = DP * NT > 128;
+
 template <int DP, int NT, typename T>
-__device__ void attend(const AttendArgs &a, const Seq &s, uint32_t b, uint32_t q_tile, uint32_t head, uint32_t t0, uint32_t t1, int64_t part,
-                       const uint32_t *lut, float *area)
+__device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32_t b, uint32_t q_tile, uint32_t head, uint32_t t0, uint32_t t1, int32_t part,
+                       const uint32_t *lut, v8h *query)
 {
     constexpr int CPL = DP / 16, KS = DP / 32;
-    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, lane4 = lane * 4, wave = wave_in_wg();
-    const int32_t *table = a.pages + (size_t)b * a.max_pages;
-    v8h q[NT][KS];
-    float scale[NT], top[NT], sum[NT];
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, lane4 = lane * 4;
+    const uint32_t tile = s.lo_tile + t0, end = s.lo_tile + t1;
+    Pages pages;
+    pages.table = a.pages + (size_t)b * a.max_pages;
+    pages.load(a, tile, lane);
+
+    // The query rows as operands of the products, in registers or, where these are needed for the sums, in LDS: the lane's eight elements of
+    // step k of group nt.
+    v8h q[kQueryInLds<DP, NT> ? 1 : NT][KS];
+    float scale[NT], top[NT], sum[NT];  // top: the largest score so far; weights are exp2(score - top)
     int32_t pos[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const uint32_t row = (q_tile * NT + nt) * 16 + n;
         const bool in = row < s.n * a.group;
-        const uint32_t token = in ? row / a.group : 0, qh = in ? row % a.group : 0;
-        pos[nt] = in ? s.len - (int32_t)s.n + (int32_t)token : -1;
+        const uint32_t token = in ? row / a.group : 0, qh = in ? row - token * a.group : 0;
         const T *src = static_cast<const T *>(a.q) + (s.first + token) * a.q_ts + (head * a.group + qh) * a.q_hs;
-        float x[KS][8], most = 0.0f;
+        typedef T V __attribute__((ext_vector_type(8)));
+        typedef V VA __attribute__((aligned(sizeof(T))));
+        V x[KS];
+        float most = 0.0f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const uint32_t d = 16 * (g + 4 * (k / 2)) + 8 * (k % 2);
-            typedef T V __attribute__((ext_vector_type(8)));
-            typedef V VA __attribute__((aligned(sizeof(T))));
-            const bool there = in && d < a.dim;
-            V v = {};
-            if (there) v = *reinterpret_cast<const VA *>(src + d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[k][e] = (float)v[e];
-                most = fmaxf(most, fabsf(x[k][e]));
-            }
+            x[k] = V{};
+            if (in && d < a.dim) x[k] = *reinterpret_cast<const VA *>(src + d);
         }
-        const int e = exponent(max_over_groups(most));
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[nt][k][i] = (_Float16)__builtin_amdgcn_ldexpf(x[k][i], kQueryTop - e);
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)x[k][e]));
+        const int e = exponent(max_over_groups(most));
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            v8h h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = (_Float16)__builtin_amdgcn_ldexpf((float)x[k][i], kQueryTop - e);
+            if constexpr (kQueryInLds<DP, NT>)
+                query[(nt * KS + k) * kWave + lane] = h;
+            else
+                q[nt][k] = h;
+        }
+        pos[nt] = in ? s.len - (int32_t)s.n + (int32_t)token : -1;
         scale[nt] = __builtin_amdgcn_ldexpf(a.factor, e - kQueryTop);
         top[nt] = kNothing;
         sum[nt] = 0.0f;
@@ -331,235 +384,297 @@ __device__ void attend(const AttendArgs &a, const Seq &s, uint32_t b, uint32_t q
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < CPL; ++j) acc[nt][j] = v4{0, 0, 0, 0};
-    int vexp = kLeastExp;  // exponent of the largest value scale so far
+    // Weights times value scales have to fit binary16: the scales are multiplied by shrink = 2^(kWeightTop - vexp), where
+    // limit = 2^(vexp + 1) is above the largest so far.
+    int vexp = kLeastExp;
+    float shrink = __builtin_amdgcn_ldexpf(1.0f, kWeightTop - vexp), limit = __builtin_amdgcn_ldexpf(1.0f, vexp + 1);
     const int32_t p_first = s.len - (int32_t)s.n;  // position of the sequence's first query, the least of any row here
 
     auto work = [&](uint32_t tile, const TileData<DP> &d) {
-        const int32_t t = (int32_t)(tile * kTile);
-        // whether some row does not see some token of the tile (a window's lower end: rows up to the last position)
-        const bool masked = t + kTile - 1 > p_first || (a.window > 0 && t <= s.len - 1 - a.window) || d.valid != 3;
-        v4 st[NT][2];
-        v4 ks[2] = {d.ks[0], d.ks[1]}, vs[2] = {d.vs[0], d.vs[1]};
+        v4 st[NT][2], vs[2] = {d.vs[0], d.vs[1]};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) st[nt][h] = v4{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
+                if (k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
                 const v8h f = eight(lut, d.k[h][k / 2][2 * (k % 2)], d.k[h][k / 2][2 * (k % 2) + 1], lane4);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) st[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[nt][k], st[nt][h], 0, 0, 0);
+                for (int nt = 0; nt < NT; ++nt) st[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, kQueryInLds<DP, NT> ? query[(nt * KS + k) * kWave + lane] : q[kQueryInLds<DP, NT> ? 0 : nt][k], st[nt][h], 0, 0, 0);
             }
         }
-        if (masked) {  // scales of tokens that nobody here sees do not count
+        const int32_t t = (int32_t)(tile * kTile);
+        // whether some row does not see some token of the tile (a window's lower end: rows up to the last position)
+        const bool masked = t + kTile - 1 > p_first || (a.window > 0 && t <= s.len - 1 - a.window) || !d.valid[0] || !d.valid[1];
+        if (masked) {  // scales of tokens that nobody sees do not count
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (t + 16 * h + 4 * (int32_t)g + i >= s.len || !(d.valid >> h & 1)) vs[h][i] = 0.0f;
+                for (int r = 0; r < 4; ++r)
+                    if (t + 16 * h + 4 * (int32_t)g + r >= s.len || !d.valid[h]) vs[h][r] = 0.0f;
         }
-        float most = 0.0f;
+        float large = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, vs[h][i]);
-        const int e = __builtin_amdgcn_readfirstlane(exponent(max_over_groups(most)));
-        if (e > vexp) {
+            for (int r = 0; r < 4; ++r) large = fmaxf(large, vs[h][r]);
+        if (__builtin_amdgcn_ballot_w64(large >= limit) != 0) {
+            const int e = (int)uniform((uint32_t)exponent(max_over_groups(large)));
+            if (e > vexp) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int j = 0; j < CPL; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nt][j][i] = __builtin_amdgcn_ldexpf(acc[nt][j][i], vexp - e);
-            vexp = e;
+                    for (int j = 0; j < CPL; ++j) acc[nt][j] *= __builtin_amdgcn_ldexpf(1.0f, vexp - e);
+                vexp = e;
+                shrink = __builtin_amdgcn_ldexpf(1.0f, kWeightTop - vexp);
+                limit = __builtin_amdgcn_ldexpf(1.0f, vexp + 1);
+            }
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vs[h][i] = __builtin_amdgcn_ldexpf(vs[h][i], kWeightTop - vexp);
+        vs[0] *= shrink;
+        vs[1] *= shrink;
         v8h p[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float high = kNothing;
+            float x[2][4], c[2][4], y[2][4], w[2][4];  // scores x c, value scales, weights
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v = st[nt][h][i] * (ks[h][i] * scale[nt]);
-                    if (masked) {
-                        const int32_t token = t + 16 * h + 4 * (int32_t)g + i;
-                        const bool seen = token <= pos[nt] && (a.window <= 0 || token > pos[nt] - a.window) && (d.valid >> h & 1);
-                        v = seen ? v : -__builtin_inff();
-                    }
-                    st[nt][h][i] = v;
-                    high = fmaxf(high, v);
+                for (int r = 0; r < 4; ++r) {
+                    x[h][r] = st[nt][h][r];
+                    c[h][r] = d.ks[h][r] * scale[nt];
+                    y[h][r] = vs[h][r];
                 }
-            if (__builtin_amdgcn_ballot_w64(high > top[nt]) != 0) {
+            if (masked) {  // hidden tokens: weight zero, whatever their scales are
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int32_t token = t + 16 * h + 4 * (int32_t)g + r;
+                        if (!(token <= pos[nt] && (a.window <= 0 || token > pos[nt] - a.window) && d.valid[h])) {
+                            x[h][r] = -__builtin_inff();
+                            c[h][r] = 1.0f;
+                            y[h][r] = 0.0f;
+                        }
+                    }
+            }
+            auto weigh = [&]() {
+                float high = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        w[h][r] = __builtin_amdgcn_exp2f(x[h][r] * c[h][r] - top[nt]);
+                        high = fmaxf(high, w[h][r]);
+                    }
+                return high;
+            };
+            if (__builtin_amdgcn_ballot_w64(weigh() > 1.0f) != 0) {  // a score above the largest so far
+                float high = kNothing;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) high = fmaxf(high, x[h][r] * c[h][r]);
                 const float now = fmaxf(top[nt], max_over_groups(high)), less = __builtin_amdgcn_exp2f(top[nt] - now);
+                top[nt] = now;
                 sum[nt] *= less;
 #pragma unroll
-                for (int j = 0; j < CPL; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nt][j][i] *= less;
-                top[nt] = now;
+                for (int j = 0; j < CPL; ++j) acc[nt][j] *= less;
+                weigh();
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(st[nt][h][i] - top[nt]);
-                    sum[nt] += w;
-                    // a hidden token's scale may be anything, and its weight is zero
-                    p[nt][4 * h + i] = (_Float16)(masked && !(st[nt][h][i] > -__builtin_inff() || st[nt][h][i] != st[nt][h][i]) ? 0.0f : w * vs[h][i]);
+                for (int r = 0; r < 4; ++r) {
+                    sum[nt] += w[h][r];
+                    p[nt][4 * h + r] = (_Float16)(w[h][r] * y[h][r]);
                 }
         }
 #pragma unroll
-        for (int j = 0; j < CPL; ++j) {
-            // byte j of the eight tokens' words
-            v8h f;
-            const uint32_t sel = 0x0C0C0400u + ((j & 3) << 8);
+        for (int j4 = 0; j4 < CPL / 4; ++j4) {
+            uint32_t word[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                f[i] = *reinterpret_cast<const _Float16 *>(reinterpret_cast<const char *>(lut) +
-                                                           __builtin_amdgcn_perm(word_of<CPL>(d.v[i], j / 4), lane4, sel));
+            for (int r = 0; r < 8; ++r) word[r] = word_of<CPL>(d.v[r], j4);
+            __builtin_amdgcn_sched_barrier(0);
+            const v8h f0 = eighth<0>(lut, word, lane4), f1 = eighth<1>(lut, word, lane4);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, p[nt], acc[nt][j], 0, 0, 0);
+            for (int nt = 0; nt < NT; ++nt) {
+                acc[nt][4 * j4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f0, p[nt], acc[nt][4 * j4], 0, 0, 0);
+                acc[nt][4 * j4 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f1, p[nt], acc[nt][4 * j4 + 1], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const v8h f2 = eighth<2>(lut, word, lane4), f3 = eighth<3>(lut, word, lane4);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                acc[nt][4 * j4 + 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f2, p[nt], acc[nt][4 * j4 + 2], 0, 0, 0);
+                acc[nt][4 * j4 + 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f3, p[nt], acc[nt][4 * j4 + 3], 0, 0, 0);
+            }
         }
     };
 
-    uint32_t tile = s.lo_tile + t0 + wave;
-    const uint32_t end = s.lo_tile + t1;
-    if (tile < end) {
-        TileData<DP> x, y;
-        fetch<DP>(a, table, head, tile, lane, x);
-        for (;;) {
-            uint32_t next = tile + kAttendWaves;
-            fetch<DP>(a, table, head, next < end ? next : tile, lane, y);
-            work(tile, x);
-            if (next >= end) break;
-            tile = next;
-            next = tile + kAttendWaves;
-            fetch<DP>(a, table, head, next < end ? next : tile, lane, x);
-            work(tile, y);
-            if (next >= end) break;
-            tile = next;
-        }
+    // The next tile's loads are in flight while a wavefront works on the present one.  They are issued without a condition (a
+    // branch around them makes the waits for older loads wait for all); behind the last tile all lanes load its first row.
+    Walk walk{tile, end, 0};
+    TileData<DP> x, y;
+    fetch<DP>(a, pages, head, lane, walk, x);
+    for (;;) {
+        const uint32_t one = walk.tile;
+        walk.step(a, pages, lane);
+        fetch<DP>(a, pages, head, lane, walk, y);
+        work(one, x);
+        if (walk.done()) break;
+        const uint32_t two = walk.tile;
+        walk.step(a, pages, lane);
+        fetch<DP>(a, pages, head, lane, walk, x);
+        work(two, y);
+        if (walk.done()) break;
     }
 
-    // The four wavefronts' sums become one: maxima and sums of weights first, then the weighted values, four blocks of 16 x 16 at a time,
-    // of which every wavefront adds one.
-    float2 *ml = reinterpret_cast<float2 *>(area);
-    __syncthreads();  // (the area may still be read for the job before)
+    // A lane has elements 16 x (4 g + i) / 16 .. of its row: CPL neighbours for each i.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         sum[nt] = sum_over_groups(sum[nt]);
-        if (g == 0) ml[(wave * NT + nt) * 16 + n] = float2{top[nt], sum[nt]};
-    }
-    __syncthreads();
-    float all[NT], whole[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        all[nt] = kNothing;
-        whole[nt] = 0.0f;
-        for (int w = 0; w < kAttendWaves; ++w) all[nt] = fmaxf(all[nt], ml[(w * NT + nt) * 16 + n].x);
-        for (int w = 0; w < kAttendWaves; ++w) {
-            const float2 o = ml[(w * NT + nt) * 16 + n];
-            whole[nt] += o.y * __builtin_amdgcn_exp2f(o.x - all[nt]);
-        }
-        const float mine = __builtin_amdgcn_exp2f(top[nt] - all[nt]);
-#pragma unroll
-        for (int j = 0; j < CPL; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[nt][j][i] = __builtin_amdgcn_ldexpf(acc[nt][j][i] * mine, vexp - kWeightTop);
-    }
-    if (part >= 0 && wave == 0 && g == 0)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) a.sums[(size_t)part * NT * 16 + nt * 16 + n] = float2{all[nt], whole[nt]};
-    v4 *blocks = reinterpret_cast<v4 *>(area);
-#pragma unroll
-    for (int c = 0; c < CPL * NT; c += 4) {  // block c + u: group (c + u) % NT, tile (c + u) / NT
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) blocks[(u * kAttendWaves + wave) * kWave + lane] = acc[(c + u) % NT][(c + u) / NT];
-        __syncthreads();
-        v4 v = {0, 0, 0, 0};
-        for (int w = 0; w < kAttendWaves; ++w) v += blocks[(wave * kAttendWaves + w) * kWave + lane];
-        const uint32_t at = c + wave, nt = at % NT, j = at / NT;
+        const uint32_t local = nt * 16 + n, row = q_tile * NT * 16 + local;
+        const float size = __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop);
+        if (row >= s.n * a.group) continue;
         if (part >= 0) {
-            a.parts[((size_t)part * CPL * NT + at) * kWave + lane] = v;
-        } else {
-            float l = 0.0f;
+            const size_t at = (size_t)part * a.rows + local;
+            if (g == 0) a.sums[at] = float2{top[nt], sum[nt]};
 #pragma unroll
-            for (int i = 0; i < NT; ++i) l = i == (int)nt ? whole[i] : l;
-            store_block<T, DP>(a, s, head, (q_tile * NT + nt) * 16 + n, j, mean_of(a, v, l), lane);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < CPL; j += 4)
+                    *reinterpret_cast<v4 *>(a.parts + at * DP + CPL * (4 * g + i) + j) =
+                        v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * size;
+        } else {
+            const uint32_t token = row / a.group;
+            T *to = static_cast<T *>(a.out) + (s.first + token) * a.o_ts + (head * a.group + row - token * a.group) * a.o_hs;
+            const float r = sum[nt] == 0.0f ? 0.0f : size / (sum[nt] * a.entry);
+            typedef T V __attribute__((ext_vector_type(4)));
+            typedef V VA __attribute__((aligned(sizeof(T))));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < CPL; j += 4) {
+                    const uint32_t d = CPL * (4 * g + i) + j;
+                    const v4 m = v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * r;
+                    if (d < a.dim) *reinterpret_cast<VA *>(to + d) = V{(T)m.x, (T)m.y, (T)m.z, (T)m.w};
+                }
         }
     }
 }
 
 template <int DP, int NT, typename T>
-__global__ __launch_bounds__(kAttendWg) void k_cache_attend(const uint32_t *__restrict__ tab, AttendArgs a)
+__global__ __launch_bounds__(kAttendWg, 2) void k_cache_attend(const uint32_t *__restrict__ tab, AttendArgs a)
 {
-    __shared__ __align__(256) uint32_t lds[256 * kLutCopies + 4096];
-    float *area = reinterpret_cast<float *>(lds + 256 * kLutCopies);
-    place_half_table(tab, a.entry, lds);
-    const Share share = share_of(a, 16 * NT, reinterpret_cast<uint64_t *>(area));
+    __shared__ __align__(256) uint32_t lds[256 * kLutCopies];
+    __shared__ v8h queries[kQueryInLds<DP, NT> ? kAttendWaves * NT * (DP / 32) * kWave : 1];
+    const uint32_t wave = wave_in_wg(), w = blockIdx.x * kAttendWaves + wave;
+    v8h *const query = queries + (kQueryInLds<DP, NT> ? wave * NT * (DP / 32) * kWave : 0);
+    place_half_table(request_lut(tab), a.entry, lds);
+    const Share share = share_of(a, 16 * NT, w);
     __syncthreads();
-    uint32_t b = (uint32_t)__builtin_amdgcn_readfirstlane(share.b);
-    uint64_t place = share.place, at = share.begin;
-    int4 record = {0, 0, 0, 0};
+    if (a.parts && w == 0 && (threadIdx.x & 63) == 0) *a.jobs = share.jobs;
+    uint32_t b = share.b, place = share.place, at = share.begin, before = share.before;
     while (at < share.end && b < a.batch) {
         const Seq s = sequence(a, b, 16 * NT);
         const uint64_t work = work_of(a, s);
-        if (place >= work) {  // the next sequence
+        if (place >= (uint32_t)work) {  // the next sequence
+            before += (uint32_t)(work >> 32);
             ++b;
             place = 0;
             continue;
         }
-        const uint32_t job = (uint32_t)(place / s.tiles);
-        uint32_t t0 = (uint32_t)(place % s.tiles), t1 = s.tiles;
-        const uint64_t left = share.end - at;
-        int64_t part = -1;
+        const uint32_t job = uniform(place / s.tiles), t0 = uniform(place - job * s.tiles);
+        uint32_t t1 = s.tiles;
+        int32_t part = -1;
         if (a.parts) {
-            if (left < t1 - t0) t1 = t0 + (uint32_t)left;
-            if (t0 > 0 || t1 < s.tiles) part = 2 * (int64_t)blockIdx.x + (t0 == 0);
-            if (t0 == 0 && t1 < s.tiles) {  // finished by the workgroups whose parts reach the job's end
-                const uint64_t end = at + s.tiles;
-                record = int4{(int)b, (int)job, (int)((end * share.groups + share.total - 1) / share.total - blockIdx.x), 0};
-            }
-            attend<DP, NT, T>(a, s, b, job / a.kv_heads, job % a.kv_heads, t0, t1, part, lds, area);
-        } else if (t0 == 0) {  // whole jobs: those that begin in this part
-            attend<DP, NT, T>(a, s, b, job / a.kv_heads, job % a.kv_heads, t0, t1, -1, lds, area);
+            const uint32_t left = share.end - at;
+            if (left < t1 - t0) t1 = t0 + left;
+            if (t0 > 0 || t1 < s.tiles) part = 2 * (int32_t)w + (t0 == 0);
+            if (t0 == 0 && (threadIdx.x & 63) == 0)  // where it does not end here: the wavefronts whose parts reach its end
+                a.records[before + job] = int4{(int)b, (int)job, (int)w, t1 < s.tiles ? (int)(share.upto(at + s.tiles) - w) : 0};
         }
+        // without a workspace, whole jobs: those that begin in this part
+        if (a.parts || t0 == 0) attend<DP, NT, T>(a, s, b, job / a.kv_heads, job % a.kv_heads, t0, t1, part, lds, query);
         place += t1 - t0;
         at += t1 - t0;
     }
-    if (a.parts && threadIdx.x == 0) a.records[blockIdx.x] = record;
 }
 
-// A job that several workgroups worked on: workgroup w of this launch joins the parts of the job that began in workgroup w of the
-// other.
-template <int DP, int NT, typename T>
-__global__ __launch_bounds__(kAttendWg) void k_cache_join(AttendArgs a)
+// The jobs that several wavefronts worked on, one per workgroup in x, kSlice of its rows in y.  A part lies far away (another die's
+// cache wrote it), so that what counts is how many loads are in flight: a thread has four elements of a row, groups of threads take
+// every so manieth part, and the groups' sums are added in LDS.
+constexpr int kSlice = 4, kJoinParts = 256;
+
+template <int DP, int NT, int WG, typename T>
+__global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
 {
-    constexpr int CPL = DP / 16;
+    constexpr uint32_t ROWS = 16 * NT, QUADS = DP / 4, CELLS = kSlice * QUADS, GROUPS = WG / CELLS;
+    static_assert(WG % CELLS == 0, "whole groups");
+    __shared__ float factor[kJoinParts * kSlice];  // of a part and row: exp2(its largest score - the largest of all)
+    __shared__ float largest[kSlice], weights[kSlice];
+    __shared__ v4 sums[WG];
+    if (blockIdx.x >= *a.jobs) return;
     const int4 record = a.records[blockIdx.x];
-    if (record.z == 0) return;
-    const uint32_t lane = threadIdx.x & 63, n = lane & 15, wave = wave_in_wg();
-    const Seq s = sequence(a, (uint32_t)record.x, 16 * NT);
+    const uint32_t w = (uint32_t)record.z, parts = (uint32_t)record.w;
+    if (parts == 0) return;
+    auto part_of = [&](uint32_t i) { return 2 * ((size_t)w + i) + (i == 0); };
+    const Seq s = sequence(a, (uint32_t)record.x, ROWS);
     const uint32_t head = (uint32_t)record.y % a.kv_heads, q_tile = (uint32_t)record.y / a.kv_heads;
-    auto part_of = [&](int i) { return 2 * ((size_t)blockIdx.x + i) + (i == 0); };
-    for (uint32_t at = wave; at < CPL * NT; at += kAttendWaves) {
-        const uint32_t nt = at % NT, j = at / NT;
+    const uint32_t left = s.n * a.group - q_tile * ROWS, rows = left < ROWS ? left : ROWS;  // of this job
+    const uint32_t first = blockIdx.y * kSlice;
+    if (first >= rows) return;
+    if (threadIdx.x < kSlice * kWave) {  // a wavefront looks at a row's parts
+        const uint32_t row = first + (threadIdx.x >> 6);
         float top = kNothing, l = 0.0f;
-        for (int i = 0; i < record.z; ++i) top = fmaxf(top, a.sums[part_of(i) * NT * 16 + nt * 16 + n].x);
-        v4 v = {0, 0, 0, 0};
-        for (int i = 0; i < record.z; ++i) {
-            const float2 o = a.sums[part_of(i) * NT * 16 + nt * 16 + n];
-            const float f = __builtin_amdgcn_exp2f(o.x - top);
-            l += o.y * f;
-            v += a.parts[(part_of(i) * CPL * NT + at) * kWave + lane] * f;
+        if (row < rows)
+            for (uint32_t i = threadIdx.x & 63; i < parts; i += kWave) {
+                const float2 o = a.sums[part_of(i) * a.rows + row];
+                const float now = fmaxf(top, o.x);
+                l = l * __builtin_amdgcn_exp2f(top - now) + o.y * __builtin_amdgcn_exp2f(o.x - now);
+                top = now;
+            }
+        float all = top;
+#pragma unroll
+        for (int m = 1; m < kWave; m *= 2) all = fmaxf(all, __shfl_xor(all, m));
+        l *= __builtin_amdgcn_exp2f(top - all);
+#pragma unroll
+        for (int m = 1; m < kWave; m *= 2) l += __shfl_xor(l, m);
+        if ((threadIdx.x & 63) == 0) {
+            largest[threadIdx.x >> 6] = all;
+            weights[threadIdx.x >> 6] = l;
         }
-        store_block<T, DP>(a, s, head, (q_tile * NT + nt) * 16 + n, j, mean_of(a, v, l), lane);
+    }
+    const uint32_t group = threadIdx.x / CELLS, cell = threadIdx.x % CELLS, row = cell / QUADS, d = 4 * (cell % QUADS);
+    const bool mine = first + row < rows;
+    const float *p = a.parts + (size_t)(first + row) * DP + d;
+    v4 v = {0, 0, 0, 0};
+    for (uint32_t i0 = 0; i0 < parts; i0 += kJoinParts) {
+        const uint32_t some = parts - i0 < kJoinParts ? parts - i0 : kJoinParts;
+        __syncthreads();
+        for (uint32_t x = threadIdx.x; x < some * kSlice; x += WG)
+            if (first + x % kSlice < rows)
+                factor[x] = __builtin_amdgcn_exp2f(a.sums[part_of(i0 + x / kSlice) * a.rows + first + x % kSlice].x - largest[x % kSlice]);
+        __syncthreads();
+        if (mine) {
+#pragma unroll 4
+            for (uint32_t i = group; i < some; i += GROUPS) v += *reinterpret_cast<const v4 *>(p + part_of(i0 + i) * a.rows * DP) * factor[i * kSlice + row];
+        }
+    }
+    if (GROUPS > 1) {
+        sums[threadIdx.x] = v;
+        __syncthreads();
+    }
+    if (group == 0 && mine && d < a.dim) {
+#pragma unroll
+        for (uint32_t o = 1; o < GROUPS; ++o) v += sums[o * CELLS + cell];
+        const float r = weights[row] == 0.0f ? 0.0f : 1.0f / (weights[row] * a.entry);
+        const uint32_t at = q_tile * ROWS + first + row, token = at / a.group;
+        typedef T V __attribute__((ext_vector_type(4)));
+        typedef V VA __attribute__((aligned(sizeof(T))));
+        T *to = static_cast<T *>(a.out) + (s.first + token) * a.o_ts + (head * a.group + at - token * a.group) * a.o_hs;
+        *reinterpret_cast<VA *>(to + d) = V{(T)(v.x * r), (T)(v.y * r), (T)(v.z * r), (T)(v.w * r)};
     }
 }
 
@@ -567,6 +682,9 @@ __global__ __launch_bounds__(kAttendWg) void k_cache_join(AttendArgs a)
 struct Shape {
     int dp, nt;        // padded head length, groups of 16 query rows
     unsigned groups;   // workgroups
+    size_t jobs, work; // jobs and tiles, at most
+    unsigned rows;     // query rows of a job, at most
+    bool many;         // whether a job is cut into more than about sixteen parts
 };
 
 Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
@@ -577,22 +695,25 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     size_t new_tokens = a.starts ? (a.max_new ? a.max_new : a.tokens) : a.tokens / a.batch;
     if (new_tokens > a.tokens) new_tokens = a.tokens;
     const size_t rows = new_tokens * group;
-    s.nt = rows <= 16 ? 1 : rows <= 32 || s.dp == 256 ? 2 : 4;
+    s.nt = rows <= 16 || s.dp == 256 ? 1 : 2;
     // as many as are resident; no more than the work can give a tile per wavefront
     const size_t per = 16 * (size_t)s.nt;
     const size_t jobs = (a.tokens * group / per + a.batch) * (size_t)c->kv_heads;
     const size_t tiles = (a.max_pages * (size_t)c->page_size + kTile - 1) / kTile;
-    const size_t most = jobs > dq8::kCacheLimit / tiles ? dq8::kCacheLimit : jobs * tiles;
-    size_t groups = (size_t)cus * 2;
-    const size_t useful = (most + kAttendWaves - 1) / kAttendWaves;
+    s.work = jobs > SIZE_MAX / 2 / tiles ? SIZE_MAX / 2 : jobs * tiles;
+    size_t groups = (size_t)cus;  // one table per compute unit, eight wavefronts of 256 registers
+    const size_t useful = (s.work + kAttendWaves * kLeastTiles - 1) / (kAttendWaves * kLeastTiles);
     if (groups > useful) groups = useful;
     s.groups = (unsigned)groups;
+    s.jobs = jobs;
+    s.many = jobs * 16 <= groups * kAttendWaves;
+    s.rows = (unsigned)(!a.starts && rows < per ? rows : per);
     return s;
 }
 
-size_t record_bytes(const Shape &s) { return (s.groups * sizeof(int4) + 255) / 256 * 256; }
-size_t sums_bytes(const Shape &s) { return (size_t)s.groups * 2 * s.nt * 16 * sizeof(float2); }
-size_t parts_bytes(const Shape &s) { return (size_t)s.groups * 2 * (s.dp / 16) * s.nt * kWave * sizeof(v4); }
+size_t record_bytes(const Shape &s) { return (1 + s.jobs) * sizeof(int4); }  // their number takes the first
+size_t sums_bytes(const Shape &s) { return (size_t)s.groups * kAttendWaves * 2 * s.rows * sizeof(float2); }  // (a multiple of 16)
+size_t parts_bytes(const Shape &s) { return (size_t)s.groups * kAttendWaves * 2 * s.rows * s.dp * sizeof(float); }
 
 // What does not look at the arrays of the call.  0 tokens or sequences pass: such a call launches nothing.
 int check_shape(const char *who, int kind, const dq8_cache *cache, const dq8_attention *in)
@@ -644,13 +765,17 @@ int check_arrays(const char *who, const dq8_cache *cache, const dq8_attention &a
 }
 
 template <int DP, int NT>
-int launch(int type, const uint32_t *tab, const AttendArgs &k, unsigned groups, hipStream_t stream)
+int launch(int type, const uint32_t *tab, const AttendArgs &k, const Shape &s, hipStream_t stream)
 {
 #define DQ8_ATTEND(T)                                                                                                      \
-    hipLaunchKernelGGL((k_cache_attend<DP, NT, T>), dim3(groups), dim3(kAttendWg), 0, stream, tab, k);                    \
+    hipLaunchKernelGGL((k_cache_attend<DP, NT, T>), dim3(s.groups), dim3(kAttendWg), 0, stream, tab, k);                  \
     int rc = dq8::after_launch_of("k_cache_attend", stream);                                                              \
     if (rc || !k.parts) return rc;                                                                                        \
-    hipLaunchKernelGGL((k_cache_join<DP, NT, T>), dim3(groups), dim3(kAttendWg), 0, stream, k);                            \
+    const dim3 grid((unsigned)s.jobs, (s.rows + kSlice - 1) / kSlice);                                                    \
+    if (s.many)                                                                                                           \
+        hipLaunchKernelGGL((k_cache_join<DP, NT, 1024, T>), grid, dim3(1024), 0, stream, k);                              \
+    else                                                                                                                  \
+        hipLaunchKernelGGL((k_cache_join<DP, NT, 256, T>), grid, dim3(256), 0, stream, k);                                \
     return dq8::after_launch_of("k_cache_join", stream);
     if (type == DQ8_BFLOAT16) {
         DQ8_ATTEND(__bf16)
@@ -687,6 +812,7 @@ int dq8_cache_attention(int kind, const dq8_cache *cache, const dq8_attention *i
     rc = dq8::device_tables(kind, &dev);
     if (rc) return rc;
     const Shape s = shape_of(cache, a, dev.cus);
+    if (s.work >= dq8::kCacheLimit) return dq8::failed(DQ8_ERR_ARG, "%s: too much work for one call (tokens, heads and pages)", who);
     AttendArgs k;
     k.q = a.q, k.out = a.out, k.q_ts = a.q_token_stride, k.q_hs = a.q_head_stride, k.o_ts = a.out_token_stride, k.o_hs = a.out_head_stride;
     const size_t half = dq8::cache_rows(cache) / 2;
@@ -700,24 +826,23 @@ int dq8_cache_attention(int kind, const dq8_cache *cache, const dq8_attention *i
     k.window = a.window;
     k.entry = kind == DQ8_LINEAR ? 127.0f * 256.0f : 1280.0f * 32.0f;
     k.factor = a.softmax_scale * 1.44269504088896340736f / k.entry;
-    k.records = nullptr, k.sums = nullptr, k.parts = nullptr;
+    k.rows = s.rows;
+    k.jobs = nullptr, k.records = nullptr, k.sums = nullptr, k.parts = nullptr;
     if (workspace && workspace_bytes >= record_bytes(s) + sums_bytes(s) + parts_bytes(s)) {
         char *w = static_cast<char *>(workspace);
-        k.records = reinterpret_cast<int4 *>(w);
+        k.jobs = reinterpret_cast<uint32_t *>(w);
+        k.records = reinterpret_cast<int4 *>(w) + 1;
         k.sums = reinterpret_cast<float2 *>(w + record_bytes(s));
-        k.parts = reinterpret_cast<v4 *>(w + record_bytes(s) + sums_bytes(s));
+        k.parts = reinterpret_cast<float *>(w + record_bytes(s) + sums_bytes(s));
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
 #define DQ8_ATTEND_SHAPE(DP, NT) \
-    if (s.dp == DP && s.nt == NT) return launch<DP, NT>(a.type, dev.tab, k, s.groups, stream);
+    if (s.dp == DP && s.nt == NT) return launch<DP, NT>(a.type, dev.tab, k, s, stream);
     DQ8_ATTEND_SHAPE(64, 1)
     DQ8_ATTEND_SHAPE(64, 2)
-    DQ8_ATTEND_SHAPE(64, 4)
     DQ8_ATTEND_SHAPE(128, 1)
     DQ8_ATTEND_SHAPE(128, 2)
-    DQ8_ATTEND_SHAPE(128, 4)
     DQ8_ATTEND_SHAPE(256, 1)
-    DQ8_ATTEND_SHAPE(256, 2)
 #undef DQ8_ATTEND_SHAPE
     return dq8::failed(DQ8_ERR_ARG, "%s: no kernel", who);
 }

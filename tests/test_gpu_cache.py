@@ -266,14 +266,15 @@ def test_attention_of_bad_pages_lengths_and_starts(dq8):
     check_attention(got, q, want, tol)
     assert not got[2].any()  # none of its pages is one
     # starts that descend or leave the range: no access outside.  Sequence 2 counts as tokens 0 .. 2 here and sees none of its
-    # pages, so that token 0 is sequence 0's or zero
+    # pages, so that each head of token 0 is sequence 0's or zero
     bad = starts.copy()
     bad[2], bad[4] = -7, 2 ** 31 - 1
     out = torch.zeros_like(q, device="cuda")
     dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(bad), out=out)
     assert torch.isfinite(out).all() and not out[1:3].any()
-    if out[:1].any():
-        check_attention(out[:1], q, want[:1], tol[:1])
+    for h in range(heads):
+        if out[0, h].any():
+            check_attention(out[:1, h:h + 1], q, want[:1, h:h + 1], tol[:1, h:h + 1])
     negative = dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(np.full(4, -3, np.int32)), starts=cuda(starts))
     assert not negative.any()
 
