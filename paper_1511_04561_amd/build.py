@@ -17,7 +17,7 @@ BINDING = os.path.join(HERE, "_binding.so")  # Python extension over torch's C++
 BINDING_SOURCE = os.path.join(CSRC, "dq8_binding.cpp")
 SOURCES = ["dq8.hip", "dq8_avg_short.hip", "dq8_avg_long.hip", "dq8_cache_append.hip", "dq8_cache_attention.hip", "dq8_tables.cpp"]
 HEADERS = ["dq8_internal.h", "dq8_launch.hpp", "dq8_tables.hpp", "dq8_device.hpp", "dq8_plan.hpp", "dq8_units.hpp", "dq8_arith.hpp", "dq8_kernels_codec.hpp", "dq8_kernels_avg.hpp",
-           "dq8_kernels_avg_encode.hpp", "dq8_kernels_stats.hpp", "dq8_kernels_small.hpp", "dq8_kernels_segments.hpp", "dq8_cache_check.hpp", os.path.join(ROOT, "include", "dq8.h"),
+           "dq8_kernels_avg_encode.hpp", "dq8_kernels_stats.hpp", "dq8_kernels_small.hpp", "dq8_kernels_segments.hpp", "dq8_cache_check.hpp", "dq8_kernels_attend.hpp", "dq8_kernels_attend_chunk.hpp", os.path.join(ROOT, "include", "dq8.h"),
            os.path.join(ROOT, "include", "dq8_workspace.h"), os.path.join(ROOT, "include", "dq8_cache.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -49,7 +49,8 @@ def attention(kind, cache, q, pages, lens, starts, softmax_scale, window=0):
       the row, and sums in binary32 add less than (dim + 8) 2^-24 of the same;
       a weight over the sum of weights is off by 2 E' relative, E' = E and those sums, to first order, and by u for its rounding;
       a value by u: |out - exact| <= sum_j w_j |v_j| (2 u + 2 E' + (8 + len) 2^-24) (1 + 2^-5), the last factor for second orders (E' < 2^-6 in these tests);
-      a weight under the normal range of binary16 by 2^-25 of a scale at which the largest is 2^14 at least: len 2^-38 max |v|."""
+      a weight times a value scale under the normal range of binary16 by 2^-25, where the largest scale is 2^6 at least and the sum
+      of weights 1 at least: len 2^-31 max |v|."""
     codes, scales = cache
     cb = oracle.codebook(kind).astype(np.float64)
     page, dim, kv = codes.shape[3], codes.shape[4], codes.shape[2]
@@ -78,6 +79,6 @@ def attention(kind, cache, q, pages, lens, starts, softmax_scale, window=0):
                     w /= w.sum()
                     out[first + i, x] = w @ vv
                     e = (np.abs(kk) @ np.abs(row)).max() * abs(softmax_scale) * (u + (dim + 8) * 2.0 ** -24)
-                    tol[first + i, x] = w @ np.abs(vv) * (2 * u + 2 * e + (8 + length) * 2.0 ** -24) * (1 + 2.0 ** -5) + length * 2.0 ** -38 * np.abs(vv).max()
+                    tol[first + i, x] = w @ np.abs(vv) * (2 * u + 2 * e + (8 + length) * 2.0 ** -24) * (1 + 2.0 ** -5) + length * 2.0 ** -31 * np.abs(vv).max()
                     assert not e >= 2.0 ** -6, "inputs outside the derivation"
     return out, tol
