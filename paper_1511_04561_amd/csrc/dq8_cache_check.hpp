@@ -23,6 +23,7 @@ inline int check_cache(const char *who, int kind, const dq8_cache *c)
     if (c->kv_heads < 1 || c->kv_heads > 65535) return failed(DQ8_ERR_ARG, "%s: %d cached heads", who, c->kv_heads);
     if (c->pages < 1 || c->pages >= kCacheLimit / (size_t)c->page_size || c->pages * (size_t)c->page_size >= ((size_t)1 << 50) / ((size_t)c->kv_heads * (size_t)c->dim))
         return failed(DQ8_ERR_ARG, "%s: %zu pages of %d", who, c->pages, c->page_size);
+    if ((size_t)c->kv_heads * (size_t)c->page_size * (size_t)c->dim >= kCacheLimit) return failed(DQ8_ERR_ARG, "%s: a page of more than 2 GiB", who);
     return DQ8_OK;
 }
 

@@ -14,6 +14,7 @@ namespace {
 
 typedef float v16 __attribute__((ext_vector_type(16)));
 
+constexpr int kGroupVector = 0x2, kGroupMatrix = 0x8, kGroupRead = 0x100;  // instructions, for the scheduler
 constexpr int kChunkWaves = 8, kChunkWg = kChunkWaves * kWave;
 
 // The job of number idx, counted over sequences: sequence b and the number in it.  Every wavefront by itself; idx < their number.
@@ -66,12 +67,13 @@ struct ChunkShape {
     // where there are only four of them, one of either.
     static constexpr int kPairs = kKeyFrags / 2;
     static constexpr bool kApart = kPairs < kChunkWaves;
-    static constexpr int kBuffer = (kKeyFrags + kValueFrags) * 1024;  // bytes of a tile
+    static constexpr int kKeyBytes = kKeyFrags * 1024, kValueBytes = kValueFrags * 1024;  // of a tile
     static_assert(kKeyFrags == kValueFrags && (kApart ? 2 * kPairs == kChunkWaves : kPairs == kChunkWaves), "as much work for every wavefront");
     static_assert(kTokens <= kWave, "a lane for every token's scales");
 };
 
-// One tile's scales in LDS: factors of scores and of weights, which tokens are there, and the exponent that the latter were brought to.
+// One tile's scales in LDS: factors of scores and of weights, which tokens are there and the exponent that the latter were brought to.
+// A token whose value scale is not finite has weight factor 0 and a score that is NaN.
 template <int TOKENS>
 struct ChunkScales {
     float key[TOKENS], value[TOKENS];
@@ -85,8 +87,8 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     typedef ChunkShape<DP, TH> S;
     constexpr int KS = S::KS, JT = S::JT, US = S::US, TOKENS = S::kTokens;
     __shared__ __align__(256) uint32_t lut[256 * kLutCopies];
-    __shared__ __align__(16) uint8_t tiles[2 * S::kBuffer];
-    __shared__ __align__(16) ChunkScales<TOKENS> scales[2];
+    __shared__ __align__(16) uint8_t key_tiles[2 * S::kKeyBytes], value_tiles[3 * S::kValueBytes];
+    __shared__ __align__(16) ChunkScales<TOKENS> scales[3];
     const uint32_t lane = threadIdx.x & 63, wave = wave_in_wg(), n = lane & 31, hh = lane >> 5, lane4 = lane * 4;
     // the last query rows of a sequence see most: they begin first
     const Place place = place_of(a, S::kRows, blockIdx.x / splits);
@@ -152,48 +154,58 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
 
     // ---- the tile's way into LDS.  Keys: a lane takes 16 bytes of one of 32 tokens, which are its eight elements of two steps.  Values: a
     // lane takes a word of each of the eight tokens of its half of step u, two bytes of which are elements of its two groups.
+    // The page numbers of 64 groups of 16 tokens are in the lanes, those of the next 64 too.
+    constexpr uint32_t GROUPS = TOKENS / 16, BLOCK = kWave / GROUPS;  // groups of a tile; tiles of 64 groups
     const int32_t *table = a.pages + (size_t)place.b * a.max_pages;
-    auto page_at = [&](uint32_t token) {
-        const uint32_t index = token >> a.page_shift;
+    auto pages_from = [&](uint32_t tile) {
+        const uint32_t index = (tile * TOKENS + lane * 16) >> a.page_shift;
         return (uint32_t)table[index < a.max_pages ? index : a.max_pages - 1];
     };
-    auto row_of = [&](uint32_t page, uint32_t token) {
-        return (((uint64_t)(page < a.n_pages ? page : 0) * a.kv_heads + head) << a.page_shift) + (token & ((1u << a.page_shift) - 1));
-    };
+    uint32_t pages_now = pages_from(t_begin), pages_then = pages_from(t_begin + BLOCK), in_block = 0;
     const bool has_keys = !S::kApart || wave < (uint32_t)S::kPairs, has_values = !S::kApart || !has_keys;
     const uint32_t kp = wave % S::kPairs, k_half = kp / JT, k_pair = kp % JT;       // this wavefront's pair of key operands
     const uint32_t vp = wave % S::kPairs, u = vp % US, two = vp / US;               // and of value operands
     const uint32_t v_select = 0x0C0C0400u + ((two & 1) << 9);                       // its first byte of a word
+    const uint32_t in_page = (1u << a.page_shift) - 1, page_rows = a.kv_heads << a.page_shift, page_bytes = page_rows * a.dim;
+    const uint32_t head_row = head << a.page_shift;
+    const uint32_t dim = a.dim;
+    const uint32_t k_d = 32 * k_pair + 16 * hh, k_at = head_row * dim + (k_d < dim ? k_d : 0);
+    const uint32_t v_d = JT * n + 4 * (two / 2), v_at = 4 * hh * dim + (v_d < dim ? v_d : 0);
     u4 kc = {0, 0, 0, 0};
     uint32_t vc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    uint32_t k_page = 0, v_page = 0, s_page = 0;  // of the tile that is loaded next
     float ks = 0.0f, vs = 0.0f;
     bool s_there = false;
     int32_t staged = kLeastExp;  // (wavefront 0) exponent of the largest value scale so far
-    auto fetch_pages = [&](uint32_t tile) {
-        if (has_keys) k_page = page_at(tile * TOKENS + k_half * 32 + n);
-        if (has_values) v_page = page_at(tile * TOKENS + u * 16);
-        if (wave == 0) s_page = page_at(tile * TOKENS + lane % TOKENS);
-    };
+    auto inside = [&](uint32_t page) { return page < a.n_pages ? page : 0; };
+    // the loads of a tile; tiles in order
     auto fetch = [&](uint32_t tile) {
+        if (in_block == BLOCK) {
+            in_block = 0;
+            pages_now = pages_then;
+            pages_then = pages_from(tile + BLOCK);
+        }
+        const int first = (int)(in_block * GROUPS);
+        ++in_block;
         if (has_keys) {
-            const uint32_t d = 32 * k_pair + 16 * hh;
-            kc = *reinterpret_cast<const u4 *>(a.k_codes + row_of(k_page, tile * TOKENS + k_half * 32 + n) * a.dim + (d < a.dim ? d : 0));
+            const uint32_t p0 = (uint32_t)__builtin_amdgcn_readlane((int)pages_now, first + 2 * (int)k_half), p1 = (uint32_t)__builtin_amdgcn_readlane((int)pages_now, first + 2 * (int)k_half + 1);
+            const uint32_t page = n < 16 ? inside(p0) : inside(p1), token = tile * TOKENS + k_half * 32 + n;
+            kc = *reinterpret_cast<const u4 *>(a.k_codes + (uint64_t)page * page_bytes + (k_at + (token & in_page) * dim));
         }
         if (has_values) {
-            const uint32_t d = JT * n + 4 * (two / 2);
-            const uint8_t *v = a.v_codes + row_of(v_page, tile * TOKENS + u * 16 + 4 * hh) * a.dim + (d < a.dim ? d : 0);
+            const uint32_t page = inside((uint32_t)__builtin_amdgcn_readlane((int)pages_now, first + (int)u));
+            const uint8_t *v = a.v_codes + (uint64_t)page * page_bytes + (head_row + ((tile * TOKENS + u * 16) & in_page)) * dim;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint8_t *at = v + (i % 4 + 8 * (i / 4)) * a.dim;
-                vc[i] = JT == 2 ? *reinterpret_cast<const uint16_t *>(at) : *reinterpret_cast<const uint32_t *>(at);
+                const uint8_t *at = v + (i % 4 + 8 * (i / 4)) * dim;
+                vc[i] = JT == 2 ? load_at<uint16_t>(at, v_at) : load_at<uint32_t>(at, v_at);
             }
         }
         if (wave == 0) {
-            const uint64_t at = row_of(s_page, tile * TOKENS + lane % TOKENS);
+            const uint32_t page = (uint32_t)__shfl((int)pages_now, first + (int)(lane % TOKENS) / 16), token = tile * TOKENS + lane % TOKENS;
+            const uint64_t at = (uint64_t)inside(page) * page_rows + head_row + (token & in_page);
             ks = a.k_scales[at];
             vs = a.v_scales[at];
-            s_there = (int32_t)(tile * TOKENS + lane % TOKENS) < s.len && s_page < a.n_pages;
+            s_there = (int32_t)token < s.len && page < a.n_pages;
         }
     };
     const float factor = fabsf(a.factor);
@@ -204,45 +216,42 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
             f[i] = *reinterpret_cast<const _Float16 *>(reinterpret_cast<const char *>(lut) + __builtin_amdgcn_perm(vc[i], lane4, select));
         return f;
     };
-    auto put = [&](uint32_t buffer) {
-        v8h *const to = reinterpret_cast<v8h *>(tiles + buffer * S::kBuffer) + lane;
+    auto put = [&](uint32_t buffer2, uint32_t buffer3) {
         if (has_keys) {
-            v8h *const f = to + (k_half * KS + 2 * k_pair) * kWave;
+            v8h *const f = reinterpret_cast<v8h *>(key_tiles + buffer2 * S::kKeyBytes) + (k_half * KS + 2 * k_pair) * kWave + lane;
             f[0] = eight(lut, kc.x, kc.y, lane4);
             f[kWave] = eight(lut, kc.z, kc.w, lane4);
         }
-        __builtin_amdgcn_sched_barrier(0);
         if (has_values) {
-            v8h *const f = to + (S::kKeyFrags + u * JT + 2 * two) * kWave;
+            v8h *const f = reinterpret_cast<v8h *>(value_tiles + buffer3 * S::kValueBytes) + (u * JT + 2 * two) * kWave + lane;
             f[0] = eighth_of(v_select);
             f[kWave] = eighth_of(v_select + 0x100u);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (wave == 0) {
-            const float y = s_there ? vs : 0.0f;
-            float most = y;
+    };
+    auto put_scales = [&](uint32_t buffer3) {
+        if (wave != 0) return;
+        const bool finite = fabsf(vs) <= FLT_MAX;  // (if not, the score becomes NaN for whoever sees it)
+        const float y = s_there && finite ? vs : 0.0f;
+        float most = y;
 #pragma unroll
-            for (int m = 1; m < TOKENS; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
-            const int e = (int)uniform((uint32_t)exponent(fmaxf(most, 0.0f)));
-            staged = e > staged ? e : staged;
-            ChunkScales<TOKENS> &sc = scales[buffer];
-            if (lane < TOKENS) {
-                sc.key[lane] = ks * factor;
-                sc.value[lane] = y * __builtin_amdgcn_ldexpf(1.0f, kWeightTop - staged);
-            }
-            const uint64_t all = __builtin_amdgcn_ballot_w64(s_there);
-            if (lane == 0) {
-                sc.there = all;
-                sc.exponent = staged;
-            }
+        for (int m = 1; m < TOKENS; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+        const int e = (int)uniform((uint32_t)exponent(fmaxf(most, 0.0f)));
+        staged = e > staged ? e : staged;
+        ChunkScales<TOKENS> &sc = scales[buffer3];
+        if (lane < TOKENS) {
+            sc.key[lane] = finite ? ks * factor : __builtin_nanf("");
+            sc.value[lane] = y * __builtin_amdgcn_ldexpf(1.0f, kWeightTop - staged);
+        }
+        const uint64_t all = __builtin_amdgcn_ballot_w64(s_there);
+        if (lane == 0) {
+            sc.there = all;
+            sc.exponent = staged;
         }
     };
 
-    auto multiply = [&](uint32_t tile, uint32_t buffer) {
-        const v8h *const keys = reinterpret_cast<const v8h *>(tiles + buffer * S::kBuffer) + lane, *const values = keys + S::kKeyFrags * kWave;
-        const ChunkScales<TOKENS> &sc = scales[buffer];
-        const int32_t t = (int32_t)(tile * TOKENS);
-        v16 st[TH];
+    v16 st[TH];
+    auto score = [&](uint32_t buffer2) {
+        const v8h *const keys = reinterpret_cast<const v8h *>(key_tiles + buffer2 * S::kKeyBytes) + lane;
 #pragma unroll
         for (int h = 0; h < TH; ++h)
 #pragma unroll
@@ -251,6 +260,12 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int h = 0; h < TH; ++h) st[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(keys[(h * KS + k) * kWave], q[k], st[h], 0, 0, 0);
+    };
+    const int32_t hidden_upto = a.window > 0 && in ? pos - a.window : INT32_MIN;
+    auto add = [&](uint32_t tile, uint32_t buffer3) {
+        const v8h *const values = reinterpret_cast<const v8h *>(value_tiles + buffer3 * S::kValueBytes) + lane;
+        const ChunkScales<TOKENS> &sc = scales[buffer3];
+        const int32_t t = (int32_t)(tile * TOKENS);
         const int e = sc.exponent;
         if (e > vexp) {
             const float less = __builtin_amdgcn_ldexpf(1.0f, vexp - e);
@@ -267,17 +282,22 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
 #pragma unroll
                 for (int i = 0; i < 4; ++i) st[h][4 * i4 + i] *= f[i];
             }
-        const uint64_t there = sc.there;
-        const bool masked = t + TOKENS - 1 > p_first || (a.window > 0 && t <= p_last - a.window) || there != ~0ull;  // (32 tokens: both halves of the wavefront say the same)
+        const uint64_t there = sc.there;  // (32 tokens: both halves of the wavefront say the same)
+        const bool masked = t + TOKENS - 1 > p_first || (a.window > 0 && t <= p_last - a.window) || there != ~0ull;
         if (masked) {
 #pragma unroll
             for (int h = 0; h < TH; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int32_t at = 32 * h + 8 * (i / 4) + 4 * (int32_t)hh + i % 4, token = t + at;
-                    const bool seen = (token <= pos) & ((a.window <= 0) | (token > pos - a.window)) & (int)(there >> at & 1);
-                    st[h][i] = seen ? st[h][i] : -__builtin_inff();
+                    const int32_t token = t + 32 * h + 8 * (i / 4) + 4 * (int32_t)hh + i % 4;
+                    st[h][i] = ((token <= pos) & (token > hidden_upto)) ? st[h][i] : -__builtin_inff();
                 }
+            if (there != ~0ull)
+#pragma unroll
+                for (int h = 0; h < TH; ++h)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(there >> (32 * h + 8 * (i / 4) + 4 * hh + i % 4) & 1)) st[h][i] = -__builtin_inff();
         }
         float high = kNothing;
 #pragma unroll
@@ -306,43 +326,58 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
                     p[2 * h + i4 / 2][4 * (i4 % 2) + i] = (_Float16)(w * f[i]);
                 }
             }
-        if (masked)  // a hidden token's scale may be anything
-#pragma unroll
-            for (int h = 0; h < TH; ++h)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (st[h][i] == -__builtin_inff()) p[2 * h + i / 8][i % 8] = (_Float16)0.0f;
 #pragma unroll
         for (int x = 0; x < US; ++x)
 #pragma unroll
             for (int j = 0; j < JT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values[(x * JT + j) * kWave], p[x], acc[j], 0, 0, 0);
+        // the products of the first half of the tokens between the weights of the second
+        if constexpr (TH == 2) {
+            __builtin_amdgcn_sched_group_barrier(kGroupVector, 72, 0);
+#pragma unroll
+            for (int i = 0; i < US * JT / 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kGroupMatrix, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kGroupVector, 144 / (US * JT), 0);
+            }
+        }
     };
 
     __syncthreads();  // the table
     if (t_begin < t_end) {
-        // behind the last tile the last is loaded again
-        const uint32_t last = t_end - 1;
-        auto limited = [&](uint32_t tile) { return tile < t_end ? tile : last; };
-        fetch_pages(t_begin);
+        // Half of the wavefronts, one of each SIMD's two, take the weights and sums of a tile together with the next tile's scores: while one
+        // of the two uses the vector unit, the other has products to do.  A barrier per tile, two buffers of keys and three of values.
+        const bool late = wave >= kChunkWaves / 2;
+        auto seen = [&](uint32_t tile) {
+            const int32_t t = (int32_t)(tile * TOKENS);
+            return t <= p_last && (a.window <= 0 || t + TOKENS > p_first - a.window + 1);
+        };
         fetch(t_begin);
-        fetch_pages(limited(t_begin + 1));
-        put(0);
-        fetch(limited(t_begin + 1));
-        fetch_pages(limited(t_begin + 2));
+        put(0, 0);
+        put_scales(0);
+        if (t_begin + 1 < t_end) fetch(t_begin + 1);
         __syncthreads();
-        for (uint32_t tile = t_begin, buffer = 0;; ++tile, buffer ^= 1) {
-            const bool seen = (int32_t)(tile * TOKENS) <= p_last && (a.window <= 0 || (int32_t)(tile * TOKENS + TOKENS) > p_first - a.window + 1);
-            if (tile < last) {
-                // the next tile's codes are here: into the other buffer; then the loads of the tile after it and of the page
-                // numbers of the one after that
-                put(buffer ^ 1);
-                fetch(limited(tile + 2));
-                fetch_pages(limited(tile + 3));
+        uint32_t two_of = 0, three_of = 0;  // buffers of the present tile
+        for (uint32_t tile = t_begin; tile < t_end; ++tile) {
+            const uint32_t before = three_of == 0 ? 2 : three_of - 1, behind = three_of == 2 ? 0 : three_of + 1;
+            if (late && tile > t_begin && seen(tile - 1)) add(tile - 1, before);
+            // (behind the last tile that one again, for nobody; the scores of a tile that no row sees, for nobody)
+            put(two_of ^ 1, behind);
+            score(two_of);
+            if constexpr (!S::kApart) {  // products, look-ups and what they need in turn
+#pragma unroll
+                for (int i = 0; i < S::kKeyFrags; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(kGroupRead, 3, 0);
+                    __builtin_amdgcn_sched_group_barrier(kGroupMatrix, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kGroupVector, 4, 0);
+                }
             }
-            if (seen) multiply(tile, buffer);
-            if (tile == last) break;
+            put_scales(behind);
+            if (tile + 2 < t_end) fetch(tile + 2);
+            if (!late && seen(tile)) add(tile, three_of);
             __syncthreads();
+            two_of ^= 1;
+            three_of = behind;
         }
+        if (late && seen(t_end - 1)) add(t_end - 1, three_of == 0 ? 2 : three_of - 1);
     }
 
     const size_t part = (size_t)(blockIdx.x / splits) * splits + split;
