@@ -21,9 +21,11 @@
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdint>
 #include <exception>
 
+#include "dq8_cache.h"
 #include "dq8_workspace.h"
 
 namespace {
@@ -44,6 +46,9 @@ struct Library {
     decltype(&dq8_decode_avg_encode) avg_encode;
     decltype(&dq8_error_stats_ws) error_stats;
     decltype(&dq8_workspace_bytes_stats) workspace_stats;
+    decltype(&dq8_cache_append) cache_append;
+    decltype(&dq8_cache_attention) cache_attention;
+    decltype(&dq8_cache_attention_workspace_bytes) workspace_attention;
     decltype(&dq8_last_error) last_error;
 } g_lib;
 PyObject *g_error = nullptr;
@@ -476,6 +481,186 @@ PyObject *error_stats(PyObject *const *a)  // kind, x, block, scales, scales_giv
     return pair(stats, means);
 }
 
+// ---- the cache of keys and values (dq8_cache.h)
+
+// The cache's two arrays, on the current device.
+struct Cache {
+    dq8_cache c;
+    const at::Tensor *codes = nullptr;
+
+    bool take(PyObject *codes_, PyObject *scales_)
+    {
+        Buffer b, s;
+        if (!buffer(codes_, at::kByte, b) || !buffer(scales_, at::kFloat, s) || b.t->dim() != 5 || s.t->dim() != 4 || b.t->size(0) != 2) return false;
+        for (int i = 0; i < 4; ++i)
+            if (b.t->size(i) != s.t->size(i)) return false;
+        for (int i = 2; i < 5; ++i)
+            if (b.t->size(i) > INT32_MAX) return false;
+        codes = b.t;
+        c = {static_cast<uint8_t *>(b.ptr), static_cast<float *>(s.ptr), (size_t)b.t->size(1), (int)b.t->size(2), (int)b.t->size(3), (int)b.t->size(4)};
+        return same_device(*s.t);
+    }
+
+    bool same_device(const at::Tensor &t) const { return t.get_device() == codes->get_device(); }
+
+    // A contiguous tensor of n elements on the cache's device.
+    bool array(PyObject *o, at::ScalarType type, size_t n, const void *&ptr) const
+    {
+        Buffer b;
+        if (!buffer(o, type, b) || b.n != n || !same_device(*b.t)) return false;
+        ptr = b.ptr;
+        return true;
+    }
+};
+
+// [tokens, heads, dim] whose rows are contiguous.
+struct Rows {
+    const at::Tensor *t = nullptr;
+    void *ptr = nullptr;
+    size_t token_stride = 0, head_stride = 0;
+
+    bool take(PyObject *o, const Cache &c)
+    {
+        if (!THPVariable_CheckExact(o)) return false;
+        return take(THPVariable_Unpack(o), c);
+    }
+
+    bool take(const at::Tensor &x, const Cache &c)
+    {
+        if (!x.defined() || !x.is_cuda() || x.key_set().has_any(kTransformed) || x.layout() != at::kStrided || !x.has_storage() || x.dim() != 3 ||
+            x.size(2) != c.c.dim || x.stride(2) != 1 || x.stride(0) < 0 || x.stride(1) < 0 || x.size(0) == 0 || x.size(1) == 0 || x.size(1) > INT32_MAX ||
+            !c.same_device(x))
+            return false;
+        t = &x;
+        ptr = x.data_ptr();
+        token_stride = (size_t)x.stride(0);
+        head_stride = (size_t)x.stride(1);
+        return true;
+    }
+
+    bool like(const Rows &o) const { return t->scalar_type() == o.t->scalar_type() && t->size(0) == o.t->size(0) && t->size(1) == o.t->size(1); }
+};
+
+bool type_of(const at::Tensor &t, int &type)
+{
+    const at::ScalarType s = t.scalar_type();
+    type = s == at::kFloat ? DQ8_FLOAT32 : s == at::kBFloat16 ? DQ8_BFLOAT16 : DQ8_FLOAT16;
+    return s == at::kFloat || s == at::kBFloat16 || s == at::kHalf;
+}
+
+bool real(PyObject *o, double &v)
+{
+    if (!PyFloat_CheckExact(o)) return false;
+    v = PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
+// Queries in, or False (not None: the call is done) without.
+PyObject *cache_append(PyObject *const *a)  // kind, k, v, slots, codes, scales, positions, rotation, interleaved, q, q_weight, k_weight, eps, q_out
+{
+    int kind;
+    Cache cache;
+    Rows k, v, q, out;
+    bool interleaved;
+    void *stream;
+    dq8_append x = {};
+    at::Tensor made;
+    if (!kind_of(a[0], kind) || !cache.take(a[4], a[5]) || !stream_for(*cache.codes, stream) || !k.take(a[1], cache) || !v.take(a[2], cache) ||
+        !v.like(k) || k.t->size(1) != cache.c.kv_heads || !type_of(*k.t, x.type) || !flag(a[8], interleaved) || !real(a[12], x.eps))
+        return declined();
+    x.tokens = (size_t)k.t->size(0);
+    const size_t dim = (size_t)cache.c.dim;
+    const void *p = nullptr;
+    if (!cache.array(a[3], at::kLong, x.tokens, p)) return declined();
+    x.slots = static_cast<const int64_t *>(p);
+    if (a[9] != Py_None) {
+        if (!q.take(a[9], cache) || q.t->scalar_type() != k.t->scalar_type() || q.t->size(0) != k.t->size(0)) return declined();
+        if (a[13] == Py_None) {
+            made = at::empty(q.t->sizes(), q.t->options().requires_grad(false));
+            if (made.key_set().has_any(kTransformed) || !out.take(made, cache)) return declined();
+        } else if (!out.take(a[13], cache) || !out.like(q)) {
+            return declined();
+        }
+        x.heads = (int)q.t->size(1);
+        x.q = q.ptr, x.q_token_stride = q.token_stride, x.q_head_stride = q.head_stride;
+        x.q_out = out.ptr, x.q_out_token_stride = out.token_stride, x.q_out_head_stride = out.head_stride;
+    } else if (a[13] != Py_None || a[10] != Py_None) {
+        return declined();
+    }
+    x.k = k.ptr, x.k_token_stride = k.token_stride, x.k_head_stride = k.head_stride;
+    x.v = v.ptr, x.v_token_stride = v.token_stride, x.v_head_stride = v.head_stride;
+    if ((a[6] == Py_None) != (a[7] == Py_None)) return declined();
+    if (a[7] != Py_None) {
+        Buffer r;
+        if (!buffer(a[7], at::kFloat, r) || r.t->dim() != 3 || r.t->size(1) != 2 || r.t->size(2) > INT32_MAX || !cache.same_device(*r.t) ||
+            !cache.array(a[6], at::kLong, x.tokens, p))
+            return declined();
+        x.positions = static_cast<const int64_t *>(p);
+        x.rotation = static_cast<const float *>(r.ptr);
+        x.n_positions = (size_t)r.t->size(0), x.half = (int)r.t->size(2), x.interleaved = interleaved;
+    }
+    if (a[10] != Py_None) {
+        if (!cache.array(a[10], at::kFloat, dim, p)) return declined();
+        x.q_weight = static_cast<const float *>(p);
+    }
+    if (a[11] != Py_None) {
+        if (!cache.array(a[11], at::kFloat, dim, p)) return declined();
+        x.k_weight = static_cast<const float *>(p);
+    }
+    if (!enqueue("dq8_cache_append", [&] { return g_lib.cache_append(kind, &cache.c, &x, stream); })) return nullptr;
+    if (a[9] == Py_None) Py_RETURN_FALSE;
+    if (a[13] != Py_None) return Py_NewRef(a[13]);
+    return THPVariable_Wrap(made);
+}
+
+PyObject *cache_attention(PyObject *const *a)  // kind, q, codes, scales, pages, lens, starts, max_new, softmax_scale, window, out, workspace
+{
+    int kind;
+    Cache cache;
+    Rows q, out;
+    Buffer pages, space;
+    size_t window, most = 0;
+    double scale = 0.0;
+    void *stream;
+    dq8_attention x = {};
+    at::Tensor made;
+    if (!kind_of(a[0], kind) || !cache.take(a[2], a[3]) || !stream_for(*cache.codes, stream) || !q.take(a[1], cache) || !type_of(*q.t, x.type) ||
+        x.type == DQ8_FLOAT32 || !buffer(a[4], at::kInt, pages) || pages.t->dim() != 2 || pages.n == 0 || !cache.same_device(*pages.t) ||
+        (a[7] != Py_None && !whole(a[7], most)) || (a[8] != Py_None && !real(a[8], scale)) || !whole(a[9], window) || window > INT32_MAX)
+        return declined();
+    x.tokens = (size_t)q.t->size(0), x.heads = (int)q.t->size(1);
+    x.q = q.ptr, x.q_token_stride = q.token_stride, x.q_head_stride = q.head_stride;
+    x.batch = (size_t)pages.t->size(0), x.max_pages = (size_t)pages.t->size(1);
+    x.pages = static_cast<const int32_t *>(pages.ptr);
+    const void *p = nullptr;
+    if (!cache.array(a[5], at::kInt, x.batch, p)) return declined();
+    x.lens = static_cast<const int32_t *>(p);
+    if (a[6] != Py_None) {
+        if (!cache.array(a[6], at::kInt, x.batch + 1, p)) return declined();
+        x.starts = static_cast<const int32_t *>(p);
+    }
+    x.max_new = most, x.window = (int)window;
+    x.softmax_scale = a[8] == Py_None ? (float)(1.0 / std::sqrt((double)cache.c.dim)) : (float)scale;
+    if (a[10] == Py_None) {
+        made = at::empty(q.t->sizes(), q.t->options().requires_grad(false));
+        if (made.key_set().has_any(kTransformed) || !out.take(made, cache)) return declined();
+    } else if (!out.take(a[10], cache) || !out.like(q)) {
+        return declined();
+    }
+    x.out = out.ptr, x.out_token_stride = out.token_stride, x.out_head_stride = out.head_stride;
+    Scratch scratch;
+    if (a[11] == Py_None) {
+        if (!scratch.take(g_lib.workspace_attention(&cache.c, &x), *q.t, stream)) return declined();
+    } else {
+        if (!buffer(a[11], at::kByte, space) || !cache.same_device(*space.t)) return declined();
+        scratch.ptr = space.n ? space.ptr : nullptr;
+        scratch.bytes = space.n;
+    }
+    if (!enqueue("dq8_cache_attention", [&] { return g_lib.cache_attention(kind, &cache.c, &x, scratch.ptr, scratch.bytes, stream); })) return nullptr;
+    if (a[10] != Py_None) return Py_NewRef(a[10]);
+    return THPVariable_Wrap(made);
+}
+
 // bind(error class, {name: address}): the entry points of the library that dq8.py has loaded.
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -504,6 +689,9 @@ PyObject *bind(PyObject *, PyObject *args)
     take(l.avg_encode, "dq8_decode_avg_encode");
     take(l.error_stats, "dq8_error_stats_ws");
     take(l.workspace_stats, "dq8_workspace_bytes_stats");
+    take(l.cache_append, "dq8_cache_append");
+    take(l.cache_attention, "dq8_cache_attention");
+    take(l.workspace_attention, "dq8_cache_attention_workspace_bytes");
     take(l.last_error, "dq8_last_error");
     if (!ok) return nullptr;
     g_lib = l;
@@ -529,6 +717,8 @@ PyMethodDef g_methods[] = {
     method<decode_accumulate_avg_segments, 6>("decode_accumulate_avg_segments"),
     method<decode_avg_encode, 7>("decode_avg_encode"),
     method<error_stats, 7>("error_stats"),
+    method<cache_append, 14>("cache_append"),
+    method<cache_attention, 12>("cache_attention"),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -112,7 +112,8 @@ def lib():
 _BOUND = ("dq8_absmax", "dq8_encode_ws", "dq8_workspace_bytes", "dq8_decode", "dq8_absmax_segments", "dq8_encode_segments_ws",
           "dq8_workspace_bytes_segments", "dq8_decode_segments",
           "dq8_decode_accumulate_avg", "dq8_decode_accumulate_avg_local", "dq8_decode_accumulate_avg_segments",
-          "dq8_decode_avg_encode", "dq8_error_stats_ws", "dq8_workspace_bytes_stats", "dq8_last_error")
+          "dq8_decode_avg_encode", "dq8_error_stats_ws", "dq8_workspace_bytes_stats", "dq8_cache_append", "dq8_cache_attention",
+          "dq8_cache_attention_workspace_bytes", "dq8_last_error")
 
 
 def _check(rc, what):
@@ -474,6 +475,9 @@ def cache_append(kind, k, v, slots, codes, scales, positions=None, rotation=None
 
     k, v and q may be views whose rows are contiguous (parts of a projection's output).  Returns the queries (``q_out``, a new tensor
     or q itself), None without q."""
+    done = _native.cache_append(kind, k, v, slots, codes, scales, positions, rotation, interleaved, q, q_weight, k_weight, eps, q_out)
+    if done is not None:
+        return None if done is False else done
     c = _cache(codes, scales)
     dev, dim = codes.device, c.dim
     if not isinstance(k, torch.Tensor) or k.dtype not in _TYPES:
@@ -552,6 +556,9 @@ def cache_attention(kind, q, codes, scales, pages, lens, starts=None, max_new=No
     max_new: the largest number of new tokens of a sequence, where the host knows it.  window > 0: a query sees that many tokens at most.
     workspace: a uint8 tensor of cache_attention_workspace() bytes; None: taken from torch's allocator, and not while the stream is
     captured into a graph (hand one in there: without it few sequences are slow)."""
+    done = _native.cache_attention(kind, q, codes, scales, pages, lens, starts, max_new, softmax_scale, window, out, workspace)
+    if done is not None:
+        return done
     c, a = _attention(q, codes, scales, pages, lens, starts, max_new, softmax_scale, window, out)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=codes.device)
