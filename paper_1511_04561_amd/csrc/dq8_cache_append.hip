@@ -2,9 +2,11 @@
 // (dq8_cache_append of include/dq8_cache.h).  Built with the flags of dq8.hip: no contraction of products and sums.
 //
 // A row is `dim` elements of one token and head, held by LPR neighbouring lanes, eight elements each (dim <= 8 LPR), so a
-// wavefront works on 64 / LPR rows at a time and the row's sum of squares and maximum are reductions over LPR lanes.  The partner
-// of an element that is turned half a rotation away lies in another lane: it is loaded from memory once more (the same cache
-// lines, a few instructions earlier) instead of passed between lanes.
+// wavefront works on 64 / LPR rows at a time and the row's sum of squares and maximum are reductions over LPR lanes.  What a
+// wavefront is given is an item: item_steps times so many heads of one token, queries, keys or values.  A lane has the same places of
+// every head, so that the angles and weights, four times the bytes of a row of 16-bit elements, are loaded once per item.  The steps
+// are a loop and not written out: the calls of a decoding step run through this code once, and what they wait for then is the code
+// itself (2077 tokens of 12 heads in binary32: 20 us with four steps written out, 13 with the loop).
 #include <hip/hip_runtime.h>
 
 #include "dq8_cache_check.hpp"
@@ -25,6 +27,8 @@ struct AppendArgs {
     double eps;
     uint32_t tokens, heads, kv_heads, dim, half, interleaved, page_shift;
     uint32_t kv_groups;  // workgroups that work on keys and values, the rest on queries
+    uint32_t item_steps; // of 64 / LPR heads
+    uint32_t any_at;     // word of LDS from which on pairs that lie anywhere are exchanged
 };
 
 template <typename T>
@@ -68,140 +72,217 @@ __device__ __forceinline__ double row_sum(double v)
     return v;
 }
 
-// This lane's eight elements i0 .. i0 + 7 of a row, normed and turned, in F (double for keys, float for queries).  `row` and `turn`
-// are valid addresses for every lane; lanes whose elements lie behind the row (i0 >= dim) take part in the sums with zeros.
-template <typename F, int LPR, typename T>
-__device__ __forceinline__ void normed_and_turned(const AppendArgs &a, const T *row, const float *weight, const float *turn, uint32_t i0,
-                                                  F (&y)[8])
+// The value of another lane; lane4: four times its number.
+__device__ __forceinline__ float from_lane(float v, int lane4) { return u2f((uint32_t)__builtin_amdgcn_ds_bpermute(lane4, (int)f2u(v))); }
+
+__device__ __forceinline__ double from_lane(double v, int lane4)
+{
+    int w[2];
+    __builtin_memcpy(w, &v, 8);
+    w[0] = __builtin_amdgcn_ds_bpermute(lane4, w[0]);
+    w[1] = __builtin_amdgcn_ds_bpermute(lane4, w[1]);
+    __builtin_memcpy(&v, w, 8);
+    return v;
+}
+
+// How the elements of a pair lie to each other: the same places of two lanes, two places of a lane, or (kAnywhere) neither.
+enum Turn { kNoTurn, kLanes, kInside, kAnywhere };
+
+// What a lane needs of an item beside its rows: cosines and sines of its eight elements' pairs and their weights.
+struct Places {
+    float c[8], s[8], w[8];
+    Turn turn;
+    bool normed, low;
+    int partner4;  // kLanes: four times the number of the lane with the pairs' other elements
+};
+
+// `turning`: the token's row of the table, null without a rotation.
+__device__ __forceinline__ Places places_of(const AppendArgs &a, const float *weight, const float *turning, uint32_t i0, uint32_t lane)
+{
+    Places p = {};
+    p.normed = weight != nullptr;
+    const bool in = i0 < a.dim;
+    if (weight && in) load8(weight + i0, p.w);
+    const uint32_t half = a.half;
+    p.turn = !turning ? kNoTurn : a.interleaved ? half % 4 == 0 ? kInside : kAnywhere : half % 8 == 0 ? kLanes : kAnywhere;
+    p.low = i0 < half;
+    if (p.turn == kLanes) {  // (elements behind the rotation: times one, minus zero times something finite or not at all)
+        const bool turned = i0 < 2 * half;
+        p.partner4 = 4 * (int)(turned ? p.low ? lane + half / 8 : lane - half / 8 : lane);
+        const uint32_t p0 = p.low ? i0 : turned ? i0 - half : 0;
+        load8(turning + p0, p.c);
+        load8(turning + half + p0, p.s);
+    } else if (p.turn == kInside && i0 < 2 * half) {
+        typedef v4f V __attribute__((aligned(4)));
+        const v4f c = *reinterpret_cast<const V *>(turning + i0 / 2), s = *reinterpret_cast<const V *>(turning + half + i0 / 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p.c[e] = c[e], p.s[e] = s[e];
+    }
+    return p;
+}
+
+// This lane's eight elements of a row (x), normed and turned, in F (double for keys, float for queries).  Lanes whose elements lie behind
+// the row have zeros and take part in the sums.  `any`: LDS of this wavefront for pairs that lie anywhere, null where none do.
+template <typename F, int LPR, bool ANY>
+__device__ __forceinline__ void normed_and_turned(const AppendArgs &a, const Places &p, const float (&x)[8], const float *turning, uint32_t i0,
+                                                  uint32_t lane, double *any, F (&y)[8])
 {
     const bool in = i0 < a.dim;
-    float x[8] = {};
-    if (in) load8(row + i0, x);
-    F r = 1;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = x[e];
-    if (weight) {
+    if (p.normed) {
         F sum = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
-        r = F(1) / sqrt(row_sum<LPR>(sum) / F(a.dim) + F(a.eps));
-        if (in) {
-            float w[8];
-            load8(weight + i0, w);
+        const F r = F(1) / sqrt(row_sum<LPR>(sum) / F(a.dim) + F(a.eps));
+        if (in)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = y[e] * r * F(w[e]);
-        }
+            for (int e = 0; e < 8; ++e) y[e] = y[e] * r * F(p.w[e]);
     }
-    const uint32_t half = a.half;
-    if (!turn || i0 >= 2 * half) return;
-    if (!a.interleaved && half % 8 == 0) {  // all eight on one side, and so their partners
-        const bool low = i0 < half;
-        const uint32_t j0 = low ? i0 + half : i0 - half, p0 = low ? i0 : j0;
-        float other[8], c[8], s[8], w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-        load8(row + j0, other);
-        load8(turn + p0, c);
-        load8(turn + half + p0, s);
-        if (weight) load8(weight + j0, w);
+    const bool turned = i0 < 2 * a.half;
+    if (p.turn == kLanes) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const F o = weight ? F(other[e]) * r * F(w[e]) : F(other[e]);
-            y[e] = low ? y[e] * F(c[e]) - o * F(s[e]) : y[e] * F(c[e]) + o * F(s[e]);
+            const F o = from_lane(y[e], p.partner4), t = o * F(p.s[e]);
+            if (turned) y[e] = y[e] * F(p.c[e]) + (p.low ? -t : t);
         }
-    } else if (a.interleaved) {  // pairs inside the lane
+    } else if (p.turn == kInside) {
+        if (turned)
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const uint32_t p = (i0 + e) / 2;
-            if (p < half) {
-                const F c = turn[p], s = turn[half + p], u = y[e], v = y[e + 1];
+            for (int e = 0; e < 8; e += 2) {
+                const F c = p.c[e / 2], s = p.s[e / 2], u = y[e], v = y[e + 1];
                 y[e] = u * c - v * s;
                 y[e + 1] = v * c + u * s;
             }
-        }
-    } else {
+    }
+    if constexpr (ANY) {
+        if (p.turn == kNoTurn) return;
+        F *const row = reinterpret_cast<F *>(any) + (lane / LPR) * (8 * LPR);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) row[i0 + e] = y[e];
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t half = a.half;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t i = i0 + e;
             if (i < 2 * half) {
-                const bool low = i < half;
-                const uint32_t j = low ? i + half : i - half, p = low ? i : j;
-                const F o = weight ? F((float)row[j]) * r * F(weight[j]) : F((float)row[j]);
-                const F c = turn[p], s = turn[half + p];
-                y[e] = low ? y[e] * c - o * s : y[e] * c + o * s;
+                const bool low = a.interleaved ? i % 2 == 0 : i < half;
+                const uint32_t j = a.interleaved ? i ^ 1 : low ? i + half : i - half, q = a.interleaved ? i / 2 : low ? i : j;
+                const F t = row[j] * F(turning[half + q]);
+                y[e] = y[e] * F(turning[q]) + (low ? -t : t);
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
 // The angles of token t; false where its position has none.  Without a rotation: no angles, true.
-__device__ __forceinline__ bool angles(const AppendArgs &a, uint32_t t, const float **turn)
+__device__ __forceinline__ bool angles(const AppendArgs &a, uint32_t t, const float **turning)
 {
-    *turn = nullptr;
+    *turning = nullptr;
     if (!a.rotation) return true;
     const uint64_t p = (uint64_t)a.positions[t];
     const bool ok = p < a.n_positions;
-    *turn = a.rotation + (ok ? p : 0) * 2 * a.half;
+    *turning = a.rotation + (ok ? p : 0) * 2 * a.half;
     return ok;
 }
 
-// Workgroups 0 .. kv_groups - 1 walk the rows of keys, then those of values; the others walk the rows of queries.
-template <int LPR, typename T>
-__global__ __launch_bounds__(kWg) void k_cache_append(const uint32_t *__restrict__ tab, AppendArgs a)
+// kv_groups of the workgroups, spread evenly over all, walk the items of keys, then those of values (the vector unit bounds these); the
+// others walk those of queries (the memory does).
+// ANY: pairs lie anywhere (kernels of their own: the addresses that such pairs need cost the others registers).
+template <int LPR, bool ANY, typename T>
+__global__ __launch_bounds__(kWg, ANY ? 4 : 5) void k_cache_append(const uint32_t *__restrict__ tab, AppendArgs a)
 {
     extern __shared__ uint32_t lds[];
-    constexpr uint32_t kRows = kWave / LPR;  // of a wavefront
+    constexpr uint32_t kRows = kWave / LPR;  // heads at a time
+    const uint32_t item_heads = kRows * a.item_steps;
     const uint32_t lane = threadIdx.x & 63, i0 = (lane % LPR) * 8, sub = lane / LPR;
-    if (blockIdx.x >= a.kv_groups) {
-        const uint32_t rows = a.tokens * a.heads, step = (gridDim.x - a.kv_groups) * kWavesPerWg * kRows;
-        for (uint32_t at = ((blockIdx.x - a.kv_groups) * kWavesPerWg + wave_in_wg()) * kRows; at < rows; at += step) {
-            const uint32_t row = at + sub < rows ? at + sub : rows - 1;  // lanes behind the last row work on it and store nothing
-            const uint32_t t = row / a.heads, h = row % a.heads;
-            const float *turn;
-            const bool ok = angles(a, t, &turn);
-            float y[8];
-            normed_and_turned<float, LPR>(a, static_cast<const T *>(a.q) + t * a.q_ts + h * a.q_hs, a.q_weight, turn, i0, y);
-            if (!ok) {
+    typedef typename Eight<T>::type Raw;
+    typedef Raw RawAny __attribute__((aligned(sizeof(T))));
+    double *const any = reinterpret_cast<double *>(lds + a.any_at) + wave_in_wg() * (kWave * 8);
+    // this lane's elements of a head
+    auto request = [&](const T *token, size_t stride, uint32_t h, uint32_t heads) {
+        Raw raw = {};
+        if (h < heads && i0 < a.dim) raw = *reinterpret_cast<const RawAny *>(token + h * stride + i0);
+        return raw;
+    };
+    const uint32_t kv_before = blockIdx.x * a.kv_groups / gridDim.x, kv_upto = (blockIdx.x + 1) * a.kv_groups / gridDim.x;
+    if (kv_before == kv_upto) {
+        const uint32_t per = (a.heads + item_heads - 1) / item_heads, items = a.tokens * per, step = (gridDim.x - a.kv_groups) * kWavesPerWg;
+        for (uint32_t at = (blockIdx.x - kv_before) * kWavesPerWg + wave_in_wg(); at < items; at += step) {
+            const uint32_t t = at / per, h0 = (at - t * per) * item_heads, end = h0 + item_heads < a.heads ? h0 + item_heads : a.heads;
+            const T *const from = static_cast<const T *>(a.q) + t * a.q_ts;
+            T *const to = static_cast<T *>(a.q_out) + t * a.o_ts;
+            Raw next = request(from, a.q_hs, h0 + sub, end);
+            const float *turning;
+            const bool ok = angles(a, t, &turning);
+            const Places p = places_of(a, a.q_weight, turning, i0, lane);
+#pragma unroll 1
+            for (uint32_t h1 = h0; h1 < end; h1 += kRows) {
+                const uint32_t h = h1 + sub;
+                float x[8], y[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __builtin_nanf("");
+                for (int e = 0; e < 8; ++e) x[e] = (float)next[e];
+                next = request(from, a.q_hs, h + kRows, end);
+                normed_and_turned<float, LPR, ANY>(a, p, x, turning, i0, lane, any, y);
+                if (!ok) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = __builtin_nanf("");
+                }
+                if (h < a.heads && i0 < a.dim) store8(to + h * a.o_hs + i0, y);
             }
-            if (at + sub < rows && i0 < a.dim) store8(static_cast<T *>(a.q_out) + t * a.o_ts + h * a.o_hs + i0, y);
         }
         return;
     }
     const Search sr = load_bucket_table<kWg>(tab, lds);
     __syncthreads();
-    const uint32_t rows = a.tokens * a.kv_heads, steps = (rows + kRows - 1) / kRows;  // of keys, and as many of values
-    for (uint32_t at = blockIdx.x * kWavesPerWg + wave_in_wg(); at < 2 * steps; at += a.kv_groups * kWavesPerWg) {
-        const bool values = at >= steps;
-        const uint32_t first = (values ? at - steps : at) * kRows + sub;
-        const uint32_t row = first < rows ? first : rows - 1;
-        const uint32_t t = row / a.kv_heads, h = row % a.kv_heads;
-        const float *turn;
-        const bool ok = angles(a, t, &turn);
-        float y[8] = {};
-        if (values) {
-            if (i0 < a.dim) load8(static_cast<const T *>(a.v) + t * a.v_ts + h * a.v_hs + i0, y);
-        } else {
-            // binary64: whatever order its sums are taken in, the row that is compressed is the same binary32 values
-            double d[8];
-            normed_and_turned<double, LPR>(a, static_cast<const T *>(a.k) + t * a.k_ts + h * a.k_hs, a.k_weight, turn, i0, d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = i0 < a.dim ? (float)d[e] : 0.0f;
-        }
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = m > abs_bits(y[e]) ? m : abs_bits(y[e]);
-        m = group_max_u32<LPR>(m);
-        const bool finite = m < 0x7F800000u;  // a row with an infinity or NaN stands for NaN
-        const float scale = finite ? u2f(m) : __builtin_nanf(""), d = finite && m ? u2f(m) : 1.0f;
-        const v4f z = {0, 0, 0, 0}, lo = finite ? v4f{y[0], y[1], y[2], y[3]} : z, hi = finite ? v4f{y[4], y[5], y[6], y[7]} : z;
-        const uint2 word = {encode_quad_own_scale(sr, lo, d), encode_quad_own_scale(sr, hi, d)};
+    const uint32_t per = (a.kv_heads + item_heads - 1) / item_heads, items = a.tokens * per;  // of keys, and as many of values
+    for (uint32_t at = kv_before * kWavesPerWg + wave_in_wg(); at < 2 * items; at += a.kv_groups * kWavesPerWg) {
+        const bool values = at >= items;
+        const uint32_t item = values ? at - items : at, t = item / per, h0 = (item - t * per) * item_heads, end = h0 + item_heads < a.kv_heads ? h0 + item_heads : a.kv_heads;
+        const T *const from = values ? static_cast<const T *>(a.v) + t * a.v_ts : static_cast<const T *>(a.k) + t * a.k_ts;
+        const size_t stride = values ? a.v_hs : a.k_hs;
+        Raw next = request(from, stride, h0 + sub, end);
+        const float *turning;
+        const bool ok = angles(a, t, &turning);
         const uint64_t slot = (uint64_t)a.slots[t];
-        if (ok && slot < a.n_slots && first < rows) {
-            // row of the cache: ((part * pages + page) * kv_heads + h) * page_size + place
-            const uint64_t page = (slot >> a.page_shift) + (values ? a.n_slots >> a.page_shift : 0);
-            const uint64_t to = (((page * a.kv_heads + h) << a.page_shift) + (slot & ((1u << a.page_shift) - 1)));
-            if (i0 < a.dim) *reinterpret_cast<uint2 *>(a.codes + to * a.dim + i0) = word;
-            if (i0 == 0) a.scales[to] = scale;
+        if (!(ok && slot < a.n_slots)) continue;  // (uniform)
+        if (values) turning = nullptr;
+        const float *const weight = values ? nullptr : a.k_weight;
+        Places p = places_of(a, weight, turning, i0, lane);
+        // row of the cache: ((part * pages + page) * kv_heads + h) * page_size + place
+        const uint64_t page = (slot >> a.page_shift) + (values ? a.n_slots >> a.page_shift : 0), place = slot & ((1u << a.page_shift) - 1);
+#pragma unroll 1
+        for (uint32_t h1 = h0; h1 < end; h1 += kRows) {
+            const uint32_t h = h1 + sub;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = (float)next[e];
+            next = request(from, stride, h + kRows, end);
+            if (p.normed || p.turn != kNoTurn) {
+                // (made to look new: the 24 of them in binary64, kept for the loop, would be 48 registers)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(p.c[e]), "+v"(p.s[e]), "+v"(p.w[e]));
+                // binary64: whatever order its sums are taken in, the row that is compressed is the same binary32 values
+                double d[8];
+                normed_and_turned<double, LPR, ANY>(a, p, y, turning, i0, lane, any, d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = i0 < a.dim ? (float)d[e] : 0.0f;
+            }
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = m > abs_bits(y[e]) ? m : abs_bits(y[e]);
+            m = group_max_u32<LPR>(m);
+            const bool finite = m < 0x7F800000u;  // a row with an infinity or NaN stands for NaN
+            const float scale = finite ? u2f(m) : __builtin_nanf(""), d = finite && m ? u2f(m) : 1.0f;
+            const v4f z = {0, 0, 0, 0}, lo = finite ? v4f{y[0], y[1], y[2], y[3]} : z, hi = finite ? v4f{y[4], y[5], y[6], y[7]} : z;
+            const uint2 word = {encode_quad_own_scale(sr, lo, d), encode_quad_own_scale(sr, hi, d)};
+            if (h < a.kv_heads) {
+                const uint64_t to = ((page * a.kv_heads + h) << a.page_shift) + place;
+                if (i0 < a.dim) *reinterpret_cast<uint2 *>(a.codes + to * a.dim + i0) = word;
+                if (i0 == 0) a.scales[to] = scale;
+            }
         }
     }
 }
@@ -275,17 +356,30 @@ extern "C" int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_appe
     k.half = a.rotation ? (uint32_t)a.half : 0, k.interleaved = a.interleaved != 0;
     k.page_shift = (uint32_t)__builtin_ctz((unsigned)cache->page_size);
     const int lpr = dim <= 64 ? 8 : dim <= 128 ? 16 : 32;
-    const size_t per = kWavesPerWg * (kWave / lpr);  // rows of a workgroup
-    const size_t most = (size_t)dev.cus * 4;
-    size_t kv_groups = (2 * a.tokens * kv + per - 1) / per, q_groups = (a.tokens * a.heads + per - 1) / per;
-    if (kv_groups > most) kv_groups = most;
-    if (q_groups > most) q_groups = most;
+    // Items of four times the heads that a wavefront has at once where there are many, of one time where every wavefront counts.
+    const size_t at_once = (size_t)(kWave / lpr), heads = (size_t)a.heads;
+    auto items = [&](size_t steps) { return a.tokens * ((heads + at_once * steps - 1) / (at_once * steps) + 2 * ((kv + at_once * steps - 1) / (at_once * steps))); };
+    k.item_steps = items(4) >= (size_t)dev.cus * 16 ? 4 : 1;
+    const size_t per = at_once * k.item_steps, most = (size_t)dev.cus * 5;  // that are resident
+    const size_t kv_items = 2 * a.tokens * ((kv + per - 1) / per), q_items = a.tokens * ((heads + per - 1) / per);
+    size_t kv_groups = (kv_items + kWavesPerWg - 1) / kWavesPerWg, q_groups = (q_items + kWavesPerWg - 1) / kWavesPerWg;
+    if (kv_groups + q_groups > most) {
+        const size_t share = most * kv_items / (kv_items + q_items);
+        kv_groups = share < 1 ? 1 : kv_groups < share ? kv_groups : share;
+        if (q_groups > most - kv_groups) q_groups = most - kv_groups;
+    }
     k.kv_groups = (uint32_t)kv_groups;
+    k.any_at = dev.search_words;  // (whole quads)
+    const bool anywhere = a.rotation && a.half % (a.interleaved ? 4 : 8) != 0;
+    const size_t lds = dev.search_words * sizeof(uint32_t) + (anywhere ? kWg * 8 * sizeof(double) : 0);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-#define DQ8_APPEND(LPR, T) \
-    hipLaunchKernelGGL((k_cache_append<LPR, T>), dim3((unsigned)(kv_groups + q_groups)), dim3(kWg), dev.search_words * sizeof(uint32_t), stream, dev.tab, k)
-#define DQ8_APPEND_T(T)       \
-    switch (lpr) {            \
+#define DQ8_APPEND(LPR, T)                                                                                                                  \
+    if (anywhere)                                                                                                                           \
+        hipLaunchKernelGGL((k_cache_append<LPR, true, T>), dim3((unsigned)(kv_groups + q_groups)), dim3(kWg), lds, stream, dev.tab, k);     \
+    else                                                                                                                                    \
+        hipLaunchKernelGGL((k_cache_append<LPR, false, T>), dim3((unsigned)(kv_groups + q_groups)), dim3(kWg), lds, stream, dev.tab, k)
+#define DQ8_APPEND_T(T)                \
+    switch (lpr) {                     \
     case 8: DQ8_APPEND(8, T); break;   \
     case 16: DQ8_APPEND(16, T); break; \
     default: DQ8_APPEND(32, T); break; \
