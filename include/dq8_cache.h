@@ -88,7 +88,7 @@ int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_append *a, void
  * the mean of their values weighted with exp(softmax_scale * q . key).  A query that sees nothing (lens[b] smaller than the number
  * of new tokens) gets zeros.  Tokens of q behind the last sequence keep their place in `out` as it was.  Lengths beyond
  * max_pages * page_size count as that, negative ones as 0; tokens on pages outside the cache are not seen; starts outside
- * 0 .. tokens count as the nearer end.  Places of the cache that no query sees may hold anything, NaN included.
+ * 0 .. tokens count as the nearer end, and where they descend anywhere nothing is written.  Places of the cache that no query sees may hold anything, NaN included.
  * Products and sums are held in binary32; a code's value, a query and a weight are rounded to binary16 (11 bits, scaled so that
  * none leaves its range) where the matrix instructions take them: one rounding each, as large as that of a binary16 output.
  * Results do not depend on anything but the arguments (workspace size and max_new among them).

@@ -182,7 +182,8 @@ int dq8_cache_attention(int kind, const dq8_cache *cache, const dq8_attention *i
     rc = dq8::device_tables(kind, &dev);
     if (rc) return rc;
     const Shape s = shape_of(cache, a, dev.cus);
-    if (s.work >= dq8::kCacheLimit) return dq8::failed(DQ8_ERR_ARG, "%s: too much work for one call (tokens, heads and pages)", who);
+    if (s.work >= dq8::kCacheLimit || s.jobs >= dq8::kCacheLimit / 256)  // the join's workgroups are of 256, a chunk's of 512 lanes
+        return dq8::failed(DQ8_ERR_ARG, "%s: too much work for one call (tokens, heads and pages)", who);
     AttendArgs k;
     k.q = a.q, k.out = a.out, k.q_ts = a.q_token_stride, k.q_hs = a.q_head_stride, k.o_ts = a.out_token_stride, k.o_hs = a.out_head_stride;
     const size_t half = dq8::cache_rows(cache) / 2;

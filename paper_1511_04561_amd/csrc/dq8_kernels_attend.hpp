@@ -33,7 +33,7 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kTile = 32;          // tokens that a wavefront takes at a time
 constexpr int kAttendWaves = 8;    // of a workgroup: they share one table
 constexpr int kAttendWg = kAttendWaves * kWave;
-constexpr uint32_t kLeastTiles = 2;  // of a wavefront's part, where there are as many
+constexpr uint32_t kLeastTiles = 1;  // of a wavefront's part, where there are as many
 constexpr int kQueryTop = 14;      // a query row's largest element is in [2^14, 2^15) in binary16
 constexpr float kSlack = 8.0f;     // how far a score may be above the reference of its row's weights (in powers of two)
 constexpr int kWeightTop = 6;      // a value scale is below 2^7 where it multiplies a weight, the product below 2^15
@@ -62,6 +62,7 @@ struct AttendArgs {
 
 // A sequence's part of the work.
 struct Seq {
+    bool falls;            // it would end before its beginning
     uint32_t first, n;     // its new tokens in q
     int32_t len;           // cached tokens
     uint32_t lo_tile, tiles;  // tiles of kTile tokens that its queries see: lo_tile .. lo_tile + tiles - 1, one at least
@@ -76,8 +77,10 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, uint32_t b, uint32_
         const int32_t s0 = a.starts[b], s1 = a.starts[b + 1];
         s.first = s0 < 0 ? 0 : (uint32_t)s0 < a.tokens ? (uint32_t)s0 : a.tokens;
         end = s1 < 0 ? 0 : (uint32_t)s1 < a.tokens ? (uint32_t)s1 : a.tokens;
-        if (end < s.first) end = s.first;
+        s.falls = end < s.first;
+        if (s.falls) end = s.first;
     } else {
+        s.falls = false;
         s.first = b * a.each;
         end = s.first + a.each;
     }
@@ -91,6 +94,24 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, uint32_t b, uint32_
     s.tiles = hi > s.lo_tile ? hi - s.lo_tile : 1;
     s.q_tiles = (s.n * a.group + rows - 1) / rows;
     return s;
+}
+
+// Sequences that the calling lane adds up: a run of them, run * lane on.  tally(sequence) of a run is summed, and where the boundaries
+// descend anywhere, all sums are zero: such sequences lie over each other, and the host's bounds of the number of jobs, which
+// records and grids are made for, come from tokens that belong to one sequence each.
+template <typename F>
+__device__ __forceinline__ uint64_t run_sum(const AttendArgs &a, uint32_t rows, uint32_t lane, uint32_t run, F tally)
+{
+    uint64_t mine = 0;
+    bool falls = false;
+    for (uint32_t i = 0; i < run; ++i) {
+        const uint32_t b = lane * run + i;
+        if (b >= a.batch) break;
+        const Seq s = sequence(a, b, rows);
+        falls |= s.falls;
+        mine += tally(s);
+    }
+    return __builtin_amdgcn_ballot_w64(falls) ? 0 : mine;
 }
 
 // Tiles and, in the upper half, jobs of a sequence.
@@ -139,11 +160,7 @@ struct Share {
 __device__ __forceinline__ Share share_of(const AttendArgs &a, uint32_t rows, uint32_t w)
 {
     const uint32_t lane = threadIdx.x & 63, run = (a.batch + kWave - 1) / kWave;
-    uint64_t mine = 0;
-    for (uint32_t i = 0; i < run; ++i) {
-        const uint32_t b = lane * run + i;
-        if (b < a.batch) mine += work_of(a, sequence(a, b, rows));
-    }
+    const uint64_t mine = run_sum(a, rows, lane, run, [&](const Seq &s) { return work_of(a, s); });
     const uint64_t upto = wave_scan(mine, lane), all = lane_of(upto, 63);
     const uint32_t total = (uint32_t)all;
     Share s;

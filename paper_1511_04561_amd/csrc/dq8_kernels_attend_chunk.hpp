@@ -25,11 +25,7 @@ struct Place {
 __device__ __forceinline__ Place place_of(const AttendArgs &a, uint32_t rows, uint32_t idx)
 {
     const uint32_t lane = threadIdx.x & 63, run = (a.batch + kWave - 1) / kWave;
-    uint64_t mine = 0;
-    for (uint32_t i = 0; i < run; ++i) {
-        const uint32_t b = lane * run + i;
-        if (b < a.batch) mine += sequence(a, b, rows).q_tiles * a.kv_heads;
-    }
+    const uint64_t mine = run_sum(a, rows, lane, run, [&](const Seq &s) { return (uint64_t)s.q_tiles * a.kv_heads; });
     const uint64_t upto = wave_scan(mine, lane);
     Place p;
     p.jobs = (uint32_t)lane_of(upto, 63);

@@ -273,18 +273,31 @@ def test_attention_of_bad_pages_lengths_and_starts(dq8):
     got = dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(starts))
     check_attention(got, q, want, tol)
     assert not got[2].any()  # none of its pages is one
-    # starts that descend or leave the range: no access outside.  Sequence 2 counts as tokens 0 .. 2 here and sees none of its
-    # pages, so that each head of token 0 is sequence 0's or zero
+    # starts outside the range count as its nearer end
     bad = starts.copy()
-    bad[2], bad[4] = -7, 2 ** 31 - 1
-    out = torch.zeros_like(q, device="cuda")
-    dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(bad), out=out)
-    assert torch.isfinite(out).all() and not out[1:3].any()
-    for h in range(heads):
-        if out[0, h].any():
-            check_attention(out[:1, h:h + 1], q, want[:1, h:h + 1], tol[:1, h:h + 1])
+    bad[0], bad[4] = -7, 2 ** 31 - 1
+    check_attention(dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(bad)), q, want, tol)
     negative = dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(np.full(4, -3, np.int32)), starts=cuda(starts))
     assert not negative.any()
+
+
+@pytest.mark.parametrize("max_new", [1, 40])
+@pytest.mark.parametrize("sequences", [2, 64, 300])
+def test_attention_of_descending_starts_writes_nothing(dq8, sequences, max_new):
+    """Sequences that lie over each other: far more work than as many tokens can be, so that none of it is begun.  One descent
+    anywhere is enough."""
+    case = (0, "f16", 8, 2, 64, 16, [(40, 300)], 0)
+    kind, _, heads, kv, dim, page, _, _ = case
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    cuda = lambda a: torch.from_numpy(a).cuda()
+    many = (np.repeat(pages, sequences, 0), np.repeat(lens, sequences))
+    over = np.where(np.arange(sequences + 1) % 2, 40, 0).astype(np.int32)
+    last = np.full(sequences + 1, 40, np.int32)
+    last[0], last[-1] = 0, 39
+    for bad in (over, last):
+        out = torch.full_like(q, 7.0, device="cuda")
+        got = dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(many[0]), cuda(many[1]), starts=cuda(bad), max_new=max_new, out=out)
+        assert got is out and (out == 7.0).all()
 
 
 @pytest.mark.parametrize("n", [1, 50])
