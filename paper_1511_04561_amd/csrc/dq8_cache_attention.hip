@@ -20,6 +20,7 @@ struct Shape {
     unsigned groups;   // workgroups
     unsigned splits;   // chunk: workgroups per job
     size_t jobs, work; // jobs and tiles, at most
+    size_t records;    // of jobs that may be cut into parts
     unsigned rows;     // query rows of a job, at most
     size_t parts;      // that can be written
     bool many;         // whether a job is cut into more than about sixteen of them
@@ -49,6 +50,7 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
         s.groups = (unsigned)(s.jobs * s.splits);
         s.parts = s.splits > 1 ? s.groups : 0;
         s.work = s.jobs * s.splits;
+        s.records = s.jobs;
         s.many = s.splits > 16;
         return s;
     }
@@ -60,11 +62,12 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     if (groups > useful) groups = useful;
     s.groups = (unsigned)groups;
     s.parts = groups * kAttendWaves * 2;
+    s.records = s.jobs < groups * kAttendWaves ? s.jobs : groups * kAttendWaves;  // a wavefront leaves one job at most to others
     s.many = s.jobs * 16 <= groups * kAttendWaves;
     return s;
 }
 
-size_t record_bytes(const Shape &s) { return s.parts ? (1 + s.jobs) * sizeof(int4) : 0; }  // their number takes the first
+size_t record_bytes(const Shape &s) { return s.parts ? (1 + s.records) * sizeof(int4) : 0; }  // their number takes the first
 size_t sums_bytes(const Shape &s) { return (s.parts * s.rows * sizeof(float2) + 15) / 16 * 16; }
 size_t parts_bytes(const Shape &s) { return s.parts * s.rows * s.dp * sizeof(float); }
 size_t workspace_bytes_of(const Shape &s) { return record_bytes(s) + sums_bytes(s) + parts_bytes(s); }
@@ -121,11 +124,10 @@ int check_arrays(const char *who, const dq8_cache *cache, const dq8_attention &a
 template <int DP, uint32_t ROWS, typename T>
 int launch_join(const AttendArgs &k, const Shape &s, hipStream_t stream)
 {
-    const dim3 grid((unsigned)s.jobs, (s.rows + kSlice - 1) / kSlice);
     if (s.many)
-        hipLaunchKernelGGL((k_cache_join<DP, ROWS, 1024, T>), grid, dim3(1024), 0, stream, k);
+        hipLaunchKernelGGL((k_cache_join<DP, ROWS, 1, 1024, T>), dim3((unsigned)s.records, s.rows), dim3(1024), 0, stream, k);
     else
-        hipLaunchKernelGGL((k_cache_join<DP, ROWS, 256, T>), grid, dim3(256), 0, stream, k);
+        hipLaunchKernelGGL((k_cache_join<DP, ROWS, 4, 256, T>), dim3((unsigned)s.records, (s.rows + 3) / 4), dim3(256), 0, stream, k);
     return dq8::after_launch_of("k_cache_join", stream);
 }
 
@@ -197,11 +199,11 @@ int dq8_cache_attention(int kind, const dq8_cache *cache, const dq8_attention *i
     k.window = a.window;
     k.entry = kind == DQ8_LINEAR ? 127.0f * 256.0f : 1280.0f * 32.0f;
     k.factor = a.softmax_scale * 1.44269504088896340736f / k.entry;
-    k.rows = s.rows, k.in_a_row = s.chunk;
-    k.jobs = nullptr, k.records = nullptr, k.sums = nullptr, k.parts = nullptr;
+    k.rows = s.rows, k.in_a_row = s.chunk, k.by_wave = !s.chunk && s.records < s.jobs;
+    k.n_records = nullptr, k.records = nullptr, k.sums = nullptr, k.parts = nullptr;
     if (s.parts && workspace && workspace_bytes >= workspace_bytes_of(s)) {
         char *w = static_cast<char *>(workspace);
-        k.jobs = reinterpret_cast<uint32_t *>(w);
+        k.n_records = reinterpret_cast<uint32_t *>(w);
         k.records = reinterpret_cast<int4 *>(w) + 1;
         k.sums = reinterpret_cast<float2 *>(w + record_bytes(s));
         k.parts = reinterpret_cast<float *>(w + record_bytes(s) + sums_bytes(s));

@@ -52,12 +52,13 @@ struct AttendArgs {
     float entry;   // table entries are cb[c] * entry
     float factor;  // log2(e) * softmax_scale / entry
     // workspace (null: no job is split)
-    uint32_t *jobs; // how many there are
-    int4 *records;  // of each: sequence, number in it, the wavefront that begins it, parts (0: one wavefront does all of it)
+    uint32_t *n_records;
+    int4 *records;  // of a job: sequence, number in it, the part it begins with, parts (0: it has none, one wavefront did all of it)
     float2 *sums;   // per part: largest score and sum of weights of each query row
     float *parts;   // per part: weighted values [rows][DP]
     uint32_t rows;  // query rows of a part: as many as a job has at most
     uint32_t in_a_row;  // whether a job's parts lie one after the other, from the number in its record on
+    uint32_t by_wave;   // whether the records are those of the job that a wavefront begins and leaves to others, if any, else of all jobs
 };
 
 // A sequence's part of the work.
@@ -270,11 +271,14 @@ __device__ __forceinline__ uint32_t word_of(const typename Bytes<N>::type &v, in
 
 // A load from a uniform address plus a lane's 32-bit byte offset.  The offset is made to look new each time, or its extension to 64 bits is
 // kept for the whole loop and added to the base by the vector unit: two registers and an instruction per load.
-template <typename T>
+// ONCE: nobody reads it again in this call; it need not stay in the caches.
+template <typename T, bool ONCE = false>
 __device__ __forceinline__ T load_at(const void *uniform_base, uint32_t byte)
 {
     asm volatile("" : "+v"(byte));
-    return *(const DQ8_GLOBAL T *)(uniform_global(static_cast<const char *>(uniform_base)) + byte);
+    const DQ8_GLOBAL T *p = (const DQ8_GLOBAL T *)(uniform_global(static_cast<const char *>(uniform_base)) + byte);
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    return *p;
 }
 
 // The page numbers of 64 tiles from `first` on, in the lanes, so that a tile's addresses wait for no load.
@@ -317,7 +321,7 @@ struct TileData {
     bool valid[2];  // whether the half's page is one of the cache
 };
 
-template <int DP>
+template <int DP, bool ONCE>
 __device__ __forceinline__ void fetch(const AttendArgs &a, const Pages &p, uint32_t head, uint32_t lane, const Walk &w, TileData<DP> &d)
 {
     constexpr uint32_t CPL = DP / 16;
@@ -331,11 +335,11 @@ __device__ __forceinline__ void fetch(const AttendArgs &a, const Pages &p, uint3
         const uint64_t row = (((uint64_t)(d.valid[h] ? page : 0) * a.kv_heads + head) << a.page_shift) + (token & ((1u << a.page_shift) - 1));
         const uint8_t *kc = a.k_codes + row * a.dim, *vc = a.v_codes + row * a.dim;
 #pragma unroll
-        for (int c = 0; c < TileData<DP>::KL; ++c) d.k[h][c] = load_at<u4>(kc, behind ? 0 : n * a.dim + (64 * c + 16 * g < a.dim ? 64 * c + 16 * g : 0));
-        d.ks[h] = load_at<v4>(a.k_scales + row, 16 * g);
+        for (int c = 0; c < TileData<DP>::KL; ++c) d.k[h][c] = load_at<u4, ONCE>(kc, behind ? 0 : n * a.dim + (64 * c + 16 * g < a.dim ? 64 * c + 16 * g : 0));
+        d.ks[h] = load_at<v4, ONCE>(a.k_scales + row, 16 * g);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) d.v[4 * h + r] = load_at<typename Bytes<CPL>::type>(vc, behind ? 0 : (4 * g + r) * a.dim + (n * CPL < a.dim ? n * CPL : 0));
-        d.vs[h] = load_at<v4>(a.v_scales + row, 16 * g);
+        for (int r = 0; r < 4; ++r) d.v[4 * h + r] = load_at<typename Bytes<CPL>::type, ONCE>(vc, behind ? 0 : (4 * g + r) * a.dim + (n * CPL < a.dim ? n * CPL : 0));
+        d.vs[h] = load_at<v4, ONCE>(a.v_scales + row, 16 * g);
     }
 }
 
@@ -344,6 +348,11 @@ __device__ __forceinline__ void fetch(const AttendArgs &a, const Pages &p, uint3
 //
 template <int DP, int NT>
 constexpr bool kQueryInLds = DP * NT > 128;
+
+// With one group of 16 rows of shorter heads there is one job per sequence and cached head, and a tile is read once (402 MB: 78 -> 74
+// us); with more rows two jobs may read it (64 rows, 180 MB: 46 us through the caches, 50 past them).
+template <int DP, int NT>
+constexpr bool kOnce = DP <= 128 && NT == 1;
 
 template <int DP, int NT, typename T>
 __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32_t b, uint32_t q_tile, uint32_t head, uint32_t t0, uint32_t t1, int32_t part,
@@ -534,16 +543,16 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
     // branch around them makes the waits for older loads wait for all); behind the last tile all lanes load its first row.
     Walk walk{tile, end, 0};
     TileData<DP> x, y;
-    fetch<DP>(a, pages, head, lane, walk, x);
+    fetch<DP, kOnce<DP, NT>>(a, pages, head, lane, walk, x);
     for (;;) {
         const uint32_t one = walk.tile;
         walk.step(a, pages, lane);
-        fetch<DP>(a, pages, head, lane, walk, y);
+        fetch<DP, kOnce<DP, NT>>(a, pages, head, lane, walk, y);
         work(one, x);
         if (walk.done()) break;
         const uint32_t two = walk.tile;
         walk.step(a, pages, lane);
-        fetch<DP>(a, pages, head, lane, walk, x);
+        fetch<DP, kOnce<DP, NT>>(a, pages, head, lane, walk, x);
         work(two, y);
         if (walk.done()) break;
     }
@@ -592,7 +601,9 @@ __global__ __launch_bounds__(kAttendWg, 2) void k_cache_attend(const uint32_t *_
     place_half_table(request_lut(tab), a.entry, lds);
     const Share share = share_of(a, 16 * NT, w);
     __syncthreads();
-    if (a.parts && w == 0 && (threadIdx.x & 63) == 0) *a.jobs = share.jobs;
+    const bool first = (threadIdx.x & 63) == 0;
+    if (a.parts && w == 0 && first) *a.n_records = a.by_wave ? gridDim.x * kAttendWaves : share.jobs;
+    bool recorded = false;
     uint32_t b = share.b, place = share.place, at = share.begin, before = share.before;
     while (at < share.end && b < a.batch) {
         const Seq s = sequence(a, b, 16 * NT);
@@ -610,40 +621,54 @@ __global__ __launch_bounds__(kAttendWg, 2) void k_cache_attend(const uint32_t *_
             const uint32_t left = share.end - at;
             if (left < t1 - t0) t1 = t0 + left;
             if (t0 > 0 || t1 < s.tiles) part = 2 * (int32_t)w + (t0 == 0);
-            if (t0 == 0 && (threadIdx.x & 63) == 0)  // where it does not end here: the wavefronts whose parts reach its end
-                a.records[before + job] = int4{(int)b, (int)job, (int)w, t1 < s.tiles ? (int)(share.upto(at + s.tiles) - w) : 0};
+            if (t0 == 0 && (!a.by_wave || t1 < s.tiles)) {  // where it does not end here: the wavefronts whose parts reach its end
+                recorded = true;
+                if (first) a.records[a.by_wave ? w : before + job] = int4{(int)b, (int)job, (int)w, t1 < s.tiles ? (int)(share.upto(at + s.tiles) - w) : 0};
+            }
         }
         // without a workspace, whole jobs: those that begin in this part
         if (a.parts || t0 == 0) attend<DP, NT, T>(a, s, b, job / a.kv_heads, job % a.kv_heads, t0, t1, part, lds, query);
         place += t1 - t0;
         at += t1 - t0;
     }
+    if (a.parts && a.by_wave && !recorded && first) a.records[w] = int4{0, 0, 0, 0};
 }
 
-// The jobs that several wavefronts worked on, one per workgroup in x, kSlice of its rows in y.  A part lies far away (another die's
-// cache wrote it), so that what counts is how many loads are in flight: a thread has four elements of a row, groups of threads take
-// every so manieth part, and the groups' sums are added in LDS.
-constexpr int kSlice = 4, kJoinParts = 256;
+// The jobs that several wavefronts worked on, one per workgroup in x, SLICE of its rows in y.  A part lies far away (another die's
+// cache wrote it), so that what counts is how many loads are in flight and how few wait for each other: a thread has four elements of
+// a row, groups of threads take every so manieth part, the first of them before anything is known of the sums, and the groups' sums are
+// added in LDS.
+constexpr int kJoinParts = 256, kJoinAhead = 4;
 
-template <int DP, uint32_t ROWS, int WG, typename T>
+template <int DP, uint32_t ROWS, int SLICE, int WG, typename T>
 __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
 {
-    constexpr uint32_t QUADS = DP / 4, CELLS = kSlice * QUADS, GROUPS = WG / CELLS;
-    static_assert(WG % CELLS == 0, "whole groups");
-    __shared__ float factor[kJoinParts * kSlice];  // of a part and row: exp2(its largest score - the largest of all)
-    __shared__ float largest[kSlice], weights[kSlice];
+    constexpr uint32_t QUADS = DP / 4, CELLS = SLICE * QUADS, GROUPS = WG / CELLS;
+    static_assert(WG % CELLS == 0 && WG >= SLICE * kWave, "whole groups, a wavefront per row");
+    __shared__ float factor[kJoinParts * SLICE];  // of a part and row: exp2(its largest score - the largest of all)
+    __shared__ float largest[SLICE], weights[SLICE];
     __shared__ v4 sums[WG];
-    if (blockIdx.x >= *a.jobs) return;
-    const int4 record = a.records[blockIdx.x];
+    const uint32_t records = *a.n_records;
+    const int4 record = a.records[blockIdx.x];  // (there is room for as many as the grid has)
+    if (blockIdx.x >= records) return;
     const uint32_t w = (uint32_t)record.z, parts = (uint32_t)record.w;
     if (parts == 0) return;
     auto part_of = [&](uint32_t i) { return a.in_a_row ? (size_t)w + i : 2 * ((size_t)w + i) + (i == 0); };
     const Seq s = sequence(a, (uint32_t)record.x, ROWS);
     const uint32_t head = (uint32_t)record.y % a.kv_heads, q_tile = (uint32_t)record.y / a.kv_heads;
     const uint32_t left = s.n * a.group - q_tile * ROWS, rows = left < ROWS ? left : ROWS;  // of this job
-    const uint32_t first = blockIdx.y * kSlice;
+    const uint32_t first = blockIdx.y * SLICE;
     if (first >= rows) return;
-    if (threadIdx.x < kSlice * kWave) {  // a wavefront looks at a row's parts
+    const uint32_t group = threadIdx.x / CELLS, cell = threadIdx.x % CELLS, row = cell / QUADS, d = 4 * (cell % QUADS);
+    const bool mine = first + row < rows;
+    const float *p = a.parts + (size_t)(mine ? first + row : first) * DP + d;
+    v4 ahead[kJoinAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kJoinAhead; ++k) {
+        const uint32_t i = group + k * GROUPS;
+        ahead[k] = *reinterpret_cast<const v4 *>(p + part_of(i < parts ? i : 0) * a.rows * DP);
+    }
+    if (threadIdx.x < SLICE * kWave) {  // a wavefront looks at a row's parts
         const uint32_t row = first + (threadIdx.x >> 6);
         float top = kNothing, l = 0.0f;
         if (row < rows)
@@ -664,20 +689,23 @@ __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
             weights[threadIdx.x >> 6] = l;
         }
     }
-    const uint32_t group = threadIdx.x / CELLS, cell = threadIdx.x % CELLS, row = cell / QUADS, d = 4 * (cell % QUADS);
-    const bool mine = first + row < rows;
-    const float *p = a.parts + (size_t)(first + row) * DP + d;
     v4 v = {0, 0, 0, 0};
     for (uint32_t i0 = 0; i0 < parts; i0 += kJoinParts) {
         const uint32_t some = parts - i0 < kJoinParts ? parts - i0 : kJoinParts;
         __syncthreads();
-        for (uint32_t x = threadIdx.x; x < some * kSlice; x += WG)
-            if (first + x % kSlice < rows)
-                factor[x] = __builtin_amdgcn_exp2f(a.sums[part_of(i0 + x / kSlice) * a.rows + first + x % kSlice].x - largest[x % kSlice]);
+        for (uint32_t x = threadIdx.x; x < some * SLICE; x += WG)
+            if (first + x % SLICE < rows)
+                factor[x] = __builtin_amdgcn_exp2f(a.sums[part_of(i0 + x / SLICE) * a.rows + first + x % SLICE].x - largest[x % SLICE]);
         __syncthreads();
         if (mine) {
+            uint32_t i = group;
+            if (i0 == 0) {
+#pragma unroll
+                for (uint32_t k = 0; k < kJoinAhead; ++k, i += GROUPS)
+                    if (i < some) v += ahead[k] * factor[i * SLICE + row];
+            }
 #pragma unroll 4
-            for (uint32_t i = group; i < some; i += GROUPS) v += *reinterpret_cast<const v4 *>(p + part_of(i0 + i) * a.rows * DP) * factor[i * kSlice + row];
+            for (; i < some; i += GROUPS) v += *reinterpret_cast<const v4 *>(p + part_of(i0 + i) * a.rows * DP) * factor[i * SLICE + row];
         }
     }
     if (GROUPS > 1) {
@@ -685,7 +713,7 @@ __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
         __syncthreads();
     }
     if (group == 0 && mine && d < a.dim) {
-#pragma unroll
+#pragma unroll 8
         for (uint32_t o = 1; o < GROUPS; ++o) v += sums[o * CELLS + cell];
         const float r = weights[row] == 0.0f ? 0.0f : 1.0f / (weights[row] * a.entry);
         const uint32_t at = q_tile * ROWS + first + row, token = at / a.group;

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const uint32_t lane = threadIdx.x & 63, wave = wave_in_wg(), n = lane & 31, hh = lane >> 5, lane4 = lane * 4;
     // the last query rows of a sequence see most: they begin first
     const Place place = place_of(a, S::kRows, blockIdx.x / splits);
-    if (a.parts && blockIdx.x == 0 && threadIdx.x == 0) *a.jobs = place.jobs;
+    if (a.parts && blockIdx.x == 0 && threadIdx.x == 0) *a.n_records = place.jobs;
     if (blockIdx.x / splits >= place.jobs) return;
     {
         const _Float16 h = (_Float16)(u2f(tab[kCbOff + (threadIdx.x & 255)]) * a.entry);
