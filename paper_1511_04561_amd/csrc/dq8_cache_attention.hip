@@ -23,7 +23,7 @@ struct Shape {
     size_t records;    // of jobs that may be cut into parts
     unsigned rows;     // query rows of a job, at most
     size_t parts;      // that can be written
-    bool many;         // whether a job is cut into more than about sixteen of them
+    bool few;          // whether the join has few rows
 };
 
 constexpr size_t kChunkFrom = 64;  // query rows per cached head of a sequence from which on the kernel for many is faster
@@ -45,13 +45,13 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     if (s.chunk) {
         const size_t tiles = (capacity + 63) / 64;
         size_t splits = s.jobs ? (size_t)cus / s.jobs : 1;
-        if (splits > tiles / 4) splits = tiles / 4;
+        if (splits > tiles / 2) splits = tiles / 2;
         s.splits = splits < 1 ? 1 : (unsigned)splits;
         s.groups = (unsigned)(s.jobs * s.splits);
         s.parts = s.splits > 1 ? s.groups : 0;
         s.work = s.jobs * s.splits;
         s.records = s.jobs;
-        s.many = s.splits > 16;
+        s.few = s.records * s.rows <= 2 * (size_t)cus;
         return s;
     }
     s.splits = 1;
@@ -63,7 +63,7 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     s.groups = (unsigned)groups;
     s.parts = groups * kAttendWaves * 2;
     s.records = s.jobs < groups * kAttendWaves ? s.jobs : groups * kAttendWaves;  // a wavefront leaves one job at most to others
-    s.many = s.jobs * 16 <= groups * kAttendWaves;
+    s.few = s.records * s.rows <= 2 * (size_t)cus;
     return s;
 }
 
@@ -124,7 +124,7 @@ int check_arrays(const char *who, const dq8_cache *cache, const dq8_attention &a
 template <int DP, uint32_t ROWS, typename T>
 int launch_join(const AttendArgs &k, const Shape &s, hipStream_t stream)
 {
-    if (s.many)
+    if (s.few)
         hipLaunchKernelGGL((k_cache_join<DP, ROWS, 1, 1024, T>), dim3((unsigned)s.records, s.rows), dim3(1024), 0, stream, k);
     else
         hipLaunchKernelGGL((k_cache_join<DP, ROWS, 4, 256, T>), dim3((unsigned)s.records, (s.rows + 3) / 4), dim3(256), 0, stream, k);
