@@ -26,7 +26,19 @@ struct Shape {
     bool few;          // whether the join has few rows
 };
 
-constexpr size_t kChunkFrom = 64;  // query rows per cached head of a sequence from which on the kernel for many is faster
+// Which kernel has the query rows of a cached head and sequence, up to 16 of them the one for few.  us, 8 cached heads of 128 (in
+// parentheses of 64), few | many:
+//   one sequence of 8192, 20 rows 29 | 25 (22 | 19), 64 rows 34 | 28 (28 | 22);  of 1024, 20 rows 18 | 18, 96 rows 23 | 19;
+//   of 400, 20 rows 17 | 21, 96 rows 21 | 22;  2 of 16384, 20 rows 34 | 54 (24 | 42), 96 rows 61 | 59 (39 | 43);
+//   16 of 4096, 20 rows 43 | 95 (27 | 72), 96 rows 92 | 103 (56 | 77), 128 rows 104 | 106 (66 | 79), 192 rows 149 | 114 (94 | 87)
+// A tile costs the one for many as much whatever the rows, but it leaves a part per workgroup to the join and not one per wavefront: it has
+// them above 128 rows, and fewer where its workgroups have a few tiles each of sequences that are not short.  Heads of 256, whose keys
+// and values the one for few reads again for every 16 rows: 16 of 4096, 64 rows 304 | 391, 68 rows 418 | 400.
+bool for_many(size_t rows, int dp, size_t jobs, size_t tiles, int cus)
+{
+    if (dp == 256) return rows > 64;
+    return rows > 128 || (rows > 16 && tiles >= 16 && jobs <= 4 * (size_t)cus / tiles);
+}
 
 Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
 {
@@ -36,16 +48,17 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     size_t new_tokens = a.starts ? (a.max_new ? a.max_new : a.tokens) : a.tokens / a.batch;
     if (new_tokens > a.tokens) new_tokens = a.tokens;
     const size_t rows = new_tokens * group;
-    s.chunk = rows > kChunkFrom;
-    s.rows16 = rows <= 16 || s.dp == 256 ? 1 : 2;
+    const size_t capacity = a.max_pages * (size_t)c->page_size, tiles64 = (capacity + 63) / 64;
+    s.chunk = for_many(rows, s.dp, a.batch * (size_t)c->kv_heads, tiles64, cus);
+    s.rows16 = rows <= 16 || s.dp == 256 ? 1 : 2;  // (16 sequences of 4096, 64 rows: 101 us with groups of 16, 66 of 32; 16 rows 36, 48)
     const size_t per = s.chunk ? 32 * kChunkWaves : 16 * (size_t)s.rows16;
     s.jobs = (a.starts ? a.tokens * group / per + a.batch : a.batch * ((rows + per - 1) / per)) * (size_t)c->kv_heads;
     s.rows = (unsigned)(!a.starts && rows < per ? rows : per);
-    const size_t capacity = a.max_pages * (size_t)c->page_size;
     if (s.chunk) {
-        const size_t tiles = (capacity + 63) / 64;
+        // Idle compute units take parts of jobs, of two tiles at least (two sequences' heads, 256 rows, 2048 tokens: 94 us undivided, 28 with
+        // parts of four tiles, 25 of two; 512 tokens 32, 27, 22).
         size_t splits = s.jobs ? (size_t)cus / s.jobs : 1;
-        if (splits > tiles / 2) splits = tiles / 2;
+        if (splits > tiles64 / 2) splits = tiles64 / 2;
         s.splits = splits < 1 ? 1 : (unsigned)splits;
         s.groups = (unsigned)(s.jobs * s.splits);
         s.parts = s.splits > 1 ? s.groups : 0;
@@ -57,9 +70,10 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     s.splits = 1;
     const size_t tiles = (capacity + kTile - 1) / kTile;
     s.work = s.jobs > SIZE_MAX / 2 / tiles ? SIZE_MAX / 2 : s.jobs * tiles;
-    size_t groups = (size_t)cus;  // one table per compute unit, eight wavefronts of 256 registers
-    const size_t useful = (s.work + kAttendWaves * kLeastTiles - 1) / (kAttendWaves * kLeastTiles);
-    if (groups > useful) groups = useful;
+    // One table per compute unit, eight wavefronts of 256 registers, a tile at least for each (one sequence of 1337: 14 us; two tiles: 16,
+    // four: 22).
+    size_t groups = (size_t)cus;
+    if (groups > (s.work + kAttendWaves - 1) / kAttendWaves) groups = (s.work + kAttendWaves - 1) / kAttendWaves;
     s.groups = (unsigned)groups;
     s.parts = groups * kAttendWaves * 2;
     s.records = s.jobs < groups * kAttendWaves ? s.jobs : groups * kAttendWaves;  // a wavefront leaves one job at most to others
@@ -124,6 +138,8 @@ int check_arrays(const char *who, const dq8_cache *cache, const dq8_attention &a
 template <int DP, uint32_t ROWS, typename T>
 int launch_join(const AttendArgs &k, const Shape &s, hipStream_t stream)
 {
+    // Few rows leave most compute units idle: a workgroup of sixteen wavefronts for each, to have its parts on their way at once (one sequence
+    // of 16384: 22 us, with the other 33; 80 rows of each of 16 sequences of 4096: 55, with the other 44).
     if (s.few)
         hipLaunchKernelGGL((k_cache_join<DP, ROWS, 1, 1024, T>), dim3((unsigned)s.records, s.rows), dim3(1024), 0, stream, k);
     else

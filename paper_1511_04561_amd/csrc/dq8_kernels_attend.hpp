@@ -33,7 +33,6 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kTile = 32;          // tokens that a wavefront takes at a time
 constexpr int kAttendWaves = 8;    // of a workgroup: they share one table
 constexpr int kAttendWg = kAttendWaves * kWave;
-constexpr uint32_t kLeastTiles = 1;  // of a wavefront's part, where there are as many
 constexpr int kQueryTop = 14;      // a query row's largest element is in [2^14, 2^15) in binary16
 constexpr float kSlack = 8.0f;     // how far a score may be above the reference of its row's weights (in powers of two)
 constexpr int kWeightTop = 6;      // a value scale is below 2^7 where it multiplies a weight, the product below 2^15
@@ -166,8 +165,7 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, uint32_t rows, ui
     const uint32_t total = (uint32_t)all;
     Share s;
     s.jobs = (uint32_t)(all >> 32);
-    const uint32_t most = (total + kLeastTiles - 1) / kLeastTiles;
-    s.waves = gridDim.x * kAttendWaves < most ? gridDim.x * kAttendWaves : most;
+    s.waves = gridDim.x * kAttendWaves < total ? gridDim.x * kAttendWaves : total;
     s.per = s.waves ? total / s.waves : 0;
     s.more = total - s.per * s.waves;
     s.b = s.place = s.begin = s.end = s.before = 0;

@@ -88,7 +88,7 @@ def test_the_structs_are_those_of_the_header(tmp_path):
 CACHE_REFUSALS = [(2, -1, {}), (2, 4, {}), (1, 0, {"codes": None}), (1, 0, {"scales": None}), (3, 0, {"codes": at(0, 8)}), (3, 0, {"scales": at(1, 4)}),
                   (3, 0, {"dim": 0}), (3, 0, {"dim": 24}), (3, 0, {"dim": 272}), (3, 0, {"dim": -16}), (3, 0, {"page_size": 8}), (3, 0, {"page_size": 48}),
                   (3, 0, {"page_size": 2048}), (3, 0, {"page_size": 0}), (3, 0, {"kv_heads": 0}), (3, 0, {"kv_heads": 70000}), (3, 0, {"pages": 0}),
-                  (3, 0, {"pages": 1 << 27}), (3, 0, {"pages": 1 << 63})]
+                  (3, 0, {"pages": 1 << 27}), (3, 0, {"pages": 1 << 63}), (3, 0, {"kv_heads": 8192, "page_size": 1024, "dim": 256, "pages": 1})]
 
 
 @pytest.mark.parametrize("status,kind,change", CACHE_REFUSALS)

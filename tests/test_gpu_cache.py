@@ -183,6 +183,10 @@ ATTENTIONS = [
     (3, "f16", 4, 4, 32, 64, [(257, 400), (100, 64)], 70),
     (0, "bf16", 5, 1, 128, 16, [(64, 1000), (0, 0), (90, 60), (1, 1)], 0),
     (0, "f16", 16, 2, 96, 16, [(33, 63), (40, 64), (41, 65), (9, 0)], 31),
+    # some rows of a few sequences that are not short: the same kernel, jobs cut into parts, of which some lie behind a window
+    (0, "bf16", 4, 1, 128, 64, [(5, 1500)], 0),
+    (1, "f16", 6, 2, 64, 32, [(9, 1100), (11, 1030), (0, 700), (7, 3)], 200),
+    (2, "bf16", 8, 2, 112, 128, [(8, 1025), (8, 2049)], 0),
 ]
 
 
@@ -370,7 +374,7 @@ def near(got, want):
 def test_attention_of_long_sequences_and_many(dq8):
     """Work cut over the token axis: one long history, many short ones, and more sequences than a workgroup has threads."""
     g = torch.Generator(device="cuda").manual_seed(3)
-    for batch, longest, heads, kv, dim, page in ((1, 70001, 8, 1, 128, 64), (600, 90, 4, 2, 64, 16), (3, 9000, 32, 8, 128, 128)):
+    for batch, longest, heads, kv, dim, page in ((1, 70001, 8, 1, 128, 64), (600, 90, 4, 2, 64, 16), (701, 70, 8, 4, 80, 16), (3, 9000, 32, 8, 128, 128)):
         per = -(-longest // page)
         pool = batch * per + 1
         codes = torch.randint(0, 256, (2, pool, kv, page, dim), dtype=torch.uint8, device="cuda", generator=g)
@@ -438,18 +442,19 @@ def test_prompt_chunks_and_decoding_equal_one_pass(dq8):
     assert torch.isfinite(values).all() and values.abs().max() > 0
 
 
-def test_cache_calls_recorded_in_a_graph(dq8):
-    """A decoding step captured once and replayed with new inputs and lengths, eager work and synchronisations between."""
-    kind, batch, heads, kv, dim, page, most = 0, 3, 8, 2, 128, 16, 320
+@pytest.mark.parametrize("n,most", [(1, 320), (12, 1280)])
+def test_cache_calls_recorded_in_a_graph(dq8, n, most):
+    """A step of one or more tokens captured once and replayed with new inputs and lengths, eager work and synchronisations between."""
+    kind, batch, heads, kv, dim, page = 0, 3, 8, 2, 128, 16
     g = torch.Generator(device="cuda").manual_seed(5)
     codes, scales = dq8.cache_buffers(batch * most // page, kv, page, dim)
     codes.random_(0, 256, generator=g)
     scales.uniform_(0.5, 1.5, generator=g)
     pages = torch.randperm(batch * most // page, device="cuda", generator=g).to(torch.int32).view(batch, -1)
-    x = torch.zeros((batch, heads + 2 * kv, dim), dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros((batch * n, heads + 2 * kv, dim), dtype=torch.bfloat16, device="cuda")
     q, k, v = x.split([heads, kv, kv], 1)
-    slots, lens = torch.zeros(batch, dtype=torch.int64, device="cuda"), torch.zeros(batch, dtype=torch.int32, device="cuda")
-    q2, out = torch.empty((batch, heads, dim), dtype=torch.bfloat16, device="cuda"), torch.empty((batch, heads, dim), dtype=torch.bfloat16, device="cuda")
+    slots, lens = torch.zeros(batch * n, dtype=torch.int64, device="cuda"), torch.zeros(batch, dtype=torch.int32, device="cuda")
+    q2, out = (torch.empty((batch * n, heads, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
     space = torch.empty(dq8.cache_attention_workspace(q, codes, scales, pages, lens), dtype=torch.uint8, device="cuda")
     stream = torch.cuda.Stream()
     graph = torch.cuda.CUDAGraph()
@@ -459,9 +464,10 @@ def test_cache_calls_recorded_in_a_graph(dq8):
         dq8.cache_attention(kind, q2, codes, scales, pages, lens, out=out, workspace=space)
     for rep in range(4):
         x.copy_(torch.randn(x.shape, device="cuda", generator=g))
-        length = torch.randint(1, most + 1, (batch,), device="cuda", generator=g)
+        length = torch.randint(n, most + 1, (batch,), device="cuda", generator=g)
         lens.copy_(length)
-        slots.copy_(pages.long().gather(1, ((length - 1) // page)[:, None])[:, 0] * page + (length - 1) % page)
+        j = length[:, None] - n + torch.arange(n, device="cuda")
+        slots.copy_((pages.long().gather(1, j // page) * page + j % page).reshape(-1))
         other = codes.clone(), scales.clone()
         dq8.cache_append(kind, k, v, slots, *other)
         eager = dq8.cache_attention(kind, q, *other, pages, lens, workspace=torch.empty(space.numel(), dtype=torch.uint8, device="cuda"))
@@ -578,3 +584,13 @@ def test_refusals(dq8):
             pytest.fail("refusal %d" % i)
     torch.cuda.synchronize()
     assert not codes.any() and not scales.any()
+
+
+def test_work_of_2_to_the_31_tiles_is_refused(dq8):
+    """64 heads of one sequence whose pages would hold 2^30 tokens; the sequence itself has one."""
+    codes, scales = dq8.cache_buffers(1, 64, 1024, 16)
+    q = torch.ones((1, 64, 16), dtype=torch.float16, device="cuda")
+    pages, lens = torch.zeros((1, 1 << 20), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(dq8.Dq8Error, match="too much work"):
+        dq8.cache_attention(0, q, codes, scales, pages, lens)
+    assert not dq8.cache_attention(0, q, codes, scales, pages[:, :1 << 18], lens).any()
