@@ -64,7 +64,7 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
         s.parts = s.splits > 1 ? s.groups : 0;
         s.work = s.jobs * s.splits;
         s.records = s.jobs;
-        s.few = s.records * s.rows <= 2 * (size_t)cus;
+        s.few = s.records * s.rows <= (size_t)cus;
         return s;
     }
     s.splits = 1;
@@ -77,7 +77,7 @@ Shape shape_of(const dq8_cache *c, const dq8_attention &a, int cus)
     s.groups = (unsigned)groups;
     s.parts = groups * kAttendWaves * 2;
     s.records = s.jobs < groups * kAttendWaves ? s.jobs : groups * kAttendWaves;  // a wavefront leaves one job at most to others
-    s.few = s.records * s.rows <= 2 * (size_t)cus;
+    s.few = s.records * s.rows <= (size_t)cus;
     return s;
 }
 

@@ -347,10 +347,11 @@ __device__ __forceinline__ void fetch(const AttendArgs &a, const Pages &p, uint3
 template <int DP, int NT>
 constexpr bool kQueryInLds = DP * NT > 128;
 
-// With one group of 16 rows of shorter heads there is one job per sequence and cached head, and a tile is read once (402 MB: 78 -> 74
-// us); with more rows two jobs may read it (64 rows, 180 MB: 46 us through the caches, 50 past them).
+// With one group of 16 rows there is one job per sequence and cached head, and a tile is read once: past the caches (64 sequences of
+// 4096 at most: 73 us through them, 66 past; two of 131072: 87 and 84).  With more rows two jobs may read it (180 MB, 20 rows of each
+// of 16: 46 us and 50), and rows of 64 bytes are half a line that two loads share (75 MB: 26.8 and 28.3).
 template <int DP, int NT>
-constexpr bool kOnce = DP <= 128 && NT == 1;
+constexpr bool kOnce = DP == 128 && NT == 1;
 
 template <int DP, int NT, typename T>
 __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32_t b, uint32_t q_tile, uint32_t head, uint32_t t0, uint32_t t1, int32_t part,
