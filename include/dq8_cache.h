@@ -33,7 +33,7 @@ enum {
 /*
  * The cache.  codes: [2][pages][kv_heads][page_size][dim] bytes, keys before values; scales: [2][pages][kv_heads][page_size] floats; both
  * at a multiple of 16 bytes.  dim: a multiple of 16 up to DQ8_CACHE_MAX_DIM; page_size: a power of two from 16 to
- * DQ8_CACHE_MAX_PAGE.  Slot s is place s % page_size of page s / page_size.  The row of token slot s and head h stands for
+ * DQ8_CACHE_MAX_PAGE; kv_heads * page_size * dim below 2^31, pages * page_size too.  Slot s is place s % page_size of page s / page_size.  The row of token slot s and head h stands for
  * dq8_decode of its codes with its scale.
  */
 typedef struct {
@@ -95,8 +95,10 @@ int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_append *a, void
  * max_new: the largest number of new tokens of a sequence, as far as the host knows (0: unknown); it chooses between kernels that are
  * right for any number.
  * workspace: dq8_cache_attention_workspace_bytes bytes at a multiple of 16, whose contents are of no meaning before and after; calls that
- * may run at the same time must not share it.  Without (NULL, or too few bytes) one workgroup reads the whole of a sequence's head:
- * slow where there are few sequences.
+ * may run at the same time must not share it.  Without (NULL, or too few bytes) one wavefront or workgroup reads the whole of a
+ * sequence's head: slow where there are few sequences.  The call that asks for its size has the tokens, batch, max_pages, heads, type
+ * and max_new of the call that uses it, and starts if that has starts.
+ * Work that 32 bits do not count (query rows in groups of 16 to 256, times cached heads, times max_pages * page_size / 32: 2^31) is refused.
  */
 typedef struct {
     int type;

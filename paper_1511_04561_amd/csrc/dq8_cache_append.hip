@@ -7,6 +7,9 @@
 // every head, so that the angles and weights, four times the bytes of a row of 16-bit elements, are loaded once per item.  The steps
 // are a loop and not written out: the calls of a decoding step run through this code once, and what they wait for then is the code
 // itself (2077 tokens of 12 heads in binary32: 20 us with four steps written out, 13 with the loop).
+//
+// What bounds it: the vector unit for many rows, busy for 87 % of 54 us at 8191 tokens with 32 + 8 + 8 heads of 128, norms and a rotation (185
+// MB, 3.4 TB/s; 35 us at the rates of a large copy; without norms 43 us).  Few tokens take a launch and a chain of loads, 4 to 5 us.
 #include <hip/hip_runtime.h>
 
 #include "dq8_cache_check.hpp"
@@ -356,11 +359,12 @@ extern "C" int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_appe
     k.half = a.rotation ? (uint32_t)a.half : 0, k.interleaved = a.interleaved != 0;
     k.page_shift = (uint32_t)__builtin_ctz((unsigned)cache->page_size);
     const int lpr = dim <= 64 ? 8 : dim <= 128 ? 16 : 32;
-    // Items of four times the heads that a wavefront has at once where there are many, of one time where every wavefront counts.
+    // Items of four times the heads that a wavefront has at once where there are many, of one time where every wavefront counts (32 + 8 + 8 heads
+    // of 128 in 16 bits, us with one | four: 64 tokens 4.5 | 5.6, 256 5.5 | 5.9, 512 7.9 | 6.7, 2048 19 | 13, 8192 59 | 42).
     const size_t at_once = (size_t)(kWave / lpr), heads = (size_t)a.heads;
     auto items = [&](size_t steps) { return a.tokens * ((heads + at_once * steps - 1) / (at_once * steps) + 2 * ((kv + at_once * steps - 1) / (at_once * steps))); };
-    k.item_steps = items(4) >= (size_t)dev.cus * 16 ? 4 : 1;
-    const size_t per = at_once * k.item_steps, most = (size_t)dev.cus * 5;  // that are resident
+    k.item_steps = items(4) >= (size_t)dev.cus * 8 ? 4 : 1;
+    const size_t per = at_once * k.item_steps, most = (size_t)dev.cus * 5;  // that are resident (four: 47 us, five 43, eight 43 at 8192)
     const size_t kv_items = 2 * a.tokens * ((kv + per - 1) / per), q_items = a.tokens * ((heads + per - 1) / per);
     size_t kv_groups = (kv_items + kWavesPerWg - 1) / kWavesPerWg, q_groups = (q_items + kWavesPerWg - 1) / kWavesPerWg;
     if (kv_groups + q_groups > most) {

@@ -19,6 +19,11 @@
 // row is scaled by a power of two to a largest element of 2^14 .. 2^15, value scales by a power of two to below 2^7, which the
 // accumulators follow when a larger scale appears.  m need not be the largest score, only near it: it is moved, and the sums with it,
 // when a score exceeds it by more than kSlack, so that weights are at most 2^8 and their products with value scales 2^15.
+//
+// What bounds it: memory, less well used than by a copy.  64 sequences of up to 4096, 8 heads of 128: 292 MB in 60 us (4.9 TB/s) and 5 us of
+// join; two of up to 131072: 391 MB in 74 us (5.3 TB/s) and 7 us; loads alone in the same order reach 6.7.  A wavefront holds two tiles, one
+// in flight; LDS, a look-up per code and its 16-bit half, is busy for 57 % of the time, the vector unit 39 %, the matrix units 7 %.
+// Short calls (one sequence of 1337: 10 us) wait for the instructions themselves, the table and three loads that need each other.
 #pragma once
 #include <cfloat>
 
