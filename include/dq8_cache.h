@@ -58,7 +58,8 @@ typedef struct {
  * but for a value that lies that close to a rounding border.)  Values: compressed as they are.  A row of keys or values that
  * holds an infinity or NaN gets scale NaN and stands for NaN.
  * Queries: evaluated in binary32, rounded once to their type into q_out; q may be NULL with heads == 0.  q_out may be q with its
- * strides; otherwise it must overlap no other array.
+ * strides (k and v may then be parts of the same tokens' rows); otherwise it must overlap no other array.  Its own rows must not overlap:
+ * all heads of a token lie before the next token's, or all tokens of a head before the next head's.
  */
 typedef struct {
     int type; /* DQ8_FLOAT32, DQ8_BFLOAT16 or DQ8_FLOAT16: of q, k, v and q_out */
@@ -79,7 +80,7 @@ typedef struct {
 int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_append *a, void *hip_stream);
 
 /*
- * Attention of new tokens over the cache.  q and out: [tokens][heads][dim], `type` DQ8_BFLOAT16 or DQ8_FLOAT16, strides as above; heads is a
+ * Attention of new tokens over the cache.  q and out: [tokens][heads][dim], `type` DQ8_BFLOAT16 or DQ8_FLOAT16, strides as above (of out as of q_out); heads is a
  * multiple of kv_heads, and query head h reads cached head h / (heads / kv_heads).
  * batch sequences; the new tokens of sequence b are starts[b] .. starts[b + 1] of q (starts: batch + 1 ascending integers), or with starts ==
  * NULL tokens / batch each, which must divide.  lens[b]: tokens of the sequence in the cache, its new ones among them (append

@@ -292,6 +292,7 @@ __global__ __launch_bounds__(kWg, ANY ? 4 : 5) void k_cache_append(const uint32_
 
 }  // namespace
 
+using dq8::apart;
 using dq8::extent;
 using dq8::failed;
 using dq8::meet;
@@ -331,8 +332,8 @@ extern "C" int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_appe
         const void *p;
         size_t n;
     } read[] = {{in_place ? nullptr : a.q, in_place ? 0 : extent(a.tokens, a.q_token_stride, a.heads, a.q_head_stride, dim, size)},
-                {in_place ? nullptr : a.k, extent(a.tokens, a.k_token_stride, kv, a.k_head_stride, dim, size)},
-                {in_place ? nullptr : a.v, extent(a.tokens, a.v_token_stride, kv, a.v_head_stride, dim, size)},
+                {a.k, extent(a.tokens, a.k_token_stride, kv, a.k_head_stride, dim, size)},
+                {a.v, extent(a.tokens, a.v_token_stride, kv, a.v_head_stride, dim, size)},
                 {a.slots, a.tokens * 8},
                 {a.positions, a.positions ? a.tokens * 8 : 0},
                 {a.rotation, a.rotation ? a.n_positions * 2 * (size_t)a.half * 4 : 0},
@@ -340,11 +341,20 @@ extern "C" int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_appe
                 {a.k_weight, a.k_weight ? (size_t)dim * 4 : 0}};
     bool bad = meet(a.q_out, n_out, cache->codes, rows * dim) || meet(a.q_out, n_out, cache->scales, rows * 4) ||
                meet(cache->codes, rows * dim, cache->scales, rows * 4);
+    // keys or values and queries in place that are parts of the same tokens: they lie side by side in each
+    auto beside = [&](const void *p, size_t token_stride, size_t head_stride) {
+        const intptr_t stride = (intptr_t)(a.q_out_token_stride * size);
+        if (!in_place || token_stride != a.q_out_token_stride || stride == 0) return false;
+        const intptr_t from = ((intptr_t)p - (intptr_t)a.q_out) % stride, at = from < 0 ? from + stride : from;
+        return at >= (intptr_t)extent(1, 0, a.heads, a.q_out_head_stride, dim, size) && at + (intptr_t)extent(1, 0, kv, head_stride, dim, size) <= stride;
+    };
     for (const auto &r : read) {
         if (r.p == nullptr) continue;
-        bad = bad || meet(r.p, r.n, cache->codes, rows * dim) || meet(r.p, r.n, cache->scales, rows * 4) || meet(r.p, r.n, a.q_out, n_out);
+        const bool side = (r.p == a.k && beside(a.k, a.k_token_stride, a.k_head_stride)) || (r.p == a.v && beside(a.v, a.v_token_stride, a.v_head_stride));
+        bad = bad || meet(r.p, r.n, cache->codes, rows * dim) || meet(r.p, r.n, cache->scales, rows * 4) || (!side && meet(r.p, r.n, a.q_out, n_out));
     }
-    if (bad) return failed(DQ8_ERR_ARG, "%s: an output overlaps another array", who);
+    bad = bad || !apart(a.tokens, a.q_out_token_stride, a.heads, a.q_out_head_stride, dim);
+    if (bad) return failed(DQ8_ERR_ARG, "%s: an output overlaps another array or itself", who);
     dq8::DeviceTables dev;
     rc = dq8::device_tables(kind, &dev);
     if (rc) return rc;

@@ -131,7 +131,8 @@ int check_arrays(const char *who, const dq8_cache *cache, const dq8_attention &a
                 {a.starts, a.starts ? (a.batch + 1) * 4 : 0}};
     bool bad = workspace && meet(a.out, n_out, workspace, workspace_bytes);
     for (const auto &r : read) bad = bad || meet(a.out, n_out, r.p, r.n) || (workspace && meet(workspace, workspace_bytes, r.p, r.n));
-    if (bad) return failed(DQ8_ERR_ARG, "%s: out or workspace overlaps another array", who);
+    if (bad || !dq8::apart(a.tokens, a.out_token_stride, a.heads, a.out_head_stride, cache->dim))
+        return failed(DQ8_ERR_ARG, "%s: out or workspace overlaps another array or itself", who);
     return DQ8_OK;
 }
 

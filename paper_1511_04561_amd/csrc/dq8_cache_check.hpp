@@ -39,6 +39,15 @@ inline size_t extent(size_t tokens, size_t token_stride, int heads, size_t head_
 // Strides whose products with tokens and heads stay far inside 64 bits.
 inline bool sane(size_t stride) { return stride < (size_t)1 << 40; }
 
+// Whether no two rows of an array that is written overlap: all heads of a token lie before the next token's, or the other way round.
+inline bool apart(size_t tokens, size_t token_stride, int heads, size_t head_stride, int dim)
+{
+    if (tokens == 0 || heads == 0) return true;
+    const size_t t = tokens - 1, h = (size_t)heads - 1, d = (size_t)dim;
+    return ((h == 0 || head_stride >= d) && (t == 0 || token_stride >= h * head_stride + d)) ||
+           ((t == 0 || token_stride >= d) && (h == 0 || head_stride >= t * token_stride + d));
+}
+
 inline bool meet(const void *a, size_t na, const void *b, size_t nb)
 {
     const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;

@@ -92,7 +92,7 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, uint32_t b, uint32_
     s.n = end - s.first;
     const int32_t most = (int32_t)(a.max_pages << a.page_shift), len = a.lens[b];
     s.len = len < 0 ? 0 : len < most ? len : most;
-    int32_t lo = a.window > 0 ? s.len - (int32_t)s.n + 1 - a.window : 0;
+    int32_t lo = a.window > 0 && s.len > (int32_t)s.n ? s.len - (int32_t)s.n + 1 - a.window : 0;
     if (lo < 0) lo = 0;
     s.lo_tile = (uint32_t)lo / kTile;
     const uint32_t hi = ((uint32_t)s.len + kTile - 1) / kTile;

@@ -108,7 +108,8 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const int32_t p0 = s.len - (int32_t)s.n;  // position of the sequence's first query
     // tokens that some row of the workgroup sees: from .. upto - 1
     const uint32_t last_row = row0 + S::kRows < total_rows ? row0 + S::kRows - 1 : total_rows - 1;
-    const int32_t upto = p0 + (int32_t)(last_row / a.group) + 1, lowest = a.window > 0 ? p0 + (int32_t)(row0 / a.group) - a.window + 1 : 0;
+    const int32_t upto = p0 + (int32_t)(last_row / a.group) + 1, first_pos = p0 + (int32_t)(row0 / a.group);
+    const int32_t lowest = a.window > 0 && first_pos > 0 ? first_pos - a.window + 1 : 0;  // (queries before position 0 see nothing)
     const uint32_t first_tile = lowest > 0 ? (uint32_t)lowest / TOKENS : 0, end_tile = upto > 0 ? ((uint32_t)upto + TOKENS - 1) / TOKENS : 0;
     const uint32_t count = end_tile > first_tile ? end_tile - first_tile : 0;
     const uint32_t t_begin = first_tile + (uint32_t)((uint64_t)count * split / splits), t_end = first_tile + (uint32_t)((uint64_t)count * (split + 1) / splits);
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
         const bool late = wave >= kChunkWaves / 2;
         auto seen = [&](uint32_t tile) {
             const int32_t t = (int32_t)(tile * TOKENS);
-            return t <= p_last && (a.window <= 0 || t + TOKENS > p_first - a.window + 1);
+            return t <= p_last && (a.window <= 0 || p_first <= 0 || t + TOKENS > p_first - a.window + 1);
         };
         fetch(t_begin);
         put(0, 0);

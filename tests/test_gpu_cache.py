@@ -304,6 +304,32 @@ def test_attention_of_descending_starts_writes_nothing(dq8, sequences, max_new):
         assert got is out and (out == 7.0).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [5, 60, 300])
+@pytest.mark.parametrize("window", [1, 2 ** 31 - 1])
+def test_attention_of_windows_where_the_first_queries_see_nothing(dq8, dim, n, window):
+    """Sequences with fewer cached tokens than new ones under the smallest and the largest window."""
+    case = (0, "f16", 2, 1, dim, 16, [(n, 2), (n, 0), (n, n - 1), (n, n + 40)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    want, tol = ref.attention(0, cache, host(q), pages, lens, starts, dim ** -0.5, window)
+    cuda = lambda a: torch.from_numpy(a).cuda()
+    for max_new in (1, n):
+        got = dq8.cache_attention(0, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(starts), max_new=max_new, window=window)
+        check_attention(got, q, want, tol)
+        assert not got[:n - 2].any()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 1e-44])
+@pytest.mark.parametrize("n", [2, 140])
+def test_attention_of_any_softmax_scale(dq8, n, scale):
+    case = (0, "f16", 4, 2, 128, 16, [(n, n + 100), (n, n)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    want, tol = ref.attention(0, cache, host(q), pages, lens, starts, scale)
+    cuda = lambda a: torch.from_numpy(a).cuda()
+    got = dq8.cache_attention(0, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), softmax_scale=scale)
+    check_attention(got, q, want, tol)
+
+
 @pytest.mark.parametrize("n", [1, 50])
 def test_attention_of_values_of_very_different_sizes(dq8, n):
     """Scales over thirty-six decades: weights follow the largest so far, whatever the order."""
@@ -558,6 +584,8 @@ def test_refusals(dq8):
         (dq8.Dq8Error, lambda: dq8.cache_append(4, k, k, slots, codes, scales)),
         (dq8.Dq8Error, lambda: dq8.cache_append(0, k, k, slots, codes, scales, k_weight=w, eps=float("nan"))),
         (dq8.Dq8Error, lambda: dq8.cache_append(0, k, k, slots, codes, scales, q=q, q_out=q[:, :, :].as_strided(q.shape, (256, 32, 1)))),
+        (dq8.Dq8Error, lambda: dq8.cache_append(0, k, k, slots, codes, scales, q=q, q_out=torch.empty_like(q[:1]).expand(3, 4, 64))),
+        (dq8.Dq8Error, lambda: dq8.cache_append(0, q[:, 2:], k, slots, codes, scales, q=q, q_out=q)),
         (dq8.Dq8Error, lambda: dq8.cache_append(0, k[:, :, :40], k[:, :, :40], slots, codes[..., :40].contiguous(), scales)),
     ]
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
@@ -572,6 +600,7 @@ def test_refusals(dq8):
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q[:, :3], codes, scales, pages, lens)),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q[:2], codes, scales, pages, lens)),  # two tokens of three sequences
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, out=q)),
+        (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, out=torch.empty_like(q[:, :1]).expand(3, 4, 64))),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, window=-1)),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, softmax_scale=float("inf"))),
         (dq8.Dq8Error, lambda: dq8.cache_attention(9, q, codes, scales, pages, lens)),
