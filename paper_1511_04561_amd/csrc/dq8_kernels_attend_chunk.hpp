@@ -349,9 +349,10 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
         // Half of the wavefronts, one of each SIMD's two, take the weights and sums of a tile together with the next tile's scores: while one
         // of the two uses the vector unit, the other has products to do.  A barrier per tile, two buffers of keys and three of values.
         const bool late = wave >= kChunkWaves / 2;
+        const int32_t low = a.window > 0 && p_first > 0 ? p_first - a.window + 1 : 0, least = low > 0 ? low : 0;  // of the tokens that its rows see
         auto seen = [&](uint32_t tile) {
             const int32_t t = (int32_t)(tile * TOKENS);
-            return t <= p_last && (a.window <= 0 || p_first <= 0 || t + TOKENS > p_first - a.window + 1);
+            return t <= p_last && t > least - TOKENS;
         };
         fetch(t_begin);
         put(0, 0);

@@ -533,6 +533,8 @@ def _attention(q, codes, scales, pages, lens, starts, max_new, softmax_scale, wi
     if starts is not None:
         a.starts = _on(dev, starts, torch.int32, (a.batch + 1,), "starts")
     a.max_new = 0 if max_new is None else int(max_new)
+    if int(window) >= 2 ** 31:
+        raise ValueError("window must be below 2^31")
     a.window = int(window)
     a.softmax_scale = dim ** -0.5 if softmax_scale is None else float(softmax_scale)
     if out is not None:

@@ -602,6 +602,8 @@ def test_refusals(dq8):
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, out=q)),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, out=torch.empty_like(q[:, :1]).expand(3, 4, 64))),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, window=-1)),
+        (ValueError, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, window=2 ** 32 + 5)),
+        (ValueError, lambda: dq8.cache_attention(0, q, codes, scales, torch.zeros((3, 2), dtype=torch.int32, device="cuda")[:, :1], lens)),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, pages, lens, softmax_scale=float("inf"))),
         (dq8.Dq8Error, lambda: dq8.cache_attention(9, q, codes, scales, pages, lens)),
         (dq8.Dq8Error, lambda: dq8.cache_attention(0, q, codes, scales, i32(3, 0), lens)),
