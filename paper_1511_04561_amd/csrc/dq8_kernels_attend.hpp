@@ -59,7 +59,7 @@ struct AttendArgs {
     uint32_t *n_records;
     int4 *records;  // of a job: sequence, number in it, the part it begins with, parts (0: it has none, one wavefront did all of it)
     float2 *sums;   // per part: largest score and sum of weights of each query row
-    float *parts;   // per part: weighted values [rows][DP]
+    float *parts;   // per part: its output [rows][DP], in binary32 as large as the values themselves (their weighted sum may not fit)
     uint32_t rows;  // query rows of a part: as many as a job has at most
     uint32_t in_a_row;  // whether a job's parts lie one after the other, from the number in its record on
     uint32_t by_wave;   // whether the records are those of the job that a wavefront begins and leaves to others, if any, else of all jobs
@@ -566,7 +566,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
     for (int nt = 0; nt < NT; ++nt) {
         sum[nt] = sum_over_groups(sum[nt]);
         const uint32_t local = nt * 16 + n, row = q_tile * NT * 16 + local;
-        const float size = __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop);
+        const float r = sum[nt] == 0.0f ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop) / (sum[nt] * a.entry);
         if (row >= s.n * a.group) continue;
         if (part >= 0) {
             const size_t at = (size_t)part * a.rows + local;
@@ -576,11 +576,10 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
 #pragma unroll
                 for (int j = 0; j < CPL; j += 4)
                     *reinterpret_cast<v4 *>(a.parts + at * DP + CPL * (4 * g + i) + j) =
-                        v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * size;
+                        v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * r;
         } else {
             const uint32_t token = row / a.group;
             T *to = static_cast<T *>(a.out) + (s.first + token) * a.o_ts + (head * a.group + row - token * a.group) * a.o_hs;
-            const float r = sum[nt] == 0.0f ? 0.0f : size / (sum[nt] * a.entry);
             typedef T V __attribute__((ext_vector_type(4)));
             typedef V VA __attribute__((aligned(sizeof(T))));
 #pragma unroll
@@ -649,7 +648,7 @@ __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
 {
     constexpr uint32_t QUADS = DP / 4, CELLS = SLICE * QUADS, GROUPS = WG / CELLS;
     static_assert(WG % CELLS == 0 && WG >= SLICE * kWave, "whole groups, a wavefront per row");
-    __shared__ float factor[kJoinParts * SLICE];  // of a part and row: exp2(its largest score - the largest of all)
+    __shared__ float factor[kJoinParts * SLICE];  // of a part and row: its share of the sum of weights
     __shared__ float largest[SLICE], weights[SLICE];
     __shared__ v4 sums[WG];
     const uint32_t records = *a.n_records;
@@ -698,8 +697,11 @@ __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
         const uint32_t some = parts - i0 < kJoinParts ? parts - i0 : kJoinParts;
         __syncthreads();
         for (uint32_t x = threadIdx.x; x < some * SLICE; x += WG)
-            if (first + x % SLICE < rows)
-                factor[x] = __builtin_amdgcn_exp2f(a.sums[part_of(i0 + x / SLICE) * a.rows + first + x % SLICE].x - largest[x % SLICE]);
+            if (first + x % SLICE < rows) {
+                const float2 o = a.sums[part_of(i0 + x / SLICE) * a.rows + first + x % SLICE];
+                const float all = weights[x % SLICE];
+                factor[x] = all == 0.0f ? 0.0f : o.y * __builtin_amdgcn_exp2f(o.x - largest[x % SLICE]) / all;
+            }
         __syncthreads();
         if (mine) {
             uint32_t i = group;
@@ -719,12 +721,11 @@ __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
     if (group == 0 && mine && d < a.dim) {
 #pragma unroll 8
         for (uint32_t o = 1; o < GROUPS; ++o) v += sums[o * CELLS + cell];
-        const float r = weights[row] == 0.0f ? 0.0f : 1.0f / (weights[row] * a.entry);
         const uint32_t at = q_tile * ROWS + first + row, token = at / a.group;
         typedef T V __attribute__((ext_vector_type(4)));
         typedef V VA __attribute__((aligned(sizeof(T))));
         T *to = static_cast<T *>(a.out) + (s.first + token) * a.o_ts + (head * a.group + at - token * a.group) * a.o_hs;
-        *reinterpret_cast<VA *>(to + d) = V{(T)(v.x * r), (T)(v.y * r), (T)(v.z * r), (T)(v.w * r)};
+        *reinterpret_cast<VA *>(to + d) = V{(T)v.x, (T)v.y, (T)v.z, (T)v.w};
     }
 }
 

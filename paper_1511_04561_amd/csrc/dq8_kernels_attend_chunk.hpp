@@ -387,8 +387,8 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const size_t part = (size_t)(blockIdx.x / splits) * splits + split;
     if (a.parts && splits > 1 && split == 0 && threadIdx.x == 0)
         a.records[blockIdx.x / splits] = int4{(int)place.b, (int)(q_tile * a.kv_heads + head), (int)part, (int)splits};
-    const float size = __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop);
     sum += __shfl_xor(sum, 32);
+    const float r = sum == 0.0f ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop) / (sum * a.entry);
     if (!in) return;
     constexpr int W = JT < 4 ? JT : 4;
     if (splits > 1) {
@@ -401,13 +401,12 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
             for (int j = 0; j < JT; j += W) {
                 V v;
 #pragma unroll
-                for (int x = 0; x < W; ++x) v[x] = acc[j + x][i] * size;
+                for (int x = 0; x < W; ++x) v[x] = acc[j + x][i] * r;
                 *reinterpret_cast<V *>(a.parts + at * DP + JT * (8 * (i / 4) + 4 * hh + i % 4) + j) = v;
             }
         return;
     }
     T *to = static_cast<T *>(a.out) + (s.first + row_token) * a.o_ts + row_head * a.o_hs;
-    const float r = sum == 0.0f ? 0.0f : size / (sum * a.entry);
     typedef T V __attribute__((ext_vector_type(W)));
     typedef V VA __attribute__((aligned(sizeof(T))));
 #pragma unroll
