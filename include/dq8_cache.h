@@ -90,8 +90,11 @@ int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_append *a, void
  * of new tokens) gets zeros.  Tokens of q behind the last sequence keep their place in `out` as it was.  Lengths beyond
  * max_pages * page_size count as that, negative ones as 0; tokens on pages outside the cache are not seen; starts outside
  * 0 .. tokens count as the nearer end, and where they descend anywhere nothing is written.  Places of the cache that no query sees may hold anything, NaN included.
- * Products and sums are held in binary32; a code's value, a query and a weight are rounded to binary16 (11 bits, scaled so that
- * none leaves its range) where the matrix instructions take them: one rounding each, as large as that of a binary16 output.
+ * Products and sums are held in binary32; a code's value, a query and a weight times its value's scale are rounded to binary16 (11 bits)
+ * where the matrix instructions take them: one rounding each, as large as that of a binary16 output.  Each query's products of
+ * weight and scale are brought into range by the largest that it sees itself: one that is less than 2^-19 of that is off by at most 2^-30 of it
+ * instead, and nothing that the query does not see counts.  (Where the largest is made of a value scale below 1e-28 or above 1e35, bits are
+ * lost sooner.)
  * Results do not depend on anything but the arguments (workspace size and max_new among them).
  * max_new: the largest number of new tokens of a sequence, as far as the host knows (0: unknown); it chooses between kernels that are
  * right for any number.

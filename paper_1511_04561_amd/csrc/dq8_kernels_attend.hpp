@@ -16,9 +16,14 @@
 // cb[c] * 32 * 1280 (linear: * 256 * 127): the magnitudes above a tenth of the maximum are whole numbers of 1/1280 there, at most 1920,
 // so that binary16's 11 bits hold them exactly; smaller ones are rounded once, and the smallest but zero is above 2^-12, none subnormal.
 // (With entries cb[c] 2^15, all rounded, binary16 outputs were off by 4.9e-4 of their size, 2.1e-4 of it their own rounding.)  A query
-// row is scaled by a power of two to a largest element of 2^14 .. 2^15, value scales by a power of two to below 2^7, which the
-// accumulators follow when a larger scale appears.  m need not be the largest score, only near it: it is moved, and the sums with it,
-// when a score exceeds it by more than kSlack, so that weights are at most 2^8 and their products with value scales 2^15.
+// row is scaled by a power of two to a largest element of 2^14 .. 2^15.
+//
+// m need not be the largest score.  What becomes binary16 is a weight times a value scale, and every row has its own m, which brings the
+// largest of these products that the row has met to 2^kProductTop; it moves, and the sums with it, when one passes 2^kProductLimit.
+// So a product is rounded once to 11 bits, below 2^-22 of the row's largest to a multiple of 2^-32 of that, and what a row does not see,
+// or only others see, changes nothing of it.  (One exponent for all value scales that a wavefront had met, seen or not, took as many
+// instructions, but outputs of rows that saw only scales 2^-30 times as large vanished.)  Value scales so far from one that the
+// weights would leave binary32 have an m of their own: Row.
 //
 // What bounds it: memory, less well used than by a copy.  64 sequences of up to 4096, 8 heads of 128: 292 MB in 60 us (4.9 TB/s) and 5 us of
 // join; two of up to 131072: 391 MB in 74 us (5.3 TB/s) and 7 us; loads alone in the same order reach 6.7.  A wavefront holds two tiles, one
@@ -39,10 +44,10 @@ constexpr int kTile = 32;          // tokens that a wavefront takes at a time
 constexpr int kAttendWaves = 8;    // of a workgroup: they share one table
 constexpr int kAttendWg = kAttendWaves * kWave;
 constexpr int kQueryTop = 14;      // a query row's largest element is in [2^14, 2^15) in binary16
-constexpr float kSlack = 8.0f;     // how far a score may be above the reference of its row's weights (in powers of two)
-constexpr int kWeightTop = 6;      // a value scale is below 2^7 where it multiplies a weight, the product below 2^15
-constexpr int kLeastExp = -90;     // of scales and queries that are still brought to those ranges
-constexpr float kNothing = -FLT_MAX;  // the largest score before anything was seen
+constexpr float kProductTop = 8.0f, kProductLimit = 15.0f;  // powers of two: of a row's largest weight times value scale, and of any
+constexpr float kApart = 60.0f, kWeightLimit = 68.0f;        // of a row's largest weight, from one, and of any
+constexpr float kDeep = 56.0f;     // how far products are lifted beyond that (a weight times that is below 2^124)
+constexpr int kLeastExp = -90;     // of queries that are still brought to that range
 
 struct AttendArgs {
     const void *q;
@@ -58,7 +63,7 @@ struct AttendArgs {
     // workspace (null: no job is split)
     uint32_t *n_records;
     int4 *records;  // of a job: sequence, number in it, the part it begins with, parts (0: it has none, one wavefront did all of it)
-    float2 *sums;   // per part: largest score and sum of weights of each query row
+    float2 *sums;   // per part and query row: sum_of_part
     float *parts;   // per part: its output [rows][DP], in binary32 as large as the values themselves (their weighted sum may not fit)
     uint32_t rows;  // query rows of a part: as many as a job has at most
     uint32_t in_a_row;  // whether a job's parts lie one after the other, from the number in its record on
@@ -248,6 +253,42 @@ __device__ __forceinline__ int exponent(float v)
     return e < kLeastExp ? kLeastExp : e > 127 ? 127 : e;
 }
 
+// A query row's references: weights are exp2(score - shift), their products with value scales are taken as exp2(score - product) times
+// the scale.  The two are the same number unless scales lie beyond 2^-kApart .. 2^kApart.
+struct Row {
+    float shift, product, sum;  // sum: of the weights
+
+    __device__ __forceinline__ void clear()
+    {
+        shift = product = -FLT_MAX;
+        sum = 0.0f;
+    }
+
+    // high: the largest score of what comes next, large: the log2 of its largest product of exp2(score) and scale (-infinity: none).
+    // Returns the factor of the products that were added up.
+    __device__ __forceinline__ float raise(float high, float large)
+    {
+        float p = fmaxf(product, large - kProductTop);
+        const float s = fmaxf(fmaxf(shift, fminf(p, high + kApart)), high - kApart);
+        p = fmaxf(p, s - kDeep);
+        const float less = __builtin_amdgcn_exp2f(product - p);
+        sum *= __builtin_amdgcn_exp2f(shift - s);
+        shift = s;
+        product = p;
+        return less;
+    }
+
+    __device__ __forceinline__ float rest() const { return __builtin_amdgcn_exp2f(shift - product); }
+};
+
+// A part's sum of weights as a number near one and the log2 of what it is to be multiplied with: references of parts may lie further
+// apart than binary32 reaches.
+__device__ __forceinline__ float2 sum_of_part(float shift, float sum)
+{
+    const int e = __builtin_amdgcn_frexp_expf(sum);
+    return float2{shift + (float)e, __builtin_amdgcn_ldexpf(sum, -e)};
+}
+
 template <int N>
 struct Bytes;
 template <>
@@ -372,7 +413,9 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
     // The query rows as operands of the products, in registers or, where these are needed for the sums, in LDS: the lane's eight elements of
     // step k of group nt.
     v8h q[kQueryInLds<DP, NT> ? 1 : NT][KS];
-    float scale[NT], top[NT], sum[NT];  // top: the reference: weights are exp2(score - top)
+    float scale[NT];
+    Row ref[NT];
+    bool far = false;  // whether some row's two references differ
     int32_t pos[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -407,22 +450,17 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
         }
         pos[nt] = in ? s.len - (int32_t)s.n + (int32_t)token : -1;
         scale[nt] = __builtin_amdgcn_ldexpf(a.factor, e - kQueryTop);
-        top[nt] = kNothing;
-        sum[nt] = 0.0f;
+        ref[nt].clear();
     }
     v4 acc[NT][CPL];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < CPL; ++j) acc[nt][j] = v4{0, 0, 0, 0};
-    // Weights times value scales have to fit binary16: the scales are multiplied by shrink = 2^(kWeightTop - vexp), where
-    // limit = 2^(vexp + 1) is above the largest so far.
-    int vexp = kLeastExp;
-    float shrink = __builtin_amdgcn_ldexpf(1.0f, kWeightTop - vexp), limit = __builtin_amdgcn_ldexpf(1.0f, vexp + 1);
     const int32_t p_first = s.len - (int32_t)s.n;  // position of the sequence's first query, the least of any row here
 
     auto work = [&](uint32_t tile, const TileData<DP> &d) {
-        v4 st[NT][2], vs[2] = {d.vs[0], d.vs[1]};
+        v4 st[NT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -438,43 +476,17 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
         const int32_t t = (int32_t)(tile * kTile);
         // whether some row does not see some token of the tile (a window's lower end: rows up to the last position)
         const bool masked = t + kTile - 1 > p_first || (a.window > 0 && t <= s.len - 1 - a.window) || !d.valid[0] || !d.valid[1];
-        if (masked) {  // scales of tokens that nobody sees do not count
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (t + 16 * h + 4 * (int32_t)g + r >= s.len || !d.valid[h]) vs[h][r] = 0.0f;
-        }
-        float large = 0.0f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) large = fmaxf(large, vs[h][r]);
-        if (__builtin_amdgcn_ballot_w64(large >= limit) != 0) {
-            const int e = (int)uniform((uint32_t)exponent(max_over_groups(large)));
-            if (e > vexp) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < CPL; ++j) acc[nt][j] *= __builtin_amdgcn_ldexpf(1.0f, vexp - e);
-                vexp = e;
-                shrink = __builtin_amdgcn_ldexpf(1.0f, kWeightTop - vexp);
-                limit = __builtin_amdgcn_ldexpf(1.0f, vexp + 1);
-            }
-        }
-        vs[0] *= shrink;
-        vs[1] *= shrink;
         v8h p[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float x[2][4], c[2][4], y[2][4], w[2][4];  // scores x c, value scales, weights
+            float x[2][4], c[2][4], y[2][4], w[2][4], z[2][4];  // scores x c, value scales, weights, products
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     x[h][r] = st[nt][h][r];
                     c[h][r] = d.ks[h][r] * scale[nt];
-                    y[h][r] = vs[h][r];
+                    y[h][r] = d.vs[h][r];
                 }
             if (masked) {  // hidden tokens: weight zero, whatever their scales are
 #pragma unroll
@@ -489,37 +501,53 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
                         }
                     }
             }
-            auto weigh = [&]() {
-                float high = 0.0f;
+            Row &row = ref[nt];
+            float added;
+            auto weigh = [&]() {  // whether one leaves its range
+                float large = 0.0f;
+                added = 0.0f;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        w[h][r] = __builtin_amdgcn_exp2f(x[h][r] * c[h][r] - top[nt]);
-                        high = fmaxf(high, w[h][r]);
+                        w[h][r] = __builtin_amdgcn_exp2f(x[h][r] * c[h][r] - row.shift);
+                        z[h][r] = w[h][r] * y[h][r];
+                        added += w[h][r];
                     }
-                return high;
-            };
-            if (__builtin_amdgcn_ballot_w64(weigh() > (float)(1 << (int)kSlack)) != 0) {
-                float high = kNothing;
+                if (far) {
+                    const float rest = row.rest();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) z[h][r] = w[h][r] * rest * y[h][r];
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) high = fmaxf(high, x[h][r] * c[h][r]);
-                const float now = fmaxf(top[nt], max_over_groups(high)), less = __builtin_amdgcn_exp2f(top[nt] - now);
-                top[nt] = now;
-                sum[nt] *= less;
+                    for (int r = 0; r < 4; ++r) large = fmaxf(large, fabsf(z[h][r]));
+                return added > 0x1p68f || large > 0x1p15f;
+            };
+            if (__builtin_amdgcn_ballot_w64(weigh()) != 0) {
+                float high = -FLT_MAX, large = -__builtin_inff();
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float t = x[h][r] * c[h][r];
+                        high = fmaxf(high, t);
+                        large = fmaxf(large, t + __builtin_amdgcn_logf(fabsf(y[h][r])));
+                    }
+                const float less = row.raise(max_over_groups(high), max_over_groups(large));
 #pragma unroll
                 for (int j = 0; j < CPL; ++j) acc[nt][j] *= less;
+                far = far || __builtin_amdgcn_ballot_w64(row.shift != row.product) != 0;
                 weigh();
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    sum[nt] += w[h][r];
-                    p[nt][4 * h + r] = (_Float16)(w[h][r] * y[h][r]);
-                }
+                for (int r = 0; r < 4; ++r) p[nt][4 * h + r] = (_Float16)z[h][r];
+            row.sum += added;
         }
 #pragma unroll
         for (int j4 = 0; j4 < CPL / 4; ++j4) {
@@ -564,19 +592,19 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
     // A lane has elements 16 x (4 g + i) / 16 .. of its row: CPL neighbours for each i.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        sum[nt] = sum_over_groups(sum[nt]);
+        const float sum = sum_over_groups(ref[nt].sum);
         const uint32_t local = nt * 16 + n, row = q_tile * NT * 16 + local;
-        const float r = sum[nt] == 0.0f ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop) / (sum[nt] * a.entry);
+        const float r = sum == 0.0f ? 0.0f : 1.0f / (sum * a.entry), down = __builtin_amdgcn_exp2f(ref[nt].product - ref[nt].shift);
         if (row >= s.n * a.group) continue;
         if (part >= 0) {
             const size_t at = (size_t)part * a.rows + local;
-            if (g == 0) a.sums[at] = float2{top[nt], sum[nt]};
+            if (g == 0) a.sums[at] = sum_of_part(ref[nt].shift, sum);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < CPL; j += 4)
                     *reinterpret_cast<v4 *>(a.parts + at * DP + CPL * (4 * g + i) + j) =
-                        v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * r;
+                        v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * r * down;
         } else {
             const uint32_t token = row / a.group;
             T *to = static_cast<T *>(a.out) + (s.first + token) * a.o_ts + (head * a.group + row - token * a.group) * a.o_hs;
@@ -587,7 +615,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
 #pragma unroll
                 for (int j = 0; j < CPL; j += 4) {
                     const uint32_t d = CPL * (4 * g + i) + j;
-                    const v4 m = v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * r;
+                    const v4 m = v4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * r * down;
                     if (d < a.dim) *reinterpret_cast<VA *>(to + d) = V{(T)m.x, (T)m.y, (T)m.z, (T)m.w};
                 }
         }
@@ -673,7 +701,7 @@ __global__ __launch_bounds__(WG) void k_cache_join(AttendArgs a)
     }
     if (threadIdx.x < SLICE * kWave) {  // a wavefront looks at a row's parts
         const uint32_t row = first + (threadIdx.x >> 6);
-        float top = kNothing, l = 0.0f;
+        float top = -FLT_MAX, l = 0.0f;
         if (row < rows)
             for (uint32_t i = threadIdx.x & 63; i < parts; i += kWave) {
                 const float2 o = a.sums[part_of(i) * a.rows + row];

@@ -6,7 +6,9 @@
 // in which the lanes of a matrix instruction take it (16 bytes per lane, so that neither side has bank conflicts), one tile ahead of
 // the one that is multiplied.  Products are 32x32x16: S^T = K Q^T with a query per column, lane % 32, sixteen tokens in a lane's
 // registers; these are P^T as operand of out^T = V^T P^T, where the order of a lane's eight tokens is that of its registers.
-// The scales of a tile's tokens go through LDS as factors of scores and weights, brought into range by one wavefront.
+// The scales of a tile's tokens go through LDS as factors of scores and weights.  Whether a row's products of weights and value scales stay
+// in range is asked of its largest weight and the tile's largest scale; where they may not, its reference is moved by these two too, which
+// say too much by 2^kEven at most, or else by all of its products.
 //
 // What bounds it (2048 new tokens after 8192, 32 heads on 8 of 128: 309 GFLOP in 440 us, 0.70 PFLOP/s; a large matrix product of the library
 // reaches 1.20): the matrix units are busy for 29 % of the time, the vector unit 43 %, LDS 49 %, and wavefronts wait for half of
@@ -74,13 +76,18 @@ struct ChunkShape {
     static_assert(kTokens <= kWave, "a lane for every token's scales");
 };
 
-// One tile's scales in LDS: factors of scores and of weights, which tokens are there and the exponent that the latter were brought to.
+constexpr int kEven = 3;
+constexpr float kStaged = 14.0f;  // value scales are staged times 2^-kStaged: weights stay normal numbers beside scales near 2^128, down to 2^-22 of the largest
+
+// One tile's scales in LDS: factors of scores and of weights, which tokens are there, the log2 of the largest of the latter
+// and whether some are less than 2^-kEven of it.
 // A token whose value scale is not finite has weight factor 0 and a score that is NaN.
 template <int TOKENS>
 struct ChunkScales {
     float key[TOKENS], value[TOKENS];
     uint64_t there;
-    int32_t exponent, pad;
+    float most;
+    uint32_t uneven;
 };
 
 template <int DP, int TH, typename T>
@@ -120,7 +127,11 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const bool in = row < total_rows;
     const uint32_t row_token = in ? row / a.group : 0, row_head = head * a.group + (in ? row - row_token * a.group : 0);
     const int32_t pos = in ? p0 + (int32_t)row_token : -1;
-    float up, top = kNothing, sum = 0.0f;  // up: the power of two that a row's scores are multiplied by; top: the reference of its weights
+    float up;  // the power of two that a row's scores are multiplied by
+    Row ref;
+    ref.clear();
+    float sum = 0.0f;  // of the weights exp2(score - ref.product)
+    bool far = false;  // whether some row's two references differ, now or before: the sum is then ref.sum
     {
         const T *src = static_cast<const T *>(a.q) + (s.first + row_token) * a.q_ts + row_head * a.q_hs;
         typedef T V __attribute__((ext_vector_type(8)));
@@ -150,7 +161,6 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[j][i] = 0.0f;
-    int vexp = kLeastExp;
     // positions of the wavefront's first and last row (-1: it has none)
     const int32_t p_first = w_first < total_rows ? p0 + (int32_t)(w_first / a.group) : -1;
     const int32_t p_last = w_first < total_rows ? p0 + (int32_t)((w_first + 31 < total_rows ? w_first + 31 : total_rows - 1) / a.group) : -1;
@@ -178,7 +188,6 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     uint32_t vc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     float ks = 0.0f, vs = 0.0f;
     bool s_there = false;
-    int32_t staged = kLeastExp;  // (wavefront 0) exponent of the largest value scale so far
     auto inside = [&](uint32_t page) { return page < a.n_pages ? page : 0; };
     // the loads of a tile; tiles in order
     auto fetch = [&](uint32_t tile) {
@@ -234,21 +243,21 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     auto put_scales = [&](uint32_t buffer3) {
         if (wave != 0) return;
         const bool finite = fabsf(vs) <= FLT_MAX;  // (if not, the score becomes NaN for whoever sees it)
-        const float y = s_there && finite ? vs : 0.0f;
-        float most = y;
+        const float y = s_there && finite ? vs * 0x1p-14f : 0.0f;
+        float most = fabsf(y);
 #pragma unroll
         for (int m = 1; m < TOKENS; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
-        const int e = (int)uniform((uint32_t)exponent(fmaxf(most, 0.0f)));
-        staged = e > staged ? e : staged;
         ChunkScales<TOKENS> &sc = scales[buffer3];
         if (lane < TOKENS) {
             sc.key[lane] = finite ? ks * factor : __builtin_nanf("");
-            sc.value[lane] = y * __builtin_amdgcn_ldexpf(1.0f, kWeightTop - staged);
+            sc.value[lane] = y;
         }
         const uint64_t all = __builtin_amdgcn_ballot_w64(s_there);
+        const uint64_t low = __builtin_amdgcn_ballot_w64(s_there && fabsf(y) * (float)(1 << kEven) < most);
         if (lane == 0) {
             sc.there = all;
-            sc.exponent = staged;
+            sc.most = __builtin_amdgcn_logf(most);
+            sc.uneven = low != 0;
         }
     };
 
@@ -269,13 +278,8 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
         const v8h *const values = reinterpret_cast<const v8h *>(value_tiles + buffer3 * S::kValueBytes) + lane;
         const ChunkScales<TOKENS> &sc = scales[buffer3];
         const int32_t t = (int32_t)(tile * TOKENS);
-        const int e = sc.exponent;
-        if (e > vexp) {
-            const float less = __builtin_amdgcn_ldexpf(1.0f, vexp - e);
-#pragma unroll
-            for (int j = 0; j < JT; ++j) acc[j] *= less;
-            vexp = e;
-        }
+        const uint64_t there = sc.there;  // (32 tokens: both halves of the wavefront say the same)
+        const float most = sc.most;
         // scores times their keys' scales; those that a row does not see become -infinity
 #pragma unroll
         for (int h = 0; h < TH; ++h)
@@ -285,7 +289,6 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
 #pragma unroll
                 for (int i = 0; i < 4; ++i) st[h][4 * i4 + i] *= f[i];
             }
-        const uint64_t there = sc.there;  // (32 tokens: both halves of the wavefront say the same)
         const bool masked = t + TOKENS - 1 > p_first || (a.window > 0 && t <= p_last - a.window) || there != ~0ull;
         if (masked) {
 #pragma unroll
@@ -302,18 +305,37 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
                     for (int i = 0; i < 16; ++i)
                         if (!(there >> (32 * h + 8 * (i / 4) + 4 * hh + i % 4) & 1)) st[h][i] = -__builtin_inff();
         }
-        float high = kNothing;
+        float high = -FLT_MAX;
 #pragma unroll
         for (int h = 0; h < TH; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i) high = fmaxf(high, st[h][i]);
-        // `top` need not be the largest score, only near it: weights up to 2^kSlack fit
-        if (__builtin_amdgcn_ballot_w64(high * up > top + kSlack) != 0) {
-            const float now = fmaxf(top, fmaxf(high, __shfl_xor(high, 32)) * up), less = __builtin_amdgcn_exp2f(top - now);
-            top = now;
-            sum *= less;
+        const bool over = high * up > ref.product + kWeightLimit || high * up + most > ref.product + kProductLimit;
+        if (far || __builtin_amdgcn_ballot_w64(over) != 0) {
+            float large = high * up + most;
+            if (sc.uneven) {
+                large = -__builtin_inff();
+#pragma unroll
+                for (int h = 0; h < TH; ++h)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const v4 f = *reinterpret_cast<const v4 *>(sc.value + 32 * h + 8 * i4 + 4 * hh);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) large = fmaxf(large, st[h][4 * i4 + i] * up + __builtin_amdgcn_logf(fabsf(f[i])));
+                    }
+            }
+            if (!far) ref.shift = ref.product, ref.sum = sum;
+            const float less = ref.raise(fmaxf(high, __shfl_xor(high, 32)) * up, fmaxf(large, __shfl_xor(large, 32)));
 #pragma unroll
             for (int j = 0; j < JT; ++j) acc[j] *= less;
+            far = far || __builtin_amdgcn_ballot_w64(ref.shift != ref.product) != 0;
+            if (far) {
+#pragma unroll
+                for (int h = 0; h < TH; ++h)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) ref.sum += __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][i], up, -ref.shift));
+            }
+            sum = ref.sum;
         }
         v8h p[US];
 #pragma unroll
@@ -323,8 +345,8 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
                 const v4 f = *reinterpret_cast<const v4 *>(sc.value + 32 * h + 8 * i4 + 4 * hh);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    // (up is a power of two: the product is exact, and what is subtracted from it is such a product)
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][4 * i4 + i], up, -top));
+                    // (up is a power of two: the product is exact)
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][4 * i4 + i], up, -ref.product));
                     sum += w;
                     p[2 * h + i4 / 2][4 * (i4 % 2) + i] = (_Float16)(w * f[i]);
                 }
@@ -387,13 +409,17 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const size_t part = (size_t)(blockIdx.x / splits) * splits + split;
     if (a.parts && splits > 1 && split == 0 && threadIdx.x == 0)
         a.records[blockIdx.x / splits] = int4{(int)place.b, (int)(q_tile * a.kv_heads + head), (int)part, (int)splits};
+    if (far)
+        sum = ref.sum;
+    else
+        ref.shift = ref.product;
     sum += __shfl_xor(sum, 32);
-    const float r = sum == 0.0f ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, vexp - kWeightTop) / (sum * a.entry);
+    const float r = sum == 0.0f ? 0.0f : 1.0f / (sum * a.entry), down = __builtin_amdgcn_exp2f(ref.product - ref.shift + kStaged);
     if (!in) return;
     constexpr int W = JT < 4 ? JT : 4;
     if (splits > 1) {
         const size_t at = part * a.rows + wave * 32 + n;
-        if (hh == 0) a.sums[at] = float2{top, sum};
+        if (hh == 0) a.sums[at] = sum_of_part(ref.shift, sum);
         typedef float V __attribute__((ext_vector_type(W)));
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -401,7 +427,7 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
             for (int j = 0; j < JT; j += W) {
                 V v;
 #pragma unroll
-                for (int x = 0; x < W; ++x) v[x] = acc[j + x][i] * r;
+                for (int x = 0; x < W; ++x) v[x] = acc[j + x][i] * r * down;
                 *reinterpret_cast<V *>(a.parts + at * DP + JT * (8 * (i / 4) + 4 * hh + i % 4) + j) = v;
             }
         return;
@@ -416,7 +442,7 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
             const uint32_t d = JT * (8 * (i / 4) + 4 * hh + i % 4) + j;
             V v;
 #pragma unroll
-            for (int x = 0; x < W; ++x) v[x] = (T)(acc[j + x][i] * r);
+            for (int x = 0; x < W; ++x) v[x] = (T)(acc[j + x][i] * r * down);
             if (d < a.dim) *reinterpret_cast<VA *>(to + d) = v;
         }
 }

@@ -1,4 +1,4 @@
-"""GPU: attention over the cache at the ends of the range of values.
+"""GPU: attention over the cache where the scales of values lie far apart, and what a query does not see.
 
 The reference is that of the other cache tests, in 64 bits; its tolerance for weights below the normal range of binary16 goes by the
 largest value that a query sees.  Here that term is the smaller one that include/dq8_cache.h states: a weight times its value's scale is off by
@@ -64,3 +64,104 @@ def test_values_near_the_end_of_binary32(dq8, n, cached, size):
         cache, q, pages, lens, starts = attention_inputs(dq8, case)
         cache[1][1] *= np.float32(size)
         check_both_kernels(dq8, 0, cache, q, pages, lens, starts)
+
+
+#: (type, heads, kv_heads, dim, page, new tokens, cached): the largest max_new is more than 128 rows of a cached head
+SHAPES = [("f16", 8, 2, 64, 16, 40, 140), ("bf16", 4, 1, 128, 32, 40, 1300), ("bf16", 2, 1, 256, 16, 70, 300), ("f16", 5, 1, 80, 16, 33, 33)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%s_d%d" % (s[0], s[3]))
+@pytest.mark.parametrize("power", [20, 24, 28, 31, 60, 110])
+def test_values_of_later_tokens_do_not_count(dq8, shape, power):
+    """The new tokens' values grow from scales near one to scales near 2^power: an earlier query sees none of the large ones."""
+    type_, heads, kv, dim, page, n, cached = shape
+    case = (0, "bf16" if power > 16 else type_, heads, kv, dim, page, [(n, cached)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    j = np.arange(cached - n, cached)
+    cache[1][1, pages[0, j // page], :, j % page] *= 2.0 ** np.linspace(0, power, n)[:, None].astype(np.float32)
+    check_both_kernels(dq8, 0, cache, q, pages, lens, starts)
+
+
+@pytest.mark.parametrize("power", [24, 60, 120])
+def test_one_large_value_at_the_end(dq8, power):
+    """Two new tokens, the second one's value larger by 2^power: the first query's output is that of a cache without it."""
+    for n in (2, 140):
+        case = (0, "bf16", 2, 2, 64, 16, [(n, n + 30)], 0)
+        cache, q, pages, lens, starts = attention_inputs(dq8, case)
+        last = n + 29
+        cache[1][1, pages[0, last // 16], :, last % 16] = 2.0 ** power
+        check_both_kernels(dq8, 0, cache, q, pages, lens, starts)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%s_d%d" % (s[0], s[3]))
+@pytest.mark.parametrize("garbage", [1e30, 3.4e38, float("inf"), float("nan")])
+def test_what_lies_below_a_window_may_be_anything(dq8, shape, garbage):
+    """A window whose lower end lies inside a tile: scales of keys and values before it, in the same tile too."""
+    type_, heads, kv, dim, page, n, cached = shape
+    window = 21
+    case = (2, type_, heads, kv, dim, page, [(n, cached)], window)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    j = np.arange(max(cached - n - window + 1, 0))
+    cache[1][:, pages[0, j // page], :, j % page] = garbage
+    check_both_kernels(dq8, 2, cache, q, pages, lens, starts, window)
+
+
+@pytest.mark.parametrize("n", [2, 140])
+@pytest.mark.parametrize("place", [0, 45, 99])
+def test_a_large_value_with_hardly_any_weight(dq8, n, place):
+    """A token that every query sees with a weight of about e^-28, its value larger by 2^30: both ends of the sum count."""
+    kind, dim, page = 0, 64, 16
+    case = (kind, "bf16", 2, 1, dim, page, [(n, n + 100)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    cb = oracle.codebook(kind)
+    j = np.arange(n + 100)
+    q = torch.full_like(q, 1.0)
+    cache[0][0, pages[0, j // page], 0, j % page] = int(np.argmax(cb))  # every key the row's maximum
+    cache[1][0, pages[0, j // page], 0, j % page] = 0.25 + 0.01 * (j % 7)
+    at = pages[0, place // page], 0, place % page
+    cache[0][(0,) + at] = int(np.argmin(cb))  # and this one its opposite
+    cache[1][(0,) + at] = 3.25
+    cache[1][(1,) + at] = 2.0 ** 30
+    check_both_kernels(dq8, kind, cache, q, pages, lens, starts)
+
+
+@pytest.mark.parametrize("shape", SHAPES[:3], ids=lambda s: "%s_d%d" % (s[0], s[3]))
+@pytest.mark.parametrize("low,high", [(-36, 36), (-36, -30), (30, 38), (-4, 4)])
+def test_scales_of_any_size_in_any_order(dq8, shape, low, high):
+    _, heads, kv, dim, page, n, cached = shape
+    case = (3, "bf16", heads, kv, dim, page, [(n, cached)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    rng = np.random.default_rng(dim + low)
+    there = np.isfinite(cache[1][1])
+    cache[1][1][there] = np.minimum(10.0 ** rng.uniform(low, high, there.sum()), 3e38).astype(np.float32)
+    check_both_kernels(dq8, 3, cache, q, pages, lens, starts)
+
+
+@pytest.mark.parametrize("n", [2, 140])
+def test_values_of_zeros_under_the_largest_weights(dq8, n):
+    """Rows of zeros have the scale zero.  Under most of the weight they leave the others' sum small, not empty."""
+    kind, dim, page = 1, 128, 16
+    case = (kind, "bf16", 1, 1, dim, page, [(n, n + 75)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    j = np.arange(n + 75)
+    q = torch.full_like(q, 0.5)
+    cache[0][0, pages[0, j // page], 0, j % page] = np.where(j % 3 == 0, 127, 255)[:, None]  # the row's maximum, or its opposite
+    cache[1][0, pages[0, j // page], 0, j % page] = np.where(j % 3 == 0, 3.0, 2.0)
+    cache[1][1, pages[0, j[::3] // page], 0, j[::3] % page] = 0.0
+    check_both_kernels(dq8, kind, cache, q, pages, lens, starts)
+
+
+@pytest.mark.parametrize("n", [2, 140])
+def test_a_value_that_stands_for_nan_reaches_its_viewers_only(dq8, n):
+    kind, dim, page = 0, 64, 16
+    case = (kind, "bf16", 2, 1, dim, page, [(n, n + 60)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    want, tol = attention_by_weight(kind, cache, host(q), pages, lens, starts, dim ** -0.5)
+    bad = n + 60 - n // 2 - 1  # a new token in the middle
+    cache[1][1, pages[0, bad // page], 0, bad % page] = np.nan
+    cuda = lambda a: torch.from_numpy(a).cuda()
+    for max_new in (1, n):
+        got = dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(starts), max_new=max_new)
+        first = bad - 60
+        assert torch.isnan(got[first:]).all()
+        check_attention(got[:first], q[:first], want[:first], tol[:first])
