@@ -431,6 +431,14 @@ def cache_buffers(pages, kv_heads, page_size, dim, device="cuda"):
     return torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(shape[:-1], dtype=torch.float32, device=device)
 
 
+def _int32(v, what):
+    """v as an int that a field of 32 bits holds (ctypes takes any other modulo 2^32)."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("%s does not fit 32 bits: %d" % (what, v))
+    return v
+
+
 def _cache(codes, scales):
     _dev(codes, torch.uint8, "codes")
     _dev(scales, torch.float32, "scales")
@@ -438,7 +446,7 @@ def _cache(codes, scales):
         raise ValueError("codes must be [2, pages, kv_heads, page_size, dim] and scales the same without the last axis")
     if scales.device != codes.device:
         raise ValueError("codes and scales are on different devices")
-    return _Cache(codes.data_ptr(), scales.data_ptr(), codes.shape[1], codes.shape[2], codes.shape[3], codes.shape[4])
+    return _Cache(codes.data_ptr(), scales.data_ptr(), codes.shape[1], *(_int32(n, "an axis of codes") for n in codes.shape[2:]))
 
 
 def _on(device, t, dtype, shape, what):
@@ -491,7 +499,7 @@ def cache_append(kind, k, v, slots, codes, scales, positions=None, rotation=None
     a.slots = _on(dev, slots, torch.int64, (tokens,), "slots")
     if q is not None:
         a.q, a.q_token_stride, a.q_head_stride = _rows(q, "q", dev, k.dtype, tokens, None, dim)
-        a.heads = q.shape[1]
+        a.heads = _int32(q.shape[1], "the number of query heads")
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
         a.q_out, a.q_out_token_stride, a.q_out_head_stride = _rows(q_out, "q_out", dev, k.dtype, tokens, a.heads, dim)
@@ -504,7 +512,7 @@ def cache_append(kind, k, v, slots, codes, scales, positions=None, rotation=None
             raise ValueError("rotation needs positions")
         a.rotation = _on(dev, rotation, torch.float32, rotation.shape, "rotation")
         a.positions = _on(dev, positions, torch.int64, (tokens,), "positions")
-        a.n_positions, a.half, a.interleaved = rotation.shape[0], rotation.shape[2], bool(interleaved)
+        a.n_positions, a.half, a.interleaved = rotation.shape[0], _int32(rotation.shape[2], "an axis of rotation"), bool(interleaved)
     elif positions is not None:
         raise ValueError("positions need a rotation")
     if q_weight is not None:
@@ -512,7 +520,7 @@ def cache_append(kind, k, v, slots, codes, scales, positions=None, rotation=None
     if k_weight is not None:
         a.k_weight = _on(dev, k_weight, torch.float32, (dim,), "k_weight")
     a.eps = float(eps)
-    _enqueue(lib().dq8_cache_append, codes.get_device(), int(kind), ctypes.byref(c), ctypes.byref(a))
+    _enqueue(lib().dq8_cache_append, codes.get_device(), _int32(kind, "kind"), ctypes.byref(c), ctypes.byref(a))
     return q_out
 
 
@@ -524,7 +532,7 @@ def _attention(q, codes, scales, pages, lens, starts, max_new, softmax_scale, wi
     a = _Attention()
     a.type = _TYPES[q.dtype]
     a.q, a.q_token_stride, a.q_head_stride = _rows(q, "q", dev, q.dtype, None, None, dim)
-    a.tokens, a.heads = q.shape[0], q.shape[1]
+    a.tokens, a.heads = q.shape[0], _int32(q.shape[1], "the number of query heads")
     if not isinstance(pages, torch.Tensor) or pages.dim() != 2:
         raise ValueError("pages must be [sequences, pages of the longest]")
     a.batch, a.max_pages = pages.shape
@@ -532,10 +540,11 @@ def _attention(q, codes, scales, pages, lens, starts, max_new, softmax_scale, wi
     a.lens = _on(dev, lens, torch.int32, (a.batch,), "lens")
     if starts is not None:
         a.starts = _on(dev, starts, torch.int32, (a.batch + 1,), "starts")
-    a.max_new = 0 if max_new is None else int(max_new)
-    if int(window) >= 2 ** 31:
-        raise ValueError("window must be below 2^31")
-    a.window = int(window)
+    if max_new is not None:
+        if not 0 <= int(max_new) < 2 ** 63:
+            raise ValueError("max_new must be a number of tokens, got %d" % int(max_new))
+        a.max_new = int(max_new)
+    a.window = _int32(window, "window")
     a.softmax_scale = dim ** -0.5 if softmax_scale is None else float(softmax_scale)
     if out is not None:
         a.out, a.out_token_stride, a.out_head_stride = _rows(out, "out", dev, q.dtype, a.tokens, a.heads, dim)
@@ -574,7 +583,7 @@ def cache_attention(kind, q, codes, scales, pages, lens, starts=None, max_new=No
         _dev(workspace, torch.uint8, "workspace")
         if workspace.device != codes.device:
             raise ValueError("workspace is on another device than the cache")
-    _enqueue(lib().dq8_cache_attention, codes.get_device(), int(kind), ctypes.byref(c), ctypes.byref(a),
+    _enqueue(lib().dq8_cache_attention, codes.get_device(), _int32(kind, "kind"), ctypes.byref(c), ctypes.byref(a),
              workspace.data_ptr() if workspace is not None and workspace.numel() else None, 0 if workspace is None else workspace.numel())
     return out
 
