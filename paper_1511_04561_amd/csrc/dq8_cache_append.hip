@@ -316,9 +316,11 @@ extern "C" int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_appe
     if (a.rotation && (a.half < 1 || 2 * a.half > cache->dim || a.n_positions < 1 || a.n_positions >= dq8::kCacheLimit))
         return failed(DQ8_ERR_ARG, "%s: a rotation of %d pairs in heads of %d elements at %zu positions", who, a.half, cache->dim, a.n_positions);
     if ((a.q_weight || a.k_weight) && !(a.eps >= 0.0 && a.eps <= 1e30)) return failed(DQ8_ERR_ARG, "%s: eps must be finite and not negative", who);
-    for (size_t s : {a.q_token_stride, a.q_head_stride, a.k_token_stride, a.k_head_stride, a.v_token_stride, a.v_head_stride,
-                     a.q_out_token_stride, a.q_out_head_stride})
-        if (!sane(s)) return failed(DQ8_ERR_ARG, "%s: a stride is too large", who);
+    const size_t kv_heads = (size_t)cache->kv_heads, heads = (size_t)a.heads;
+    for (size_t s : {a.q_token_stride, a.k_token_stride, a.v_token_stride, a.q_out_token_stride})
+        if (!sane(s, a.tokens)) return failed(DQ8_ERR_ARG, "%s: a stride is too large", who);
+    if (!sane(a.q_head_stride, heads) || !sane(a.q_out_head_stride, heads) || !sane(a.k_head_stride, kv_heads) || !sane(a.v_head_stride, kv_heads))
+        return failed(DQ8_ERR_ARG, "%s: a stride is too large", who);
     const size_t size = a.type == DQ8_FLOAT32 ? 4 : 2;
     if ((((uintptr_t)a.k | (uintptr_t)a.v | (a.heads ? (uintptr_t)a.q | (uintptr_t)a.q_out : 0)) & (size - 1)) != 0 ||
         (((uintptr_t)a.rotation | (uintptr_t)a.q_weight | (uintptr_t)a.k_weight) & 3) != 0 || (((uintptr_t)a.slots | (uintptr_t)a.positions) & 7) != 0)
@@ -371,7 +373,7 @@ extern "C" int dq8_cache_append(int kind, const dq8_cache *cache, const dq8_appe
     const int lpr = dim <= 64 ? 8 : dim <= 128 ? 16 : 32;
     // Items of four times the heads that a wavefront has at once where there are many, of one time where every wavefront counts (32 + 8 + 8 heads
     // of 128 in 16 bits, us with one | four: 64 tokens 4.5 | 5.6, 256 5.5 | 5.9, 512 7.9 | 6.7, 2048 19 | 13, 8192 59 | 42).
-    const size_t at_once = (size_t)(kWave / lpr), heads = (size_t)a.heads;
+    const size_t at_once = (size_t)(kWave / lpr);
     auto items = [&](size_t steps) { return a.tokens * ((heads + at_once * steps - 1) / (at_once * steps) + 2 * ((kv + at_once * steps - 1) / (at_once * steps))); };
     k.item_steps = items(4) >= (size_t)dev.cus * 8 ? 4 : 1;
     const size_t per = at_once * k.item_steps, most = (size_t)dev.cus * 5;  // that are resident (four: 47 us, five 43, eight 43 at 8192)

@@ -106,8 +106,9 @@ int check_shape(const char *who, int kind, const dq8_cache *cache, const dq8_att
         return failed(DQ8_ERR_ARG, "%s: %zu pages per sequence", who, a.max_pages);
     if (a.window < 0) return failed(DQ8_ERR_ARG, "%s: window %d", who, a.window);
     if (!(a.softmax_scale >= -FLT_MAX && a.softmax_scale <= FLT_MAX)) return failed(DQ8_ERR_ARG, "%s: softmax_scale is not finite", who);
-    for (size_t s : {a.q_token_stride, a.q_head_stride, a.out_token_stride, a.out_head_stride})
-        if (!dq8::sane(s)) return failed(DQ8_ERR_ARG, "%s: a stride is too large", who);
+    if (!dq8::sane(a.q_token_stride, a.tokens) || !dq8::sane(a.out_token_stride, a.tokens) || !dq8::sane(a.q_head_stride, (size_t)a.heads) ||
+        !dq8::sane(a.out_head_stride, (size_t)a.heads))
+        return failed(DQ8_ERR_ARG, "%s: a stride is too large", who);
     return DQ8_OK;
 }
 

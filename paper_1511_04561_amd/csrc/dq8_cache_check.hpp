@@ -36,8 +36,8 @@ inline size_t extent(size_t tokens, size_t token_stride, int heads, size_t head_
     return tokens == 0 || heads == 0 ? 0 : ((tokens - 1) * token_stride + (size_t)(heads - 1) * head_stride + (size_t)dim) * size;
 }
 
-// Strides whose products with tokens and heads stay far inside 64 bits.
-inline bool sane(size_t stride) { return stride < (size_t)1 << 40; }
+// Strides of `count` tokens or heads over less than 2^56 elements, so that extents in bytes stay far inside 64 bits.
+inline bool sane(size_t stride, size_t count) { return stride < (size_t)1 << 40 && (count < 2 || stride < ((size_t)1 << 56) / (count - 1)); }
 
 // Whether no two rows of an array that is written overlap: all heads of a token lie before the next token's, or the other way round.
 inline bool apart(size_t tokens, size_t token_stride, int heads, size_t head_stride, int dim)
