@@ -216,7 +216,7 @@ int dq8_cache_attention(int kind, const dq8_cache *cache, const dq8_attention *i
     k.page_shift = (uint32_t)__builtin_ctz((unsigned)cache->page_size);
     k.window = a.window;
     k.entry = kind == DQ8_LINEAR ? 127.0f * 256.0f : 1280.0f * 32.0f;
-    k.factor = a.softmax_scale * 1.44269504088896340736f / k.entry;
+    k.factor = (float)((double)a.softmax_scale * 1.44269504088896340736 / (double)k.entry);  // (the product alone may leave binary32)
     k.rows = s.rows, k.in_a_row = s.chunk, k.by_wave = !s.chunk && s.records < s.jobs;
     k.n_records = nullptr, k.records = nullptr, k.sums = nullptr, k.parts = nullptr;
     if (s.parts && workspace && workspace_bytes >= workspace_bytes_of(s)) {

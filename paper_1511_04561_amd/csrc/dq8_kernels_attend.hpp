@@ -22,8 +22,8 @@
 // largest of these products that the row has met to 2^kProductTop; it moves, and the sums with it, when one passes 2^kProductLimit.
 // So a product is rounded once to 11 bits, below 2^-22 of the row's largest to a multiple of 2^-32 of that, and what a row does not see,
 // or only others see, changes nothing of it.  (One exponent for all value scales that a wavefront had met, seen or not, took as many
-// instructions, but outputs of rows that saw only scales 2^-30 times as large vanished.)  Value scales so far from one that the
-// weights would leave binary32 have an m of their own: Row.
+// instructions, but outputs of rows that saw only scales 2^-30 times as large vanished.)  Where one number does not do for weights and
+// products, there are two: Row.
 //
 // What bounds it: memory, less well used than by a copy.  64 sequences of up to 4096, 8 heads of 128: 292 MB in 60 us (4.9 TB/s) and 5 us of
 // join; two of up to 131072: 391 MB in 74 us (5.3 TB/s) and 7 us; loads alone in the same order reach 6.7.  A wavefront holds two tiles, one
@@ -253,39 +253,45 @@ __device__ __forceinline__ int exponent(float v)
     return e < kLeastExp ? kLeastExp : e > 127 ? 127 : e;
 }
 
-// A query row's references: weights are exp2(score - shift), their products with value scales are taken as exp2(score - product) times
-// the scale.  The two are the same number unless scales lie beyond 2^-kApart .. 2^kApart.
+// A query row's references: weights are exp2(score - shift), their products with value scales are taken as exp2(score - shift + lift) times
+// the scale.  The lift is zero, and the shift alone brings the products into range, unless scales lie beyond 2^-kApart .. 2^kApart or
+// scores beyond 2^20: a number near these is too coarse for that, so that the shift is then a score itself.
 struct Row {
-    float shift, product, sum;  // sum: of the weights
+    float shift, lift, sum;  // sum: of the weights
 
     __device__ __forceinline__ void clear()
     {
-        shift = product = -FLT_MAX;
-        sum = 0.0f;
+        shift = -FLT_MAX;
+        lift = sum = 0.0f;
     }
 
-    // high: the largest score of what comes next, large: the log2 of its largest product of exp2(score) and scale (-infinity: none).
-    // Returns the factor of the products that were added up.
+    // high: the largest score of what comes next (-infinity: nothing is seen), large: the log2 of its largest product of
+    // exp2(score - high) and scale (-infinity: none).  Returns the factor of the products that were added up.
     __device__ __forceinline__ float raise(float high, float large)
     {
-        float p = fmaxf(product, large - kProductTop);
-        const float s = fmaxf(fmaxf(shift, fminf(p, high + kApart)), high - kApart);
-        p = fmaxf(p, s - kDeep);
-        const float less = __builtin_amdgcn_exp2f(product - p);
-        sum *= __builtin_amdgcn_exp2f(shift - s);
-        shift = s;
-        product = p;
-        return less;
+        if (!(high > -__builtin_inff())) return 1.0f;
+        // relative to high: the shift as it was, the reference of the products as it was and as it is to be
+        const float s0 = shift - high, p0 = s0 - lift, p = fmaxf(p0, large - kProductTop);
+        const bool fine = fabsf(high) < 0x1p20f;
+        const float near = fine ? fmaxf(fminf(p, kApart), -kApart) : 0.0f;
+        if (near <= s0) {  // the shift stays
+            const float was = lift;
+            lift = fminf(lift, s0 + kProductTop - large);
+            return __builtin_amdgcn_exp2f(lift - was);
+        }
+        shift = high + near;
+        const float s = shift - high;  // (rounded as the shift is)
+        lift = fine && near == p ? 0.0f : fminf(s - p, kDeep);
+        sum *= __builtin_amdgcn_exp2f(s0 - s);
+        return __builtin_amdgcn_exp2f(p0 - (s - lift));
     }
-
-    __device__ __forceinline__ float rest() const { return __builtin_amdgcn_exp2f(shift - product); }
 };
 
 // A part's sum of weights as a number near one and the log2 of what it is to be multiplied with: references of parts may lie further
-// apart than binary32 reaches.
+// apart than binary32 reaches.  (Those that are too coarse to be moved are scores: the sum is no less than one.)
 __device__ __forceinline__ float2 sum_of_part(float shift, float sum)
 {
-    const int e = __builtin_amdgcn_frexp_expf(sum);
+    const int e = fabsf(shift) < 0x1p20f ? __builtin_amdgcn_frexp_expf(sum) : 0;
     return float2{shift + (float)e, __builtin_amdgcn_ldexpf(sum, -e)};
 }
 
@@ -415,7 +421,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
     v8h q[kQueryInLds<DP, NT> ? 1 : NT][KS];
     float scale[NT];
     Row ref[NT];
-    bool far = false;  // whether some row's two references differ
+    bool far = false;  // whether some row has a lift
     int32_t pos[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -515,7 +521,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
                         added += w[h][r];
                     }
                 if (far) {
-                    const float rest = row.rest();
+                    const float rest = __builtin_amdgcn_exp2f(row.lift);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -528,19 +534,20 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
                 return added > 0x1p68f || large > 0x1p15f;
             };
             if (__builtin_amdgcn_ballot_w64(weigh()) != 0) {
-                float high = -FLT_MAX, large = -__builtin_inff();
+                float high = -__builtin_inff(), large = -__builtin_inff();
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float t = x[h][r] * c[h][r];
-                        high = fmaxf(high, t);
-                        large = fmaxf(large, t + __builtin_amdgcn_logf(fabsf(y[h][r])));
-                    }
-                const float less = row.raise(max_over_groups(high), max_over_groups(large));
+                    for (int r = 0; r < 4; ++r) high = fmaxf(high, x[h][r] * c[h][r]);
+                high = max_over_groups(high);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) large = fmaxf(large, x[h][r] * c[h][r] - high + __builtin_amdgcn_logf(fabsf(y[h][r])));
+                const float less = row.raise(high, max_over_groups(large));
 #pragma unroll
                 for (int j = 0; j < CPL; ++j) acc[nt][j] *= less;
-                far = far || __builtin_amdgcn_ballot_w64(row.shift != row.product) != 0;
+                far = far || __builtin_amdgcn_ballot_w64(row.lift != 0.0f) != 0;
                 weigh();
             }
 #pragma unroll
@@ -594,7 +601,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, const Seq &s, uint32
     for (int nt = 0; nt < NT; ++nt) {
         const float sum = sum_over_groups(ref[nt].sum);
         const uint32_t local = nt * 16 + n, row = q_tile * NT * 16 + local;
-        const float r = sum == 0.0f ? 0.0f : 1.0f / (sum * a.entry), down = __builtin_amdgcn_exp2f(ref[nt].product - ref[nt].shift);
+        const float r = sum == 0.0f ? 0.0f : 1.0f / (sum * a.entry), down = __builtin_amdgcn_exp2f(-ref[nt].lift);
         if (row >= s.n * a.group) continue;
         if (part >= 0) {
             const size_t at = (size_t)part * a.rows + local;

@@ -77,7 +77,10 @@ struct ChunkShape {
 };
 
 constexpr int kEven = 3;
-constexpr float kStaged = 14.0f;  // value scales are staged times 2^-kStaged: weights stay normal numbers beside scales near 2^128, down to 2^-22 of the largest
+// Scales are staged times powers of two.  Value scales: beside those near 2^128 weights down to 2^-22 of the largest stay normal numbers.
+// Key scales: their products with those of 256 elements of a query and a code (2^39) stay in binary32, whatever the softmax's factor.
+constexpr float kStaged = 14.0f;
+constexpr int kKeyStaged = 40;
 
 // One tile's scales in LDS: factors of scores and of weights, which tokens are there, the log2 of the largest of the latter
 // and whether some are less than 2^-kEven of it.
@@ -98,6 +101,8 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     __shared__ __align__(256) uint32_t lut[256 * kLutCopies];
     __shared__ __align__(16) uint8_t key_tiles[2 * S::kKeyBytes], value_tiles[3 * S::kValueBytes];
     __shared__ __align__(16) ChunkScales<TOKENS> scales[3];
+    __shared__ float ups[kChunkWg];  // a thread's `up` as it is without a lift
+    __shared__ Row lifted[kChunkWg];  // and its row where rows have lifts
     const uint32_t lane = threadIdx.x & 63, wave = wave_in_wg(), n = lane & 31, hh = lane >> 5, lane4 = lane * 4;
     // the last query rows of a sequence see most: they begin first
     const Place place = place_of(a, S::kRows, blockIdx.x / splits);
@@ -127,11 +132,11 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const bool in = row < total_rows;
     const uint32_t row_token = in ? row / a.group : 0, row_head = head * a.group + (in ? row - row_token * a.group : 0);
     const int32_t pos = in ? p0 + (int32_t)row_token : -1;
-    float up;  // the power of two that a row's scores are multiplied by
-    Row ref;
-    ref.clear();
-    float sum = 0.0f;  // of the weights exp2(score - ref.product)
-    bool far = false;  // whether some row's two references differ, now or before: the sum is then ref.sum
+    // Weights are exp2(products of a row times up - from).  up: a power of two, exact, so that a largest score and its reference are the
+    // same number.  far: whether some row of the wavefront has a lift, or had; the scores are then replaced by those minus the shift plus
+    // the lift, and shift, lift and sum are in LDS, where they take no registers.
+    float up, from = -FLT_MAX, sum = 0.0f;
+    bool far = false;
     {
         const T *src = static_cast<const T *>(a.q) + (s.first + row_token) * a.q_ts + row_head * a.q_hs;
         typedef T V __attribute__((ext_vector_type(8)));
@@ -154,7 +159,9 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[k][i] = (_Float16)(__builtin_amdgcn_ldexpf((float)x[k][i], kQueryTop - e) * sign);
-        up = __builtin_amdgcn_ldexpf(1.0f, e - kQueryTop);
+        // (neither zero nor infinite: times the -infinity of what is not seen, or a score of zero, it would be NaN)
+        up = fminf(fmaxf(__builtin_amdgcn_ldexpf(1.0f, __builtin_amdgcn_frexp_expf(a.factor) + e - kQueryTop + kKeyStaged), 0x1p-149f), 0x1p127f);
+        ups[threadIdx.x] = up;
     }
     v16 acc[JT];
 #pragma unroll
@@ -220,7 +227,7 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
             s_there = (int32_t)token < s.len && page < a.n_pages;
         }
     };
-    const float factor = fabsf(a.factor);
+    const float factor = __builtin_amdgcn_ldexpf(__builtin_amdgcn_frexp_mantf(fabsf(a.factor)), -kKeyStaged);  // (its exponent is in `up`)
     auto eighth_of = [&](uint32_t select) {
         v8h f;
 #pragma unroll
@@ -305,14 +312,17 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
                     for (int i = 0; i < 16; ++i)
                         if (!(there >> (32 * h + 8 * (i / 4) + 4 * hh + i % 4) & 1)) st[h][i] = -__builtin_inff();
         }
-        float high = -FLT_MAX;
+        float high = -__builtin_inff();
 #pragma unroll
         for (int h = 0; h < TH; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i) high = fmaxf(high, st[h][i]);
-        const bool over = high * up > ref.product + kWeightLimit || high * up + most > ref.product + kProductLimit;
-        if (far || __builtin_amdgcn_ballot_w64(over) != 0) {
-            float large = high * up + most;
+        if (far || __builtin_amdgcn_ballot_w64(high * up > from + kWeightLimit || high * up + most > from + kProductLimit) != 0) {
+            const float by = ups[threadIdx.x];
+            Row ref = {from, 0.0f, sum};
+            if (far) ref = lifted[threadIdx.x];
+            high = fmaxf(high, __shfl_xor(high, 32)) * by;
+            float large = most;
             if (sc.uneven) {
                 large = -__builtin_inff();
 #pragma unroll
@@ -321,19 +331,27 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
                     for (int i4 = 0; i4 < 4; ++i4) {
                         const v4 f = *reinterpret_cast<const v4 *>(sc.value + 32 * h + 8 * i4 + 4 * hh);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) large = fmaxf(large, st[h][4 * i4 + i] * up + __builtin_amdgcn_logf(fabsf(f[i])));
+                        for (int i = 0; i < 4; ++i) large = fmaxf(large, __builtin_fmaf(st[h][4 * i4 + i], by, -high) + __builtin_amdgcn_logf(fabsf(f[i])));
                     }
+                large = fmaxf(large, __shfl_xor(large, 32));
             }
-            if (!far) ref.shift = ref.product, ref.sum = sum;
-            const float less = ref.raise(fmaxf(high, __shfl_xor(high, 32)) * up, fmaxf(large, __shfl_xor(large, 32)));
+            const float less = ref.raise(high, large);
 #pragma unroll
             for (int j = 0; j < JT; ++j) acc[j] *= less;
-            far = far || __builtin_amdgcn_ballot_w64(ref.shift != ref.product) != 0;
+            from = ref.shift;
+            far = far || __builtin_amdgcn_ballot_w64(ref.lift != 0.0f) != 0;
             if (far) {
 #pragma unroll
                 for (int h = 0; h < TH; ++h)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) ref.sum += __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][i], up, -ref.shift));
+                    for (int i = 0; i < 16; ++i) {
+                        const float t = __builtin_fmaf(st[h][i], by, -ref.shift);
+                        ref.sum += __builtin_amdgcn_exp2f(t);
+                        st[h][i] = t + ref.lift;
+                    }
+                lifted[threadIdx.x] = ref;
+                up = 1.0f;
+                from = 0.0f;
             }
             sum = ref.sum;
         }
@@ -345,8 +363,7 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
                 const v4 f = *reinterpret_cast<const v4 *>(sc.value + 32 * h + 8 * i4 + 4 * hh);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    // (up is a power of two: the product is exact)
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][4 * i4 + i], up, -ref.product));
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(st[h][4 * i4 + i], up, -from));
                     sum += w;
                     p[2 * h + i4 / 2][4 * (i4 % 2) + i] = (_Float16)(w * f[i]);
                 }
@@ -409,12 +426,11 @@ __global__ __launch_bounds__(kChunkWg, 2) void k_cache_attend_chunk(const uint32
     const size_t part = (size_t)(blockIdx.x / splits) * splits + split;
     if (a.parts && splits > 1 && split == 0 && threadIdx.x == 0)
         a.records[blockIdx.x / splits] = int4{(int)place.b, (int)(q_tile * a.kv_heads + head), (int)part, (int)splits};
-    if (far)
-        sum = ref.sum;
-    else
-        ref.shift = ref.product;
+    Row ref = {from, 0.0f, sum};
+    if (far) ref = lifted[threadIdx.x];
+    sum = ref.sum;
     sum += __shfl_xor(sum, 32);
-    const float r = sum == 0.0f ? 0.0f : 1.0f / (sum * a.entry), down = __builtin_amdgcn_exp2f(ref.product - ref.shift + kStaged);
+    const float r = sum == 0.0f ? 0.0f : 1.0f / (sum * a.entry), down = __builtin_amdgcn_exp2f(kStaged - ref.lift);
     if (!in) return;
     constexpr int W = JT < 4 ? JT : 4;
     if (splits > 1) {

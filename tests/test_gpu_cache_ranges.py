@@ -165,3 +165,51 @@ def test_a_value_that_stands_for_nan_reaches_its_viewers_only(dq8, n):
         first = bad - 60
         assert torch.isnan(got[first:]).all()
         check_attention(got[:first], q[:first], want[:first], tol[:first])
+
+
+@pytest.mark.parametrize("n", [2, 140])
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 1e38, 2.0 ** 98, 2.0 ** 101, 2.0 ** 102, -2.0 ** 103, 2.0 ** 104, 2.0 ** 106])
+def test_the_largest_softmax_scales(dq8, n, scale):
+    """Queries of about 2^-80, scores of about 2^20 to 2^50: they differ by far more than weights can say, and each output is one token's
+    value.  A step between binary32 scores of this size is larger than the range of a product in binary16 leaves room for."""
+    kind, dim, page = 0, 64, 16
+    case = (kind, "bf16", 2, 1, dim, page, [(n, n + 100)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    q = (q.float() * 2.0 ** -80).to(q.dtype)
+    cache[1][1] *= 2.0 ** np.random.default_rng(n).uniform(-20, 20, cache[1][1].shape).astype(np.float32)
+    cb = oracle.codebook(kind).astype(np.float64)
+    j = np.arange(n + 100)
+    k, v = (cb[cache[0][part, pages[0, j // page], 0, j % page]] * cache[1][part, pages[0, j // page], 0, j % page][:, None] for part in (0, 1))
+    cuda = lambda a: torch.from_numpy(a).cuda()
+    for max_new in (1, n):
+        got = host(dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(starts), max_new=max_new, softmax_scale=scale))
+        for i in range(n):
+            for h in range(2):
+                s = k[:101 + i] @ host(q)[i, h].astype(np.float64) * np.sign(scale)
+                best, second = np.argsort(s)[:-3:-1]
+                # keys are off by 2^-11, sums by (dim + 8) 2^-24 of the sum of magnitudes; a closer second is not told apart
+                if s[best] - s[second] > 2 * (2.0 ** -11 + (dim + 8) * 2.0 ** -24) * (np.abs(k[:101 + i]) @ np.abs(host(q)[i, h])).max():
+                    assert (np.abs(got[i, h] - v[best]) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(v[best])).all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 140])
+@pytest.mark.parametrize("power", [0, 18, 24, 26, 60])
+def test_ties_of_large_scores(dq8, n, power):
+    """All keys alike: every token has the same weight whatever the size of the scores, also where the tokens are cut into parts."""
+    kind, dim, page, cached = 0, 64, 64, 2001
+    case = (kind, "bf16", 4, 1, dim, page, [(n, cached)], 0)
+    cache, q, pages, lens, starts = attention_inputs(dq8, case)
+    cache[0][0] = cache[0][0, 0, 0, 0]
+    cache[1][0][np.isfinite(cache[1][0])] = 1.5
+    q = (q.float() * 2.0 ** power).to(q.dtype)
+    j = np.arange(cached)
+    v = oracle.codebook(kind).astype(np.float64)[cache[0][1, pages[0, j // page], 0, j % page]] * cache[1][1, pages[0, j // page], 0, j % page].astype(np.float64)[:, None]
+    count = np.arange(cached - n + 1, cached + 1)[:, None]
+    want, size = (np.cumsum(x, 0)[cached - n:] / count for x in (v, np.abs(v)))
+    # a code's value and a weight times a scale are rounded once to 11 bits; sums of `cached` terms in binary32
+    tol = size * (2 * 2.0 ** -11 + (8 + cached) * 2.0 ** -24) * (1 + 2.0 ** -5)
+    cuda = lambda a: torch.from_numpy(a).cuda()
+    for max_new in (1, n):
+        for workspace in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+            got = dq8.cache_attention(kind, q.cuda(), *to_gpu(cache), cuda(pages), cuda(lens), starts=cuda(starts), max_new=max_new, workspace=workspace)
+            check_attention(got, q, np.repeat(want[:, None], 4, 1), np.repeat(tol[:, None], 4, 1))
