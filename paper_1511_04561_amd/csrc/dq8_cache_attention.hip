@@ -28,12 +28,12 @@ struct Shape {
 
 // Which kernel has the query rows of a cached head and sequence, up to 16 of them the one for few.  us, 8 cached heads of 128 (in
 // parentheses of 64), few | many:
-//   one sequence of 8192, 20 rows 29 | 25 (22 | 19), 64 rows 34 | 28 (28 | 22);  of 1024, 20 rows 18 | 18, 96 rows 23 | 19;
-//   of 400, 20 rows 17 | 21, 96 rows 21 | 22;  2 of 16384, 20 rows 34 | 54 (24 | 42), 96 rows 61 | 59 (39 | 43);
-//   16 of 4096, 20 rows 43 | 95 (27 | 72), 96 rows 92 | 103 (56 | 77), 128 rows 104 | 106 (66 | 79), 192 rows 149 | 114 (94 | 87)
+//   one sequence of 8192, 20 rows 28 | 24 (22 | 20), 64 rows 35 | 28 (28 | 21);  of 1024, 20 rows 18 | 18, 96 rows 24 | 20;
+//   of 400, 20 rows 17 | 21, 96 rows 21 | 22;  2 of 16384, 20 rows 38 | 52 (25 | 41), 96 rows 61 | 59 (40 | 44);
+//   16 of 4096, 20 rows 42 | 91 (28 | 72), 96 rows 93 | 100 (57 | 78), 128 rows 106 | 104 (67 | 80), 192 rows 150 | 112 (95 | 87)
 // A tile costs the one for many as much whatever the rows, but it leaves a part per workgroup to the join and not one per wavefront: it has
 // them above 128 rows, and fewer where its workgroups have a few tiles each of sequences that are not short.  Heads of 256, whose keys
-// and values the one for few reads again for every 16 rows: 16 of 4096, 64 rows 304 | 391, 68 rows 418 | 400.
+// and values the one for few reads again for every 16 rows: 16 of 4096, 64 rows 291 | 378, 68 rows 402 | 379.
 bool for_many(size_t rows, int dp, size_t jobs, size_t tiles, int cus)
 {
     if (dp == 256) return rows > 64;

@@ -10,11 +10,13 @@
 // in range is asked of its largest weight and the tile's largest scale; where they may not, its reference is moved by these two too, which
 // say too much by 2^kEven at most, or else by all of its products.
 //
-// What bounds it (2048 new tokens after 8192, 32 heads on 8 of 128: 309 GFLOP in 440 us, 0.70 PFLOP/s; a large matrix product of the library
-// reaches 1.20): the matrix units are busy for 29 % of the time, the vector unit 43 %, LDS 49 %, and wavefronts wait for half of
-// theirs: a tile's scores, weights and sums are one chain, and two wavefronts per SIMD, all that the registers allow, do not cover it.
-// Half of the wavefronts go half a tile late, so that one's products meet another's weights (562 -> 520 us in the profiler's
-// clocks); 64 rows per wavefront and four of them: spills; without LDS, each wavefront looking up its own tiles: 3260 us.
+// What bounds it (2048 new tokens after 8192, 32 heads on 8 of 128: 309 GFLOP in 440 to 500 us by the card's clocks, 0.62 to 0.70
+// PFLOP/s; a large matrix product of the library reaches 1.20): a tile's scores, weights and sums are one chain, and two wavefronts
+// per SIMD, all that the registers allow, do not cover it.  Counters (a dispatch of 511 us): the matrix units are busy for 30 % of the time,
+// the vector unit 43 %, LDS 49 %, and wavefronts wait for half of theirs.  Half of the wavefronts go half a tile late, so that one's
+// products meet another's weights (562 -> 520 us in the profiler's clocks); 64 rows per wavefront and four of them: many more spills;
+// without LDS, each wavefront looking up its own tiles: 3260 us.  Of the 256 registers the heads of 128 spill 28: a tile with hidden tokens
+// reads 13 of them back, the others are for the branch that moves references.  Heads of 256 spill 84, some in every tile.
 #pragma once
 #include "dq8_kernels_attend.hpp"
 

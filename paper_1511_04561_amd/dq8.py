@@ -482,7 +482,7 @@ def cache_append(kind, k, v, slots, codes, scales, positions=None, rotation=None
     and sines of every position, ``positions`` int64) of the keys.  Queries [tokens, heads, dim] get theirs in the same pass.
 
     k, v and q may be views whose rows are contiguous (parts of a projection's output).  Returns the queries (``q_out``, a new tensor
-    or q itself), None without q."""
+    or q itself), None without q.  For serving: as with every call here no gradient passes through it."""
     done = _native.cache_append(kind, k, v, slots, codes, scales, positions, rotation, interleaved, q, q_weight, k_weight, eps, q_out)
     if done is not None:
         return None if done is False else done
@@ -566,7 +566,8 @@ def cache_attention(kind, q, codes, scales, pages, lens, starts=None, max_new=No
     among them.  starts int32 [sequences + 1]: where each sequence's new tokens begin in q; None: every sequence has as many.
     max_new: the largest number of new tokens of a sequence, where the host knows it.  window > 0: a query sees that many tokens at most.
     workspace: a uint8 tensor of cache_attention_workspace() bytes; None: taken from torch's allocator, and not while the stream is
-    captured into a graph (hand one in there: without it few sequences are slow)."""
+    captured into a graph (hand one in there: without it one wavefront or workgroup reads the whole of a sequence's head).  For
+    serving: as with every call here no gradient passes through it."""
     done = _native.cache_attention(kind, q, codes, scales, pages, lens, starts, max_new, softmax_scale, window, out, workspace)
     if done is not None:
         return done
