@@ -137,7 +137,18 @@ __device__ __forceinline__ void normed_and_turned(const AppendArgs &a, const Pla
         F sum = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
-        const F r = F(1) / sqrt(row_sum<LPR>(sum) / F(a.dim) + F(a.eps));
+        sum = row_sum<LPR>(sum);
+        F r = F(1) / sqrt(sum / F(a.dim) + F(a.eps));
+        if constexpr (sizeof(F) == 4) {  // squares that binary32 does not hold, or holds with few bits where eps does not hide them
+            const bool large = sum > 0x1p120f;
+            if (large || (sum < 0x1p-100f && a.eps < 0x1p-33)) {  // (the same for all lanes of a row)
+                const float by = large ? 0x1p-80f : 0x1p80f;
+                sum = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += (y[e] * by) * (y[e] * by);
+                r = by / sqrt(row_sum<LPR>(sum) / F(a.dim) + (float)(a.eps * (double)by * (double)by));
+            }
+        }
         if (in)
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = y[e] * r * F(p.w[e]);
