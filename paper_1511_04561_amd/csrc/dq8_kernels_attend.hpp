@@ -26,7 +26,7 @@
 // products, there are two: Row.
 //
 // What bounds it: memory, less well used than by a copy.  64 sequences of up to 4096, 8 heads of 128: 292 MB in 60 us (4.9 TB/s) and 5 us of
-// join; two of up to 131072: 391 MB in 74 us (5.3 TB/s) and 7 us; loads alone in the same order reach 6.7.  A wavefront holds two tiles, one
+// join; two of up to 131072: 391 MB in 75 us (5.2 TB/s) and 7 us; loads alone in the same order reach 6.7.  A wavefront holds two tiles, one
 // in flight; LDS, a look-up per code and its 16-bit half, is busy for 57 % of the time, the vector unit 39 %, the matrix units 7 %.
 // Short calls (one sequence of 1337: 10 us) wait for the instructions themselves, the table and three loads that need each other.
 #pragma once
