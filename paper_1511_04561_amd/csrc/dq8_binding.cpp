@@ -19,6 +19,7 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -26,6 +27,8 @@
 #include <exception>
 
 #include "dq8_cache.h"
+#include "dq8_serve.h"
+#include "dq8_weights.h"
 #include "dq8_workspace.h"
 
 namespace {
@@ -49,6 +52,12 @@ struct Library {
     decltype(&dq8_cache_append) cache_append;
     decltype(&dq8_cache_attention) cache_attention;
     decltype(&dq8_cache_attention_workspace_bytes) workspace_attention;
+    decltype(&dq8_weights_encode) weights_encode;
+    decltype(&dq8_weights_decode) weights_decode;
+    decltype(&dq8_weights_product) weights_product;
+    decltype(&dq8_cache_plan) cache_plan;
+    decltype(&dq8_draft_verify) draft_verify;
+    decltype(&dq8_draft_verify_workspace_bytes) workspace_verify;
     decltype(&dq8_last_error) last_error;
 } g_lib;
 PyObject *g_error = nullptr;
@@ -661,6 +670,244 @@ PyObject *cache_attention(PyObject *const *a)  // kind, q, codes, scales, pages,
     return THPVariable_Wrap(made);
 }
 
+// ---- weights in 4 bits (dq8_weights.h) and the steps around the cache (dq8_serve.h)
+
+// A new reference to a tensor that was handed in, or to the one that was made.
+PyObject *handed(PyObject *given, const at::Tensor &made) { return given == Py_None ? THPVariable_Wrap(made) : Py_NewRef(given); }
+
+// N results as a tuple.
+template <int N>
+PyObject *tuple_of(PyObject *const (&given)[N], const at::Tensor (&made)[N])
+{
+    PyObject *r = PyTuple_New(N);
+    for (int i = 0; r && i < N; ++i) {
+        PyObject *o = handed(given[i], made[i]);
+        if (!o) {
+            Py_DECREF(r);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(r, i, o);
+    }
+    return r;
+}
+
+bool fresh(at::Tensor &made, at::IntArrayRef sizes, const at::Tensor &like, at::ScalarType type)
+{
+    made = at::empty(sizes, like.options().dtype(type).requires_grad(false));
+    return !made.key_set().has_any(kTransformed);
+}
+
+// A contiguous array of one axis with n elements on `like`'s device: the one handed in or, where that is allowed, a new one.
+bool axis(PyObject *o, at::ScalarType type, size_t n, const at::Tensor &like, void *&ptr, at::Tensor *made = nullptr)
+{
+    if (made && o == Py_None) {
+        if (!fresh(*made, {(int64_t)n}, like, type)) return false;
+        ptr = made->data_ptr();
+        return true;
+    }
+    Buffer b;
+    if (!buffer(o, type, b) || b.t->dim() != 1 || b.n != n || b.t->get_device() != like.get_device()) return false;
+    ptr = b.ptr;
+    return true;
+}
+
+// [rows, cols], neither of them 0, with the elements of a row side by side.
+struct Matrix {
+    const at::Tensor *t = nullptr;
+    void *ptr = nullptr;
+    size_t rows = 0, cols = 0, stride = 0;
+    int type = 0;
+
+    bool take(PyObject *o) { return THPVariable_CheckExact(o) && take(THPVariable_Unpack(o)); }
+
+    bool take(const at::Tensor &x)
+    {
+        if (!x.defined() || !x.is_cuda() || x.key_set().has_any(kTransformed) || x.layout() != at::kStrided || !x.has_storage() || x.dim() != 2 ||
+            x.size(0) == 0 || x.size(1) == 0 || x.stride(0) < 0 || (x.stride(1) != 1 && x.size(1) != 1) || !type_of(x, type))
+            return false;
+        t = &x;
+        ptr = x.data_ptr();
+        rows = (size_t)x.size(0), cols = (size_t)x.size(1), stride = (size_t)x.stride(0);
+        return true;
+    }
+
+    bool like(const Matrix &o) const { return type == o.type && rows == o.rows && cols == o.cols && beside(*o.t); }
+    bool beside(const at::Tensor &o) const { return t->get_device() == o.get_device(); }
+};
+
+// Codes and scales of rows x cols weights (0: as many as the tiles have).
+struct Weights {
+    dq8_weights w = {};
+    const at::Tensor *codes = nullptr;
+
+    bool take(PyObject *codes_, PyObject *scales_, size_t rows, size_t cols)
+    {
+        Buffer c, s;
+        return buffer(codes_, at::kByte, c) && buffer(scales_, at::kBFloat16, s) && take(*c.t, *s.t, rows, cols);
+    }
+
+    bool take(const at::Tensor &c, const at::Tensor &s, size_t rows, size_t cols)
+    {
+        if (c.dim() != 3 || s.dim() != 4 || c.size(2) != 1024 || s.size(0) != c.size(0) || s.size(1) != c.size(1) || s.size(2) != 16 ||
+            (s.size(3) != 1 && s.size(3) != 2 && s.size(3) != 4) || c.get_device() != s.get_device())
+            return false;
+        const size_t tall = (size_t)c.size(0), wide = (size_t)c.size(1);
+        if (tall == 0 || wide == 0) return false;
+        if (rows == 0) rows = 16 * tall;
+        if (cols == 0) cols = 128 * wide;
+        if ((rows + 15) / 16 != tall || (cols + 127) / 128 != wide) return false;
+        codes = &c;
+        w = {static_cast<uint8_t *>(c.data_ptr()), s.data_ptr(), rows, cols, (int)(128 / s.size(3))};
+        return true;
+    }
+};
+
+// A positive number, or 0 for None.
+bool size_or_none(PyObject *o, size_t &v)
+{
+    v = 0;
+    return o == Py_None || (whole(o, v) && v != 0);
+}
+
+bool dtype_of(PyObject *o, at::ScalarType &type)
+{
+    if (!THPDtype_Check(o)) return false;
+    type = reinterpret_cast<THPDtype *>(o)->scalar_type;
+    return true;
+}
+
+PyObject *weights_encode(PyObject *const *a)  // w, group, codes, scales
+{
+    Matrix w;
+    size_t group;
+    Weights to;
+    void *stream;
+    at::Tensor made[2];
+    if (!w.take(a[0]) || !whole(a[1], group) || (group != 32 && group != 64 && group != 128) || !stream_for(*w.t, stream)) return declined();
+    const int64_t tall = (int64_t)(w.rows + 15) / 16, wide = (int64_t)(w.cols + 127) / 128, per = (int64_t)(128 / group);
+    const at::Tensor *t[2];
+    for (int i = 0; i < 2; ++i) {
+        if (a[2 + i] == Py_None) {
+            if (!(i == 0 ? fresh(made[0], {tall, wide, 1024}, *w.t, at::kByte) : fresh(made[1], {tall, wide, 16, per}, *w.t, at::kBFloat16))) return declined();
+            t[i] = &made[i];
+        } else {
+            Buffer b;
+            if (!buffer(a[2 + i], i == 0 ? at::kByte : at::kBFloat16, b)) return declined();
+            t[i] = b.t;
+        }
+    }
+    if (!to.take(*t[0], *t[1], w.rows, w.cols) || (size_t)to.w.group != group || !w.beside(*t[0])) return declined();
+    if (!enqueue("dq8_weights_encode", [&] { return g_lib.weights_encode(w.type, w.ptr, w.stride, &to.w, stream); })) return nullptr;
+    PyObject *const given[2] = {a[2], a[3]};
+    return tuple_of(given, made);
+}
+
+PyObject *weights_decode(PyObject *const *a)  // codes, scales, rows, cols, dtype, out
+{
+    Weights from;
+    Matrix out;
+    size_t rows, cols;
+    at::ScalarType type;
+    void *stream;
+    at::Tensor made;
+    if (!size_or_none(a[2], rows) || !size_or_none(a[3], cols) || !dtype_of(a[4], type) || !from.take(a[0], a[1], rows, cols) || !stream_for(*from.codes, stream))
+        return declined();
+    if (a[5] == Py_None) {
+        if (type != at::kFloat && type != at::kBFloat16 && type != at::kHalf) return declined();
+        if (!fresh(made, {(int64_t)from.w.rows, (int64_t)from.w.cols}, *from.codes, type) || !out.take(made)) return declined();
+    } else if (!out.take(a[5])) {
+        return declined();
+    }
+    if (out.t->scalar_type() != type || out.rows != from.w.rows || out.cols != from.w.cols || !out.beside(*from.codes)) return declined();
+    if (!enqueue("dq8_weights_decode", [&] { return g_lib.weights_decode(&from.w, out.type, out.ptr, out.stride, stream); })) return nullptr;
+    return handed(a[5], made);
+}
+
+PyObject *weights_product(PyObject *const *a)  // x, codes, scales, rows, bias, dtype, out
+{
+    Matrix x, out;
+    Weights w;
+    size_t rows;
+    void *stream, *bias = nullptr;
+    at::Tensor made;
+    dq8_product p = {};
+    if (!x.take(a[0]) || x.type == DQ8_FLOAT32 || !size_or_none(a[3], rows) || !w.take(a[1], a[2], rows, x.cols) || !x.beside(*w.codes) ||
+        !stream_for(*x.t, stream))
+        return declined();
+    at::ScalarType type = x.t->scalar_type();
+    if (a[5] != Py_None && !dtype_of(a[5], type)) return declined();
+    if (a[6] == Py_None) {
+        if ((type != x.t->scalar_type() && type != at::kFloat) || !fresh(made, {(int64_t)x.rows, (int64_t)w.w.rows}, *x.t, type) || !out.take(made)) return declined();
+    } else if (!out.take(a[6]) || (a[5] != Py_None && out.t->scalar_type() != type)) {
+        return declined();
+    }
+    if ((out.type != x.type && out.type != DQ8_FLOAT32) || out.rows != x.rows || out.cols != w.w.rows || !out.beside(*x.t)) return declined();
+    if (a[4] != Py_None && !axis(a[4], at::kFloat, w.w.rows, *x.t, bias)) return declined();
+    p.type = x.type, p.out_type = out.type, p.tokens = x.rows, p.x = x.ptr, p.x_stride = x.stride, p.out = out.ptr, p.out_stride = out.stride;
+    p.bias = static_cast<const float *>(bias);
+    if (!enqueue("dq8_weights_product", [&] { return g_lib.weights_product(&w.w, &p, stream); })) return nullptr;
+    return handed(a[6], made);
+}
+
+PyObject *cache_plan(PyObject *const *a)  // lens, new, pages, free, n_free, page_size, tokens, drop, slots, positions, starts, lens_out, granted, n_free_out
+{
+    Buffer pages, free;
+    size_t page_size, tokens;
+    void *stream, *p[11] = {};
+    at::Tensor made[6];
+    dq8_plan x = {};
+    if (!buffer(a[2], at::kInt, pages) || pages.t->dim() != 2 || pages.n == 0 || !buffer(a[3], at::kInt, free) || free.t->dim() != 1 || free.n == 0 ||
+        !whole(a[5], page_size) || page_size > INT32_MAX || !whole(a[6], tokens) || tokens > INT32_MAX || !stream_for(*pages.t, stream) ||
+        free.t->get_device() != pages.t->get_device())
+        return declined();
+    const at::Tensor &like = *pages.t;
+    x.batch = (size_t)like.size(0), x.max_pages = (size_t)like.size(1), x.tokens = tokens, x.free_capacity = free.n, x.page_size = (int)page_size;
+    if (!axis(a[0], at::kInt, x.batch, like, p[0]) || !axis(a[1], at::kInt, x.batch, like, p[1]) || !axis(a[4], at::kInt, 1, like, p[2]) ||
+        (a[7] != Py_None && !axis(a[7], at::kInt, x.batch, like, p[3])) || !axis(a[8], at::kLong, tokens, like, p[4], &made[0]) ||
+        !axis(a[9], at::kLong, tokens, like, p[5], &made[1]) || !axis(a[10], at::kInt, x.batch + 1, like, p[6], &made[2]) ||
+        !axis(a[11], at::kInt, x.batch, like, p[7], &made[3]) || !axis(a[12], at::kInt, x.batch, like, p[8], &made[4]) || !axis(a[13], at::kInt, 1, like, p[9], &made[5]))
+        return declined();
+    x.lens = static_cast<int32_t *>(p[0]), x.new_tokens = static_cast<int32_t *>(p[1]), x.n_free = static_cast<int32_t *>(p[2]), x.drop = static_cast<int32_t *>(p[3]);
+    x.pages = static_cast<int32_t *>(pages.ptr), x.free_pages = static_cast<int32_t *>(free.ptr);
+    x.slots = static_cast<int64_t *>(p[4]), x.positions = static_cast<int64_t *>(p[5]), x.starts = static_cast<int32_t *>(p[6]);
+    x.lens_out = static_cast<int32_t *>(p[7]), x.granted = static_cast<int32_t *>(p[8]), x.n_free_out = static_cast<int32_t *>(p[9]);
+    if (!enqueue("dq8_cache_plan", [&] { return g_lib.cache_plan(&x, stream); })) return nullptr;
+    PyObject *const given[6] = {a[8], a[9], a[10], a[11], a[12], a[13]};
+    return tuple_of(given, made);
+}
+
+PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace
+{
+    Matrix target, draft;
+    Buffer sample, space;
+    void *stream, *p[6] = {};
+    at::Tensor made[3];
+    dq8_verify v = {};
+    if (!target.take(a[0]) || !stream_for(*target.t, stream) || !buffer(a[3], at::kFloat, sample) || sample.t->dim() != 1 || sample.n == 0 ||
+        !target.beside(*sample.t) || (a[5] != Py_None && (!draft.take(a[5]) || !draft.like(target))))
+        return declined();
+    const at::Tensor &like = *target.t;
+    v.type = target.type, v.tokens = target.rows, v.vocab = target.cols, v.batch = sample.n;
+    v.target = target.ptr, v.target_stride = target.stride, v.draft = draft.ptr, v.draft_stride = draft.stride;
+    if (!axis(a[1], at::kLong, v.tokens, like, p[0]) || !axis(a[2], at::kFloat, v.tokens, like, p[1]) ||
+        (a[4] != Py_None && !axis(a[4], at::kInt, v.batch + 1, like, p[2])) || !axis(a[6], at::kLong, v.tokens, like, p[3], &made[0]) ||
+        !axis(a[7], at::kInt, v.batch, like, p[4], &made[1]) || !axis(a[8], at::kInt, v.batch, like, p[5], &made[2]))
+        return declined();
+    v.ids = static_cast<int64_t *>(p[0]), v.uniform = static_cast<float *>(p[1]), v.sample = static_cast<float *>(sample.ptr);
+    v.starts = static_cast<int32_t *>(p[2]), v.out = static_cast<int64_t *>(p[3]), v.accepted = static_cast<int32_t *>(p[4]), v.rejected = static_cast<int32_t *>(p[5]);
+    Scratch scratch;
+    if (a[9] == Py_None) {
+        if (!scratch.take(g_lib.workspace_verify(&v), like, stream)) return declined();
+    } else {
+        if (!buffer(a[9], at::kByte, space) || !target.beside(*space.t)) return declined();
+        scratch.ptr = space.n ? space.ptr : nullptr;
+        scratch.bytes = space.n;
+    }
+    if (!enqueue("dq8_draft_verify", [&] { return g_lib.draft_verify(&v, scratch.ptr, scratch.bytes, stream); })) return nullptr;
+    PyObject *const given[3] = {a[6], a[7], a[8]};
+    return tuple_of(given, made);
+}
+
 // bind(error class, {name: address}): the entry points of the library that dq8.py has loaded.
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -692,6 +939,12 @@ PyObject *bind(PyObject *, PyObject *args)
     take(l.cache_append, "dq8_cache_append");
     take(l.cache_attention, "dq8_cache_attention");
     take(l.workspace_attention, "dq8_cache_attention_workspace_bytes");
+    take(l.weights_encode, "dq8_weights_encode");
+    take(l.weights_decode, "dq8_weights_decode");
+    take(l.weights_product, "dq8_weights_product");
+    take(l.cache_plan, "dq8_cache_plan");
+    take(l.draft_verify, "dq8_draft_verify");
+    take(l.workspace_verify, "dq8_draft_verify_workspace_bytes");
     take(l.last_error, "dq8_last_error");
     if (!ok) return nullptr;
     g_lib = l;
@@ -719,6 +972,11 @@ PyMethodDef g_methods[] = {
     method<error_stats, 7>("error_stats"),
     method<cache_append, 14>("cache_append"),
     method<cache_attention, 12>("cache_attention"),
+    method<weights_encode, 4>("weights_encode"),
+    method<weights_decode, 6>("weights_decode"),
+    method<weights_product, 7>("weights_product"),
+    method<cache_plan, 14>("cache_plan"),
+    method<draft_verify, 10>("draft_verify"),
     {nullptr, nullptr, 0, nullptr},
 };
 

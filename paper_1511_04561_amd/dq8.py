@@ -61,6 +61,27 @@ class _Attention(ctypes.Structure):  # dq8_attention
                 + [("max_new", ctypes.c_size_t), ("window", ctypes.c_int), ("softmax_scale", ctypes.c_float)])
 
 
+class _Weights(ctypes.Structure):  # dq8_weights of include/dq8_weights.h
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_size_t), ("cols", ctypes.c_size_t), ("group", ctypes.c_int)]
+
+
+class _Product(ctypes.Structure):  # dq8_product
+    _fields_ = [("type", ctypes.c_int), ("out_type", ctypes.c_int), ("tokens", ctypes.c_size_t), ("x", ctypes.c_void_p), ("x_stride", ctypes.c_size_t),
+                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_size_t), ("bias", ctypes.c_void_p)]
+
+
+class _Plan(ctypes.Structure):  # dq8_plan of include/dq8_serve.h
+    _fields_ = ([(f, ctypes.c_size_t) for f in ("batch", "max_pages", "tokens", "free_capacity")] + [("page_size", ctypes.c_int)]
+                + [(f, ctypes.c_void_p) for f in ("lens", "new_tokens", "drop", "pages", "free_pages", "n_free", "slots", "positions", "starts", "lens_out",
+                                                  "granted", "n_free_out")])
+
+
+class _Verify(ctypes.Structure):  # dq8_verify
+    _fields_ = ([("type", ctypes.c_int)] + [(f, ctypes.c_size_t) for f in ("tokens", "batch", "vocab")] + [(f, ctypes.c_void_p) for f in ("target", "draft")]
+                + [(f, ctypes.c_size_t) for f in ("target_stride", "draft_stride")]
+                + [(f, ctypes.c_void_p) for f in ("ids", "uniform", "sample", "starts", "out", "accepted", "rejected")])
+
+
 def lib():
     """The loaded shared library (loaded on first use)."""
     global _lib, _native
@@ -93,6 +114,15 @@ def lib():
         L.dq8_cache_attention.restype = ci
         L.dq8_cache_attention_workspace_bytes.argtypes = [ctypes.POINTER(_Cache), ctypes.POINTER(_Attention)]
         L.dq8_cache_attention_workspace_bytes.restype = sz
+        L.dq8_weights_encode.argtypes = [ci, vp, sz, ctypes.POINTER(_Weights), vp]
+        L.dq8_weights_decode.argtypes = [ctypes.POINTER(_Weights), ci, vp, sz, vp]
+        L.dq8_weights_product.argtypes = [ctypes.POINTER(_Weights), ctypes.POINTER(_Product), vp]
+        L.dq8_cache_plan.argtypes = [ctypes.POINTER(_Plan), vp]
+        L.dq8_draft_verify.argtypes = [ctypes.POINTER(_Verify), vp, sz, vp]
+        L.dq8_draft_verify_workspace_bytes.argtypes = [ctypes.POINTER(_Verify)]
+        for f in (L.dq8_weights_encode, L.dq8_weights_decode, L.dq8_weights_product, L.dq8_cache_plan, L.dq8_draft_verify):
+            f.restype = ci
+        L.dq8_draft_verify_workspace_bytes.restype = sz
         dbl = ctypes.c_double
         L.dq8_model_speedup.argtypes = [ci, dbl, dbl, dbl, ci, dbl, dbl, ctypes.POINTER(dbl)]
         L.dq8_model_penalty.argtypes = [ctypes.POINTER(dbl), ctypes.POINTER(dbl), sz, ctypes.POINTER(dbl)]
@@ -113,7 +143,8 @@ _BOUND = ("dq8_absmax", "dq8_encode_ws", "dq8_workspace_bytes", "dq8_decode", "d
           "dq8_workspace_bytes_segments", "dq8_decode_segments",
           "dq8_decode_accumulate_avg", "dq8_decode_accumulate_avg_local", "dq8_decode_accumulate_avg_segments",
           "dq8_decode_avg_encode", "dq8_error_stats_ws", "dq8_workspace_bytes_stats", "dq8_cache_append", "dq8_cache_attention",
-          "dq8_cache_attention_workspace_bytes", "dq8_last_error")
+          "dq8_cache_attention_workspace_bytes", "dq8_weights_encode", "dq8_weights_decode", "dq8_weights_product", "dq8_cache_plan",
+          "dq8_draft_verify", "dq8_draft_verify_workspace_bytes", "dq8_last_error")
 
 
 def _check(rc, what):
@@ -587,6 +618,222 @@ def cache_attention(kind, q, codes, scales, pages, lens, starts=None, max_new=No
     _enqueue(lib().dq8_cache_attention, codes.get_device(), _int32(kind, "kind"), ctypes.byref(c), ctypes.byref(a),
              workspace.data_ptr() if workspace is not None and workspace.numel() else None, 0 if workspace is None else workspace.numel())
     return out
+
+
+def _matrix(t, what, device, dtypes, rows, cols):
+    """[rows, cols] (None: any) with the elements of a row side by side: (address, stride)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s, got %s" % (what, " or ".join(str(d) for d in dtypes), t.dtype))
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError("%s must have shape [%s, %s], got %s" % (what, "any" if rows is None else rows, "any" if cols is None else cols, tuple(t.shape)))
+    if t.stride(1) != 1 and t.shape[1] > 1 and t.numel():
+        raise ValueError("the elements of a row of %s must lie side by side" % what)
+    if device is not None and t.device != device:
+        raise ValueError("%s is on another device than the other arrays" % what)
+    return t.data_ptr(), t.stride(0)
+
+
+def _weights(codes, scales, rows, cols):
+    """The struct of compressed weights; rows or cols None: as many as the tiles have."""
+    _dev(codes, torch.uint8, "codes")
+    _dev(scales, torch.bfloat16, "scales")
+    if codes.dim() != 3 or codes.shape[2] != 1024 or scales.dim() != 4 or scales.shape[:2] != codes.shape[:2] or scales.shape[2] != 16 or scales.shape[3] not in (1, 2, 4):
+        raise ValueError("codes must be [row tiles, column tiles, 1024] and scales [row tiles, column tiles, 16, 128 / group]")
+    if scales.device != codes.device:
+        raise ValueError("codes and scales are on different devices")
+    tall, wide = codes.shape[:2]
+    rows = 16 * tall if rows is None else int(rows)
+    cols = 128 * wide if cols is None else int(cols)
+    if not 16 * tall - 16 < rows <= 16 * tall and (rows, tall) != (0, 0):
+        raise ValueError("%d rows do not fill %d tiles of 16" % (rows, tall))
+    if not 128 * wide - 128 < cols <= 128 * wide and (cols, wide) != (0, 0):
+        raise ValueError("%d columns do not fill %d tiles of 128" % (cols, wide))
+    return _Weights(codes.data_ptr(), scales.data_ptr(), rows, cols, 128 // scales.shape[3])
+
+
+def weights_encode(w, group=32, codes=None, scales=None):
+    """Weights [rows, cols] (float32, bfloat16 or float16) in 4 bits, one bfloat16 scale per ``group`` (32, 64 or 128) neighbours of a row.
+
+    Returns (codes uint8 [row tiles, column tiles, 1024], scales bfloat16 [row tiles, column tiles, 16, 128 / group]); a tile has 16 rows and
+    128 columns (include/dq8_weights.h has the layout), so that codes[a:b], scales[a:b] are the weights' rows 16 a .. 16 b - 1."""
+    done = _native.weights_encode(w, group, codes, scales)
+    if done is not None:
+        return done
+    at, stride = _matrix(w, "w", None, tuple(_TYPES), None, None)
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128, got %r" % (group,))
+    tall, wide = -(-w.shape[0] // 16), -(-w.shape[1] // 128)
+    if codes is None:
+        codes = torch.empty((tall, wide, 1024), dtype=torch.uint8, device=w.device)
+    if scales is None:
+        scales = torch.empty((tall, wide, 16, 128 // group), dtype=torch.bfloat16, device=w.device)
+    c = _weights(codes, scales, *w.shape)
+    if c.group != group:
+        raise ValueError("scales are those of groups of %d" % c.group)
+    if codes.device != w.device:
+        raise ValueError("w is on another device than codes")
+    _enqueue(lib().dq8_weights_encode, w.get_device(), _TYPES[w.dtype], at, stride, ctypes.byref(c))
+    return codes, scales
+
+
+def weights_decode(codes, scales, rows=None, cols=None, dtype=torch.float32, out=None):
+    """The values [rows, cols] of compressed weights (rows, cols None: whole tiles), rounded to ``dtype``."""
+    done = _native.weights_decode(codes, scales, rows, cols, dtype, out)
+    if done is not None:
+        return done
+    c = _weights(codes, scales, rows, cols)
+    if out is None:
+        out = torch.empty((c.rows, c.cols), dtype=dtype, device=codes.device)
+    elif out.dtype != dtype:
+        raise TypeError("out must be %s, got %s" % (dtype, out.dtype))
+    at, stride = _matrix(out, "out", codes.device, tuple(_TYPES), c.rows, c.cols)
+    _enqueue(lib().dq8_weights_decode, codes.get_device(), ctypes.byref(c), _TYPES[out.dtype], at, stride)
+    return out
+
+
+def weights_product(x, codes, scales, rows=None, bias=None, dtype=None, out=None):
+    """x [tokens, cols] (bfloat16 or float16) times compressed weights, out[m, n] = sum_k x[m, k] w[n, k] (+ bias[n], float32).
+
+    rows: of the weights, where these do not fill their last tile.  dtype: of the result, x's or float32.  For serving: as with every call
+    here no gradient passes through it."""
+    done = _native.weights_product(x, codes, scales, rows, bias, dtype, out)
+    if done is not None:
+        return done
+    at, stride = _matrix(x, "x", None, (torch.bfloat16, torch.float16), None, None)
+    c = _weights(codes, scales, rows, x.shape[1])
+    if codes.device != x.device:
+        raise ValueError("x is on another device than codes")
+    if dtype is None:
+        dtype = x.dtype if out is None else out.dtype
+    if dtype not in (x.dtype, torch.float32):
+        raise TypeError("dtype must be %s or torch.float32, got %s" % (x.dtype, dtype))
+    if out is None:
+        out = torch.empty((x.shape[0], c.rows), dtype=dtype, device=x.device)
+    p = _Product()
+    p.type, p.out_type, p.tokens, p.x, p.x_stride = _TYPES[x.dtype], _TYPES[dtype], x.shape[0], at, stride
+    p.out, p.out_stride = _matrix(out, "out", x.device, (dtype,), x.shape[0], c.rows)
+    if bias is not None:
+        _dev(bias, torch.float32, "bias")
+        if tuple(bias.shape) != (c.rows,) or bias.device != x.device:
+            raise ValueError("bias must have shape [%d] on x's device" % c.rows)
+        p.bias = bias.data_ptr()
+    _enqueue(lib().dq8_weights_product, x.get_device(), ctypes.byref(c), ctypes.byref(p))
+    return out
+
+
+def cache_free_list(pages, device="cuda"):
+    """(free, n_free) of a cache whose pages are all free, for cache_plan: a stack of page numbers, int32 [pages], the lowest on top, and how
+    many of its entries are valid, int32 [1]."""
+    return torch.arange(int(pages) - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), int(pages), dtype=torch.int32, device=device)
+
+
+def _given(t, device, dtype, shape, what):
+    """A contiguous tensor of exactly this type, shape and device (None: a new one)."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _dev(t, dtype, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if t.device != device:
+        raise ValueError("%s is on another device than the other arrays" % what)
+    return t
+
+
+def cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop=None, slots=None, positions=None, starts=None, lens_out=None, granted=None,
+               n_free_out=None):
+    """Where the new tokens of a step go in a paged cache.
+
+    lens int32 [sequences]: cached tokens; drop int32 (None: none): how many of them are taken back first (rejected drafts; all of a
+    sequence that has ended); new int32: how many are added.  pages int32 [sequences, n]: each sequence's page numbers, in place; free int32 and n_free
+    int32 [1]: the stack of free pages, pages given back and taken in place.  A sequence gets all places that it needs or is refused and
+    stays as it was (granted -1).  tokens: rows of the step, padding among them.
+
+    Returns (slots int64 [tokens], positions int64 [tokens], starts int32 [sequences + 1], lens_out, granted, n_free_out): -1 in slots and positions
+    for padding and refused sequences; lens_out may be lens and n_free_out may be n_free."""
+    done = _native.cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop, slots, positions, starts, lens_out, granted, n_free_out)
+    if done is not None:
+        return done
+    _dev(pages, torch.int32, "pages")
+    _dev(free, torch.int32, "free")
+    if pages.dim() != 2 or free.dim() != 1:
+        raise ValueError("pages must be [sequences, pages of the longest] and free [pages]")
+    tokens = int(tokens)
+    if not 0 <= tokens < 2 ** 31:
+        raise ValueError("tokens must be a number of tokens, got %d" % tokens)
+    dev, batch = pages.device, pages.shape[0]
+    p = _Plan()
+    p.batch, p.max_pages, p.tokens, p.free_capacity, p.page_size = batch, pages.shape[1], tokens, free.shape[0], _int32(page_size, "page_size")
+    lens, new, n_free = (_given(t, dev, torch.int32, (n,), what) if t is not None else _dev(t, torch.int32, what)
+                         for t, n, what in ((lens, batch, "lens"), (new, batch, "new"), (n_free, 1, "n_free")))
+    if drop is not None:
+        p.drop = _given(drop, dev, torch.int32, (batch,), "drop").data_ptr()
+    if free.device != dev:
+        raise ValueError("free is on another device than pages")
+    slots, positions = _given(slots, dev, torch.int64, (tokens,), "slots"), _given(positions, dev, torch.int64, (tokens,), "positions")
+    starts, lens_out = _given(starts, dev, torch.int32, (batch + 1,), "starts"), _given(lens_out, dev, torch.int32, (batch,), "lens_out")
+    granted, n_free_out = _given(granted, dev, torch.int32, (batch,), "granted"), _given(n_free_out, dev, torch.int32, (1,), "n_free_out")
+    p.lens, p.new_tokens, p.pages, p.free_pages, p.n_free = (t.data_ptr() for t in (lens, new, pages, free, n_free))
+    p.slots, p.positions, p.starts, p.lens_out, p.granted, p.n_free_out = (t.data_ptr() for t in (slots, positions, starts, lens_out, granted, n_free_out))
+    _enqueue(lib().dq8_cache_plan, pages.get_device(), ctypes.byref(p))
+    return slots, positions, starts, lens_out, granted, n_free_out
+
+
+def _draft(target, ids, uniform, sample, starts, draft):
+    v = _Verify()
+    v.target, v.target_stride = _matrix(target, "target", None, tuple(_TYPES), None, None)
+    dev = target.device
+    v.type, v.tokens, v.vocab = _TYPES[target.dtype], target.shape[0], target.shape[1]
+    if draft is not None:
+        v.draft, v.draft_stride = _matrix(draft, "draft", dev, (target.dtype,), target.shape[0], target.shape[1])
+    _dev(sample, torch.float32, "sample")
+    if sample.dim() != 1 or sample.device != dev:
+        raise ValueError("sample must be [sequences] on target's device")
+    v.batch, v.sample = sample.shape[0], sample.data_ptr()
+    for name, t, dtype, n in (("ids", ids, torch.int64, v.tokens), ("uniform", uniform, torch.float32, v.tokens), ("starts", starts, torch.int32, v.batch + 1)):
+        if t is None and name == "starts":
+            continue
+        _dev(t, dtype, name)
+        setattr(v, name, _given(t, dev, dtype, (n,), name).data_ptr())
+    return v
+
+
+def draft_verify_workspace(target, ids, uniform, sample, starts=None, draft=None):
+    """Bytes of scratch memory that draft_verify can use for these arguments."""
+    return int(lib().dq8_draft_verify_workspace_bytes(ctypes.byref(_draft(target, ids, uniform, sample, starts, draft))))
+
+
+def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None, accepted=None, rejected=None, workspace=None):
+    """Which drafted tokens stay, and the token behind them.
+
+    Rows starts[b] .. starts[b + 1] - 1 of a step (None: every sequence has as many) are a sequence's last accepted token and its drafts, ids int64
+    [tokens] what was fed there.  target [tokens, vocab] (float32, bfloat16 or float16): the target model's probabilities behind each row; draft, of the same
+    type: those that the token of the next row was drawn from (None: the draft was sure of it).  uniform float32 [tokens], sample float32
+    [sequences]: random numbers from 0 to 1; row i's token of row i + 1 stays while uniform[i] * draft < target.
+
+    Returns (out int64 [tokens]: accepted tokens, the one drawn behind them, -1; accepted int32 [sequences]; rejected int32 [sequences]: what
+    cache_plan takes back as ``drop``).  workspace: a uint8 tensor of draft_verify_workspace() bytes; None: taken from torch's allocator, and not while the
+    stream is captured into a graph (hand one in there: without it one workgroup reads a sequence's whole row)."""
+    done = _native.draft_verify(target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace)
+    if done is not None:
+        return done
+    v = _draft(target, ids, uniform, sample, starts, draft)
+    dev = target.device
+    out = _given(out, dev, torch.int64, (v.tokens,), "out")
+    accepted, rejected = _given(accepted, dev, torch.int32, (v.batch,), "accepted"), _given(rejected, dev, torch.int32, (v.batch,), "rejected")
+    v.out, v.accepted, v.rejected = out.data_ptr(), accepted.data_ptr(), rejected.data_ptr()
+    if workspace is None:
+        with torch.cuda.device(dev):
+            if not torch.cuda.is_current_stream_capturing():
+                workspace = torch.empty(int(lib().dq8_draft_verify_workspace_bytes(ctypes.byref(v))), dtype=torch.uint8, device=dev)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
+        if workspace.device != dev:
+            raise ValueError("workspace is on another device than target")
+    _enqueue(lib().dq8_draft_verify, target.get_device(), ctypes.byref(v), workspace.data_ptr() if workspace is not None and workspace.numel() else None,
+             0 if workspace is None else workspace.numel())
+    return out, accepted, rejected
 
 
 def model_speedup(n_gpus, total_ms, fc_ms, conv_penalty_ms, sub_batches, parallel_fc_ms, fc_penalty_ms):

@@ -1,0 +1,291 @@
+"""Weights in 4 bits and their products against plain implementations in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1511_04561_amd import dq8
+
+from . import serve_reference as ref
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.bfloat16, torch.float16]
+STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}  # half a step, relative
+
+
+def array(t):
+    return t.detach().cpu().double().numpy()
+
+
+def weights(rows, cols, seed):
+    rng = np.random.default_rng(seed)
+    w = (rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    w[rng.random(w.shape) < 0.02] = 0.0
+    return w
+
+
+def compressed(rows, cols, group, seed):
+    codes, scales = ref.encode(weights(rows, cols, seed), group)
+    return torch.from_numpy(codes).cuda(), torch.from_numpy(scales).to(torch.bfloat16).cuda(), ref.decode(codes, scales, rows, cols)
+
+
+def within(got, want, size, group, cols, dtype, bias=0.0):
+    """got against want: sums in binary32 of cols products of size `size` in all, one rounding to dtype.
+
+    A product is exact.  Each of the at most 128 additions in a group, of the additions of groups (one fused with the scale) and of the eight parts and the bias
+    is off by at most 2^-23 (whichever way the matrix unit rounds) of a sum of absolute values: (128 + cols / group + 10) 2^-23 size.  Results
+    below the type's normal numbers are off by half of its smallest one."""
+    tiny = {torch.float32: 2.0 ** -150, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}[dtype]
+    bound = (min(group, cols) + -(-cols // group) + 10) * 2.0 ** -23 * (size + np.abs(bias))
+    bound = bound + STEP[dtype] * (np.abs(want) + bound) + tiny
+    assert (np.abs(got - want) <= bound).all(), (np.abs(got - want) / bound).max()
+
+
+SHAPES = [(1, 1), (16, 128), (5, 31), (17, 129), (33, 1000), (100, 257), (64, 2048), (48, 136)]
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32] + DTYPES)
+def test_encode_and_decode(rows, cols, group, dtype):
+    w = torch.from_numpy(weights(rows, cols, rows + cols)).to(dtype)
+    codes, scales = ref.encode(w.float().numpy(), group)
+    c, s = dq8.weights_encode(w.cuda(), group)
+    assert np.array_equal(c.cpu().numpy(), codes) and np.array_equal(array(s), scales)
+    want = ref.decode(codes, scales, rows, cols)
+    for to in [torch.float32] + DTYPES:
+        got = dq8.weights_decode(c, s, rows, cols, dtype=to)
+        assert got.dtype == to and torch.equal(got.cpu(), torch.from_numpy(want).to(torch.float32).to(to))
+    # whole tiles: zeros behind the last row and column
+    whole = array(dq8.weights_decode(c, s))
+    assert np.array_equal(whole[:rows, :cols], want) and not whole[rows:].any() and not whole[:, cols:].any()
+
+
+def test_encode_on_and_next_to_every_border():
+    borders = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], np.float32)
+    w = np.zeros((16, 128), np.float32)
+    for r, scale in enumerate([1.0, 3.0, 2.0 ** -126, 2.0 ** -132, 1.5 * 2.0 ** -133, 170 * 2.0 ** 118, 2.0 ** 100, 255.0]):
+        for i, b in enumerate(borders):
+            at = np.float32(b * scale)
+            w[r, 4 * i : 4 * i + 3] = np.nextafter(at, np.float32(0)), at, -np.nextafter(at, np.float32(np.inf))
+        w[r, 31] = 6 * scale
+    codes, scales = ref.encode(w, 32)
+    c, s = dq8.weights_encode(torch.from_numpy(w).cuda(), 32)
+    assert np.array_equal(c.cpu().numpy(), codes) and np.array_equal(array(s), scales)
+
+
+def test_encode_extremes():
+    top = np.finfo(np.float32).max
+    w = np.zeros((16, 256), np.float32)
+    w[0, :5] = top, -top, top / 2, 1.0, -0.0
+    w[1, 3], w[1, 40], w[1, 70], w[1, 100] = np.inf, -np.inf, np.nan, 1.0
+    w[2, :] = -0.0
+    w[3, :3] = 1e-45, -1e-45, 5e-39
+    w[4, :2] = 6 * 2.0 ** -134, 6 * 2.0 ** -135  # the scale between zero and the smallest bfloat16 number
+    codes, scales = ref.encode(w, 32)
+    c, s = dq8.weights_encode(torch.from_numpy(w).cuda(), 32)
+    assert np.array_equal(c.cpu().numpy(), codes)
+    assert np.array_equal(array(s), scales, equal_nan=True)
+    got = array(dq8.weights_decode(c, s))
+    assert np.array_equal(got, ref.decode(codes, scales, 16, 256), equal_nan=True)
+    assert np.isnan(got[1, :96]).all() and np.isfinite(got[[0, 2, 3, 4]]).all() and np.array_equal(np.signbit(got[2]), np.ones(256, bool))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32] + DTYPES)
+def test_encode_and_decode_with_strides_and_guards(dtype):
+    rows, cols = 37, 203
+    big = torch.from_numpy(weights(rows + 2, cols + 14, 3)).to(dtype).cuda()
+    view = big[1 : rows + 1, 5 : 5 + cols]
+    c, s = dq8.weights_encode(view, 64)
+    c2, s2 = dq8.weights_encode(view.contiguous(), 64)
+    assert torch.equal(c, c2) and torch.equal(s, s2)
+    out = torch.full((rows + 2, cols + 9), 77.0, dtype=dtype, device="cuda")
+    got = dq8.weights_decode(c, s, rows, cols, dtype=dtype, out=out[1 : rows + 1, 3 : 3 + cols])
+    assert torch.equal(got, dq8.weights_decode(c, s, rows, cols, dtype=dtype))
+    assert (out[0] == 77).all() and (out[-1] == 77).all() and (out[:, :3] == 77).all() and (out[:, 3 + cols :] == 77).all()
+    # outputs handed in, inside guard bands
+    band = torch.full((c.numel() + 64,), 9, dtype=torch.uint8, device="cuda")
+    sband = torch.full((s.numel() + 32,), 9.0, dtype=torch.bfloat16, device="cuda")
+    dq8.weights_encode(view, 64, codes=band[32:-32].view(c.shape), scales=sband[16:-16].view(s.shape))
+    assert torch.equal(band[32:-32].view(c.shape), c) and torch.equal(sband[16:-16].view(s.shape), s)
+    assert (band[:32] == 9).all() and (band[-32:] == 9).all() and (sband[:16] == 9).all() and (sband[-16:] == 9).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5, 8, 13, 16, 17, 31, 32, 33, 48, 64, 65, 130])
+@pytest.mark.parametrize("rows,cols,group", [(16, 128, 32), (37, 300, 32), (130, 1025, 64), (200, 2048, 128), (5, 7, 64)])
+def test_products(tokens, rows, cols, group):
+    codes, scales, w = compressed(rows, cols, group, tokens)
+    rng = np.random.default_rng(rows)
+    bias = torch.from_numpy(rng.standard_normal(rows).astype(np.float32)).cuda()
+    for dtype in DTYPES:
+        x = torch.from_numpy(rng.standard_normal((tokens, cols)).astype(np.float32)).to(dtype).cuda()
+        want, size = array(x) @ w.T, np.abs(array(x)) @ np.abs(w).T
+        for to in (dtype, torch.float32):
+            got = dq8.weights_product(x, codes, scales, rows=rows, dtype=to)
+            assert got.dtype == to
+            within(array(got), want, size, group, cols, to)
+            got = dq8.weights_product(x, codes, scales, rows=rows, dtype=to, bias=bias)
+            within(array(got), want + array(bias), size, group, cols, to, array(bias))
+
+
+@pytest.mark.parametrize("rows,cols,group,tokens", [(4096, 4096, 32, 1), (8200, 1000, 64, 4), (1024, 14336, 128, 16), (20000, 640, 32, 9), (2048, 2048, 64, 300),
+                                                    (512, 28672, 32, 40), (12345, 999, 128, 64)])
+def test_large_products(rows, cols, group, tokens):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    w = torch.randn(rows, cols, generator=g, device="cuda") * cols ** -0.5
+    codes, scales = dq8.weights_encode(w, group)
+    w = dq8.weights_decode(codes, scales, rows, cols).double()
+    for dtype in DTYPES:
+        x = torch.randn(tokens, cols, generator=g, device="cuda").to(dtype)
+        want, size = x.double() @ w.T, x.double().abs() @ w.abs().T
+        for to in (dtype, torch.float32):
+            within(array(dq8.weights_product(x, codes, scales, rows=rows, dtype=to)), array(want), array(size), group, cols, to)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens", [1, 3, 20, 70])
+def test_products_with_strides_and_guards(dtype, tokens):
+    rows, cols, group = 53, 333, 32
+    codes, scales, w = compressed(rows, cols, group, 5)
+    big = torch.randn(tokens + 2, cols + 40, device="cuda").to(dtype)
+    big[:, :7] = float("nan")
+    big[:, 7 + cols :] = float("nan")  # what lies beside the rows is not read into them
+    big[0], big[-1] = float("nan"), float("nan")
+    x = big[1:-1, 7 : 7 + cols]
+    want, size = array(x) @ w.T, np.abs(array(x)) @ np.abs(w).T
+    for to in (dtype, torch.float32):
+        out = torch.full((tokens + 2, rows + 5), 7.0, dtype=to, device="cuda")
+        got = dq8.weights_product(x, codes, scales, rows=rows, out=out[1:-1, 3 : 3 + rows])
+        within(array(got), want, size, group, cols, to)
+        assert (out[0] == 7).all() and (out[-1] == 7).all() and (out[:, :3] == 7).all() and (out[:, 3 + rows :] == 7).all()
+    # every row the same one (a stride of zero), every second row
+    same = big[1:2, 7 : 7 + cols].expand(tokens, cols)
+    assert torch.equal(dq8.weights_product(same, codes, scales, rows=rows), dq8.weights_product(same.contiguous(), codes, scales, rows=rows))
+    half = torch.randn(2 * tokens, cols, device="cuda").to(dtype)[::2]
+    assert torch.equal(dq8.weights_product(half, codes, scales, rows=rows), dq8.weights_product(half.contiguous(), codes, scales, rows=rows))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_of_infinities_and_nan_stay_by_themselves(dtype):
+    rows, cols, tokens = 40, 200, 21
+    codes, scales, w = compressed(rows, cols, 32, 8)
+    x = torch.randn(tokens, cols, device="cuda").to(dtype)
+    clean = dq8.weights_product(x, codes, scales, rows=rows)
+    x[3, 5], x[17, 199] = float("nan"), float("inf")
+    got = dq8.weights_product(x, codes, scales, rows=rows)
+    others = [i for i in range(tokens) if i not in (3, 17)]
+    assert torch.equal(got[others], clean[others])
+    assert got[3].isnan().all() and not got[17].isfinite().any()
+    zero = torch.from_numpy(w[:, 199] == 0).cuda()
+    assert torch.equal(got[17].isnan(), zero)
+
+
+def test_products_of_the_largest_and_smallest_activations():
+    """A group's sum of products leaves binary32 for no bfloat16 activations whose result is finite."""
+    rows, cols = 16, 256
+    w = np.full((rows, cols), 6e-3, np.float32)
+    codes, scales = ref.encode(w, 128)
+    w = ref.decode(codes, scales, rows, cols)
+    c, s = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).to(torch.bfloat16).cuda()
+    for size in (2.0 ** 127, 2.0 ** 100, 2.0 ** -100, 2.0 ** -120):
+        x = torch.full((2, cols), size, dtype=torch.bfloat16, device="cuda")
+        x[1, ::2] *= -1
+        got = array(dq8.weights_product(x, c, s, dtype=torch.float32))
+        within(got, array(x) @ w.T, np.abs(array(x)) @ w.T, 128, cols, torch.float32)
+    # scales at the ends of their range
+    for scale in (170 * 2.0 ** 118, 2.0 ** -133):
+        s2 = torch.full(s.shape, scale, dtype=torch.float64).to(torch.bfloat16).cuda()
+        w2 = ref.decode(codes, array(s2), rows, cols)
+        x = torch.full((1, cols), 2.0 ** -9 if scale > 1 else 2.0 ** 100, dtype=torch.bfloat16, device="cuda")
+        x[:, ::2] *= -0.5
+        within(array(dq8.weights_product(x, c, s2, dtype=torch.float32)), array(x) @ w2.T, np.abs(array(x)) @ np.abs(w2).T, 128, cols, torch.float32)
+
+
+def test_a_group_of_nan_weights_is_one_row_s_nan():
+    w = weights(20, 256, 1)
+    w[7, 130] = np.inf
+    c, s = dq8.weights_encode(torch.from_numpy(w).cuda(), 64)
+    x = torch.randn(3, 256, device="cuda").bfloat16()
+    got = dq8.weights_product(x, c, s, rows=20)
+    assert got[:, 7].isnan().all() and got[:, [i for i in range(20) if i != 7]].isfinite().all()
+
+
+def test_parts_of_weights_are_weights():
+    """Tiles of rows by themselves: what one rank of several has of a layer."""
+    w = torch.randn(96, 512, device="cuda")
+    c, s = dq8.weights_encode(w, 32)
+    x = torch.randn(5, 512, device="cuda").half()
+    whole = dq8.weights_product(x, c, s)
+    parts = [dq8.weights_product(x, c[a:b], s[a:b]) for a, b in ((0, 2), (2, 3), (3, 6))]
+    assert torch.equal(torch.cat(parts, 1), whole)
+
+
+def test_products_on_another_stream_and_in_a_graph():
+    codes, scales, w = compressed(300, 700, 64, 2)
+    x = torch.randn(7, 700, device="cuda").bfloat16()
+    want = dq8.weights_product(x, codes, scales, rows=300)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = dq8.weights_product(x, codes, scales, rows=300)
+    side.synchronize()
+    assert torch.equal(got, want)
+    out, new, values = torch.empty_like(want), x.clone(), torch.empty(300, 700, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dq8.weights_product(new, codes, scales, rows=300, out=out)
+        dq8.weights_decode(codes, scales, 300, 700, out=values)
+    for seed in range(4):
+        new.copy_(torch.randn(7, 700, generator=torch.Generator().manual_seed(seed)).bfloat16())
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, dq8.weights_product(new, codes, scales, rows=300))
+        assert torch.equal(values, dq8.weights_decode(codes, scales, 300, 700))
+
+
+def test_the_python_path_gives_the_same(monkeypatch):
+    w = torch.randn(50, 400, device="cuda")
+    x = torch.randn(6, 400, device="cuda").half()
+    bias = torch.randn(50, device="cuda")
+
+    def calls():
+        c, s = dq8.weights_encode(w, 64)
+        return c, s, dq8.weights_decode(c, s, 50, 400, dtype=torch.float16), dq8.weights_product(x, c, s, rows=50, bias=bias, dtype=torch.float32)
+
+    want = calls()
+    monkeypatch.setattr(dq8, "_native", dq8._Unbound())
+    assert all(torch.equal(a, b) for a, b in zip(calls(), want))
+    # nothing to do
+    empty = dq8.weights_product(x[:0], want[0], want[1], rows=50)
+    assert empty.shape == (0, 50)
+
+
+def test_refusals():
+    w = torch.randn(40, 300, device="cuda")
+    c, s = dq8.weights_encode(w, 32)
+    x = torch.randn(2, 300, device="cuda").bfloat16()
+    bad = [
+        (ValueError, lambda: dq8.weights_encode(w, 48)),
+        (ValueError, lambda: dq8.weights_encode(w.T, 32)),
+        (TypeError, lambda: dq8.weights_encode(w.double(), 32)),
+        (ValueError, lambda: dq8.weights_encode(w, 64, scales=s)),
+        (ValueError, lambda: dq8.weights_encode(w, 32, codes=c[:2])),
+        (TypeError, lambda: dq8.weights_decode(c, s.float())),
+        (ValueError, lambda: dq8.weights_decode(c, s, rows=32)),
+        (ValueError, lambda: dq8.weights_decode(c, s, cols=385)),
+        (ValueError, lambda: dq8.weights_decode(c, s[:, :2])),
+        (TypeError, lambda: dq8.weights_decode(c, s, out=torch.empty(48, 384, dtype=torch.bfloat16, device="cuda"))),
+        (TypeError, lambda: dq8.weights_product(x.float(), c, s, rows=40)),
+        (ValueError, lambda: dq8.weights_product(x[:, :200], c, s, rows=40)),
+        (ValueError, lambda: dq8.weights_product(x, c, s, rows=49)),
+        (TypeError, lambda: dq8.weights_product(x, c, s, rows=40, dtype=torch.float16)),
+        (ValueError, lambda: dq8.weights_product(x, c, s, rows=40, bias=torch.zeros(48, device="cuda"))),
+        (TypeError, lambda: dq8.weights_product(x, c, s, rows=40, bias=torch.zeros(40, device="cuda").half())),
+        (ValueError, lambda: dq8.weights_product(x, c, s, rows=40, out=torch.empty(2, 48, device="cuda").bfloat16())),
+        (ValueError, lambda: dq8.weights_product(x[0], c, s, rows=40)),
+        (dq8.Dq8Error, lambda: dq8.weights_product(x, c, s, rows=40, out=x[:, :40])),
+        (dq8.Dq8Error, lambda: dq8.weights_product(x, c, s, rows=40, out=torch.empty(40, device="cuda").bfloat16().expand(2, 40))),
+    ]
+    for error, call in bad:
+        with pytest.raises(error):
+            call()
