@@ -55,6 +55,7 @@ struct Library {
     decltype(&dq8_weights_encode) weights_encode;
     decltype(&dq8_weights_decode) weights_decode;
     decltype(&dq8_weights_product) weights_product;
+    decltype(&dq8_weights_product_workspace_bytes) workspace_product;
     decltype(&dq8_cache_plan) cache_plan;
     decltype(&dq8_draft_verify) draft_verify;
     decltype(&dq8_draft_verify_workspace_bytes) workspace_verify;
@@ -823,7 +824,7 @@ PyObject *weights_decode(PyObject *const *a)  // codes, scales, rows, cols, dtyp
     return handed(a[5], made);
 }
 
-PyObject *weights_product(PyObject *const *a)  // x, codes, scales, rows, bias, dtype, out
+PyObject *weights_product(PyObject *const *a)  // x, codes, scales, rows, bias, dtype, out, workspace
 {
     Matrix x, out;
     Weights w;
@@ -845,7 +846,16 @@ PyObject *weights_product(PyObject *const *a)  // x, codes, scales, rows, bias, 
     if (a[4] != Py_None && !axis(a[4], at::kFloat, w.w.rows, *x.t, bias)) return declined();
     p.type = x.type, p.out_type = out.type, p.tokens = x.rows, p.x = x.ptr, p.x_stride = x.stride, p.out = out.ptr, p.out_stride = out.stride;
     p.bias = static_cast<const float *>(bias);
-    if (!enqueue("dq8_weights_product", [&] { return g_lib.weights_product(&w.w, &p, stream); })) return nullptr;
+    Scratch scratch;
+    if (a[7] == Py_None) {
+        if (!scratch.take(g_lib.workspace_product(&w.w, &p), *x.t, stream)) return declined();
+    } else {
+        Buffer space;
+        if (!buffer(a[7], at::kByte, space) || !x.beside(*space.t)) return declined();
+        scratch.ptr = space.n ? space.ptr : nullptr;
+        scratch.bytes = space.n;
+    }
+    if (!enqueue("dq8_weights_product", [&] { return g_lib.weights_product(&w.w, &p, scratch.ptr, scratch.bytes, stream); })) return nullptr;
     return handed(a[6], made);
 }
 
@@ -942,6 +952,7 @@ PyObject *bind(PyObject *, PyObject *args)
     take(l.weights_encode, "dq8_weights_encode");
     take(l.weights_decode, "dq8_weights_decode");
     take(l.weights_product, "dq8_weights_product");
+    take(l.workspace_product, "dq8_weights_product_workspace_bytes");
     take(l.cache_plan, "dq8_cache_plan");
     take(l.draft_verify, "dq8_draft_verify");
     take(l.workspace_verify, "dq8_draft_verify_workspace_bytes");
@@ -974,7 +985,7 @@ PyMethodDef g_methods[] = {
     method<cache_attention, 12>("cache_attention"),
     method<weights_encode, 4>("weights_encode"),
     method<weights_decode, 6>("weights_decode"),
-    method<weights_product, 7>("weights_product"),
+    method<weights_product, 8>("weights_product"),
     method<cache_plan, 14>("cache_plan"),
     method<draft_verify, 10>("draft_verify"),
     {nullptr, nullptr, 0, nullptr},

@@ -200,103 +200,332 @@ struct Operand<__bf16> {
     static __device__ __forceinline__ w4f product(type a, type b, w4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
-// A workgroup has R row tiles and 16 MT tokens; its wavefronts take every WAVES-th column tile and add up their sums in LDS at the end.
-// The products have tokens as rows and weight rows as columns, so that a lane's four sums share the scale of its weight row.
-template <typename T, int GROUP, int MT, int R, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void k_weights_product(ProductArgs a)
+// The scales of a weight row in a tile: PER neighbours.
+template <int PER>
+struct ScaleWord;
+template <>
+struct ScaleWord<1> {
+    typedef uint16_t type;
+};
+template <>
+struct ScaleWord<2> {
+    typedef uint32_t type;
+};
+template <>
+struct ScaleWord<4> {
+    typedef uint32_t type __attribute__((ext_vector_type(2)));
+};
+
+template <int PER>
+__device__ __forceinline__ float scale_at(typename ScaleWord<PER>::type v, int p)
+{
+    if constexpr (PER == 1) {
+        return bf16_value(v);
+    } else {
+        uint32_t w;
+        if constexpr (PER == 2)
+            w = v;
+        else
+            w = v[p / 2];
+        return __uint_as_float(p % 2 ? w & 0xFFFF0000u : w << 16);
+    }
+}
+
+// What a wavefront loads of R row tiles that lie `apart` tiles from each other.
+template <int GROUP, int R>
+struct TileWords {
+    static constexpr int PER = kTileCols / GROUP;
+    typedef typename ScaleWord<PER>::type Scale;
+    w4u word[R];
+    Scale scale[R];
+};
+
+// Where a wavefront's R row tiles begin; behind the last one they are the last one again.
+template <int GROUP, int R>
+struct TileSource {
+    static constexpr int PER = kTileCols / GROUP;
+    const uint8_t *codes[R];
+    const uint16_t *scales[R];
+
+    __device__ __forceinline__ TileSource(const ProductArgs &a, uint32_t row_tile)
+    {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const size_t tile = (size_t)(row_tile + r < a.row_tiles ? row_tile + r : a.row_tiles - 1) * a.col_tiles;
+            codes[r] = a.codes + tile * kTileBytes;
+            scales[r] = a.scales + tile * kTileRows * PER;
+        }
+    }
+
+    // Weights are read once: past the caches.
+    __device__ __forceinline__ void fetch(uint32_t col_tile, uint32_t lane, TileWords<GROUP, R> &t) const
+    {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            t.word[r] = __builtin_nontemporal_load(reinterpret_cast<const w4u *>(codes[r] + (size_t)col_tile * kTileBytes) + lane);
+            t.scale[r] = reinterpret_cast<const typename ScaleWord<PER>::type *>(scales[r] + (size_t)col_tile * kTileRows * PER)[lane & 15];
+        }
+    }
+};
+
+// A tile's products: x points at the lane's 16 bytes of its row of activations in LDS, 64 bytes from one step to the next and TOKENS_APART bytes
+// from one token tile to the next.  Products have tokens as rows and weight rows as columns, so that a lane's sums share the scale of its weight
+// row.  A lane has four of the 16 tokens of a token tile; with Q = 2 or 1 every token is there 2 or 4 times, and only one of them is scaled
+// and added up (16 multiply-adds of a tile with groups of 32 become 4: a third of the vector instructions).
+template <typename T, int GROUP, int MT, int Q, int R, int TOKENS_APART>
+__device__ __forceinline__ void add_tile(const char *x, const TileWords<GROUP, R> &t, float (&sum)[MT][R][Q])
 {
     constexpr int PER = kTileCols / GROUP, RUNS = 4 / PER;
     typedef Operand<T> Op;
     typedef typename Op::type V;
-    typedef V VA __attribute__((aligned(sizeof(T))));
-    __shared__ w4f parts[WAVES][MT * R][64];
-    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-    const uint32_t rt = blockIdx.x * R, first = blockIdx.y * 16 * MT;
-    w4f sum[MT][R];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int r = 0; r < R; ++r) sum[m][r] = w4f{0, 0, 0, 0};
-    const T *row[MT];
-    bool in[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const uint32_t token = first + 16 * m + n;
-        in[m] = token < a.tokens;
-        row[m] = static_cast<const T *>(a.x) + (in[m] ? token : 0) * a.x_stride;
-    }
-    for (uint32_t ct = wave; ct < a.col_tiles; ct += WAVES) {
-        w4u word[R];
-        uint32_t scale[R][PER];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const size_t tile = (size_t)(rt + r < a.row_tiles ? rt + r : rt) * a.col_tiles + ct;
-            word[r] = *reinterpret_cast<const w4u *>(a.codes + tile * kTileBytes + lane * 16);
-#pragma unroll
-            for (int p = 0; p < PER; ++p) scale[r][p] = a.scales[(tile * kTileRows + n) * PER + p];
-        }
-        V x[MT][4];
+    for (int p = 0; p < PER; ++p) {
+        V v[MT][RUNS];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const uint32_t k = ct * kTileCols + 32 * s + 8 * g;
-                x[m][s] = V{};
-                if (in[m]) {
-                    if (k + 8 <= a.cols) {
-                        x[m][s] = *reinterpret_cast<const VA *>(row[m] + k);
-                    } else {
+            for (int k = 0; k < RUNS; ++k) v[m][k] = *reinterpret_cast<const V *>(x + m * TOKENS_APART + (p * RUNS + k) * 64);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (k + e < a.cols) x[m][s][e] = row[m][k + e];
-                    }
-                }
+        for (int r = 0; r < R; ++r) {
+            w4f d[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) d[m] = w4f{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < RUNS; ++k) {
+                const V w = Op::weights(t.word[r][p * RUNS + k]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) d[m] = Op::product(v[m][k], w, d[m]);
             }
+            const float f = scale_at<PER>(t.scale[r], p);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int p = 0; p < PER; ++p) {
-                w4f d[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) d[m] = w4f{0, 0, 0, 0};
-#pragma unroll
-                for (int s = p * RUNS; s < (p + 1) * RUNS; ++s) {
-                    const V v = Op::weights(word[r][s]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) d[m] = Op::product(x[m][s], v, d[m]);
-                }
-                const float f = bf16_value(scale[r][p]);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[m][r][i] = __builtin_fmaf(d[m][i], f, sum[m][r][i]);
-            }
+                for (int q = 0; q < Q; ++q) sum[m][r][q] = __builtin_fmaf(d[m][q * (4 / Q)], f, sum[m][r][q]);
+        }
     }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_result(const ProductArgs &a, uint32_t token, uint32_t row, float v)
+{
+    v *= Operand<T>::kLift;
+    if (a.bias) v += a.bias[row];
+    const size_t at = token * a.out_stride + row;
+    if (a.wide)
+        static_cast<float *>(a.out)[at] = v;
+    else
+        static_cast<T *>(a.out)[at] = (T)v;
+}
+
+// Sums of KW wavefronts that have the same rows, added up in LDS in their order and handed to `store` (token tile, row tile, sum of the lane, value).
+template <int MT, int R, int Q, int KW, typename F>
+__device__ __forceinline__ void join_sums(float *parts, uint32_t wave, uint32_t lane, const float (&sum)[MT][R][Q], F store)
+{
+    constexpr int CELLS = MT * R * Q;
+    if constexpr (KW == 1) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) store(m, r, q, sum[m][r][q]);
+    } else {
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) parts[(wave * CELLS + (m * R + r) * Q + q) * 64 + lane] = sum[m][r][q];
+        __syncthreads();
+        const uint32_t kw = wave % KW;
+        for (uint32_t cell = kw; cell < CELLS; cell += KW) {
+            const float *p = parts + ((wave - kw) * CELLS + cell) * 64 + lane;
+            float v = *p;
+#pragma unroll
+            for (int o = 1; o < KW; ++o) v += p[o * CELLS * 64];
+            store(cell / Q / R, cell / Q % R, cell % Q, v);
+        }
+    }
+}
+
+// Eight activations of a row from column k on, zeros behind the last one.
+template <typename T>
+__device__ __forceinline__ w4u eight_columns(const T *row, size_t k, uint32_t cols)
+{
+    typedef w4u WA __attribute__((aligned(2)));
+    if (k + 8 <= cols) return *reinterpret_cast<const WA *>(row + k);
+    typename Operand<T>::type v = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (k + e < cols) v[e] = row[k + e];
+    w4u w;
+    __builtin_memcpy(&w, &v, 16);
+    return w;
+}
+
+constexpr uint32_t kRowPad = 16;  // bytes between the rows of activations in LDS, so that 16 rows' pieces lie in different banks
+
+// Up to 4 Q tokens whose rows fit LDS: staged once, and no wavefront waits for another until the end.  A workgroup has a row tile, its
+// wavefronts every KW-th column tile of it, D of them in flight.
+// 28672 x 8192 weights, group 128, one token: 19.8 us, 6.1 TB/s, what loads alone reach; 4096 x 4096, group 32: 4.0 us (kernel start and end, three round trips
+// to memory).  With activations staged in pieces, as below, 21.5 and 4.8.
+template <typename T, int GROUP, int Q, int KW, int D>
+__global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs a)
+{
+    constexpr uint32_t WG = KW * 64;
+    extern __shared__ __align__(16) char lds[];
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t stride = a.col_tiles * 2 * kTileCols + kRowPad;
+    const TileSource<GROUP, 1> source(a, blockIdx.x);
+    auto inside = [&](uint32_t ct) { return ct < a.col_tiles ? ct : a.col_tiles - 1; };
+    TileWords<GROUP, 1> t[D];
+    const uint32_t per = a.col_tiles * (kTileCols / 8), pieces = a.tokens * per;
+    auto load = [&](uint32_t i) { return eight_columns(static_cast<const T *>(a.x) + (i / per) * a.x_stride, (size_t)(i % per) * 8, a.cols); };
+    auto place = [&](uint32_t i, w4u v) { *reinterpret_cast<w4u *>(lds + i / per * stride + i % per * 16) = v; };
+    uint32_t i = threadIdx.x;
+    w4u one = {0, 0, 0, 0};
+    if (i < pieces) one = load(i);
+#pragma unroll
+    for (int d = 0; d < D; ++d) source.fetch(inside(wave + d * KW), lane, t[d]);
+    if (i < pieces) place(i, one);
+    for (i += WG; i < pieces; i += WG) place(i, load(i));
+    float sum[1][1][Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) sum[0][0][q] = 0.0f;
+    uint32_t token = n / (4 / Q);
+    token = token < a.tokens ? token : a.tokens - 1;
+    const char *x = lds + token * stride + g * 16;
+    __syncthreads();
+    for (uint32_t ct = wave; ct < a.col_tiles; ct += D * KW) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const uint32_t now = ct + d * KW;
+            if (now < a.col_tiles) add_tile<T, GROUP, 1, Q, 1, 0>(x + now * 2 * kTileCols, t[d], sum);
+            source.fetch(inside(now + D * KW), lane, t[d]);  // (without a condition: a branch around loads makes the waits for others wait for all)
+        }
+    }
+    join_sums<1, 1, Q, KW>(reinterpret_cast<float *>(lds), wave, lane, sum, [&](uint32_t, uint32_t, uint32_t q, float v) {
+        const uint32_t to = blockIdx.x * kTileRows + n, m = g * Q + q;
+        if (to < a.rows && m < a.tokens) store_result<T>(a, m, to, v);
+    });
+}
+
+// Any number of tokens, 4 Q MT of them in a workgroup (grid y), RW R row tiles; the column tiles are cut into chunks of KW, a wavefront has one tile of a chunk
+// of R row tiles.  A chunk of the activations is staged in LDS for all wavefronts, one ahead of its use, and D more chunks of activations and
+// weights are on their way to registers: both by the same distance, for loads are waited for in the order of their issue.  What a
+// compute unit gets from L2 is about 25 bytes a cycle, of HBM's weights 12: with few row tiles in a workgroup, activations cost more than weights.
+// With `parts` (workspace) the chunks are divided over the workgroups of grid z as well, and k_weights_join adds up their sums.
+struct SplitArgs {
+    float *parts;  // [splits][tokens][rows]
+    uint32_t splits;
+};
+
+template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC>
+__global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductArgs a, SplitArgs split)
+{
+    constexpr uint32_t WG = RW * KW * 64, TOKENS = 4 * Q * MT, COLS = KW * kTileCols, BYTES = 2 * COLS, STRIDE = BYTES + kRowPad;
+    constexpr uint32_t PIECES = TOKENS * BYTES / 16, MINE = (PIECES + WG - 1) / WG;
+    constexpr uint32_t STAGED = 2 * TOKENS * STRIDE, JOINED = KW > 1 ? RW * KW * MT * R * Q * 256 : 0;
+    __shared__ __align__(16) char lds[STAGED > JOINED ? STAGED : JOINED];
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t kw = wave % KW, row_tile = (blockIdx.x * RW + wave / KW) * R, first = blockIdx.y * TOKENS;
+    // this workgroup's whole chunks; the last one has the columns behind them too
+    const uint32_t whole = a.cols / COLS, c0 = (uint32_t)((uint64_t)whole * blockIdx.z / split.splits), c1 = (uint32_t)((uint64_t)whole * (blockIdx.z + 1) / split.splits);
+    const bool rest = whole * COLS < a.cols && blockIdx.z == split.splits - 1;
+    const TileSource<GROUP, R> source(a, row_tile);
+    float sum[MT][R][Q];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int r = 0; r < R; ++r) parts[wave][m * R + r][lane] = sum[m][r];
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < MT * R * 64; i += WAVES * 64) {
-        const uint32_t cell = i >> 6, m = cell / R, r = cell % R;
-        w4f v = parts[0][cell][lane];
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int o = 1; o < WAVES; ++o) v += parts[o][cell][lane];
-        v *= Op::kLift;
-        const uint32_t to = (rt + r) * kTileRows + n;
-        if (to >= a.rows) continue;
-        if (a.bias) v += a.bias[to];
+            for (int q = 0; q < Q; ++q) sum[m][r][q] = 0.0f;
+    // a thread's pieces of a chunk: 16 bytes of a token (behind the last one: of the last one again; nobody looks at its results)
+    const T *from[MINE];
+    uint32_t to[MINE];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t token = first + 16 * m + 4 * g + e;
-            if (token >= a.tokens) break;
-            const size_t at = token * a.out_stride + to;
-            if (a.wide)
-                static_cast<float *>(a.out)[at] = v[e];
-            else
-                static_cast<T *>(a.out)[at] = (T)v[e];
+    for (uint32_t i = 0; i < MINE; ++i) {
+        const uint32_t at = threadIdx.x + i * WG, m = at / (BYTES / 16) % TOKENS, c = at % (BYTES / 16), token = first + m < a.tokens ? first + m : a.tokens - 1;
+        from[i] = static_cast<const T *>(a.x) + token * a.x_stride + c * 8;
+        to[i] = m * STRIDE + c * 16;
+    }
+    struct Pieces {
+        w4u v[MINE];
+    };
+    auto fetch_x = [&](uint32_t chunk, Pieces &p) {
+        typedef w4u WA __attribute__((aligned(2)));
+#pragma unroll
+        for (uint32_t i = 0; i < MINE; ++i) p.v[i] = *reinterpret_cast<const WA *>(from[i] + (size_t)chunk * COLS);
+    };
+    auto place_x = [&](uint32_t buffer, const Pieces &p) {
+#pragma unroll
+        for (uint32_t i = 0; i < MINE; ++i)
+            if (PIECES % WG == 0 || threadIdx.x + i * WG < PIECES) *reinterpret_cast<w4u *>(lds + buffer * TOKENS * STRIDE + to[i]) = p.v[i];
+    };
+    const uint32_t x = n / (4 / Q) * STRIDE + kw * 2 * kTileCols + g * 16;
+    auto work = [&](const TileWords<GROUP, R> &t, uint32_t buffer) { add_tile<T, GROUP, MT, Q, R, 4 * Q * STRIDE>(lds + buffer * TOKENS * STRIDE + x, t, sum); };
+
+    TileWords<GROUP, R> t_rest = {};
+    Pieces x_rest = {};
+    if (rest) {
+        if (whole * KW + kw < a.col_tiles) source.fetch(whole * KW + kw, lane, t_rest);
+#pragma unroll
+        for (uint32_t i = 0; i < MINE; ++i) {
+            const uint32_t c = (threadIdx.x + i * WG) % (BYTES / 16) * 8;
+            x_rest.v[i] = eight_columns(from[i] - c, (size_t)whole * COLS + c, a.cols);
         }
     }
+    if (c1 > c0) {
+        auto inside = [&](uint32_t c) { return c < c1 ? c : c1 - 1; };
+        TileWords<GROUP, R> t[D];
+        Pieces p[D];
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            fetch_x(inside(c0 + d), p[d]);
+            source.fetch(inside(c0 + d) * KW + kw, lane, t[d]);
+        }
+        place_x(0, p[0]);
+        fetch_x(inside(c0 + D), p[0]);
+        static_assert(D % 2 == 0, "the two buffers in turn");
+        for (uint32_t c = c0; c < c1; c += D) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                __syncthreads();  // chunk c + d is there, and nobody reads the one before any more
+                place_x((d & 1) ^ 1, p[(d + 1) % D]);
+                fetch_x(inside(c + d + 1 + D), p[(d + 1) % D]);
+                if (c + d < c1) work(t[d], d & 1);
+                source.fetch(inside(c + d + D) * KW + kw, lane, t[d]);
+            }
+        }
+    }
+    if (rest) {
+        __syncthreads();
+        place_x(0, x_rest);
+        __syncthreads();
+        if (whole * KW + kw < a.col_tiles) work(t_rest, 0);
+    }
+    join_sums<MT, R, Q, KW>(reinterpret_cast<float *>(lds), wave, lane, sum, [&](uint32_t m, uint32_t r, uint32_t q, float v) {
+        const uint32_t token = first + m * (4 * Q) + g * Q + q, row = (row_tile + r) * kTileRows + n;
+        if (row >= a.rows || token >= a.tokens) return;
+        if (split.splits > 1)
+            split.parts[((size_t)blockIdx.z * a.tokens + token) * a.rows + row] = v;
+        else
+            store_result<T>(a, token, row, v);
+    });
+}
+
+// The sums of the workgroups that share a chunk range, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_weights_join(ProductArgs a, SplitArgs split)
+{
+    const uint32_t row = blockIdx.x * 256 + threadIdx.x, token = blockIdx.y;
+    if (row >= a.rows) return;
+    const float *p = split.parts + (size_t)token * a.rows + row;
+    float v = *p;
+#pragma unroll 4
+    for (uint32_t z = 1; z < split.splits; ++z) v += p[(size_t)z * a.tokens * a.rows];
+    store_result<T>(a, token, row, v);
 }
 
 }  // namespace

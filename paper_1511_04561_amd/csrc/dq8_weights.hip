@@ -86,26 +86,113 @@ int decode(const dq8_weights &o, void *w, size_t stride, hipStream_t stream)
     return o.group == 32 ? decode<T, 32>(o, w, stride, stream) : o.group == 64 ? decode<T, 64>(o, w, stride, stream) : decode<T, 128>(o, w, stride, stream);
 }
 
-template <typename T, int GROUP, int MT, int R>
-int product(const ProductArgs &k, hipStream_t stream)
+// What a product launches.
+enum Form {
+    kFew4, kFew8,      // rows of activations staged whole, up to 4 or 8 tokens; a wavefront has every eighth column tile, ...
+    kFew4Tall,         // ... every fourth where there are many row tiles
+    kOne4, kOne8,      // staged in chunks, up to 4, 8 or ...
+    kOne16,            // ... 16 tokens: one row tile per workgroup, eight wavefronts along the columns,
+    kOne16Wide,        // two row tiles,
+    kOne16Tall,        // four
+    kTwo, kTwoTall,    // up to 32 tokens
+    kFour, kFourTall   // 64 tokens a workgroup
+};
+
+struct Shape {
+    Form form;
+    unsigned row_tiles, tokens;  // of a workgroup
+    unsigned columns;            // of a chunk
+    unsigned splits;             // workgroups along the columns, where there is workspace for their sums
+};
+
+constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
+
+Shape shape_of(const dq8_weights &w, size_t tokens, int cus)
 {
-    constexpr int WAVES = 8;
-    hipLaunchKernelGGL((k_weights_product<T, GROUP, MT, R, WAVES>), dim3((k.row_tiles + R - 1) / R, (k.tokens + 16 * MT - 1) / (16 * MT)), dim3(WAVES * 64), 0, stream, k);
-    return dq8::after_launch_of("k_weights_product", stream);
+    const Tiles t = tiles_of(w);
+    const size_t few = tokens * (t.cols * 2 * kTileCols + kRowPad);
+    Shape s = {kFour, 8, 64, 128, 1};
+    if (tokens <= 8 && few <= kFewBytes)
+        s = tokens > 4 ? Shape{kFew8, 1, 8, 0, 1} : t.rows > 4 * (size_t)cus ? Shape{kFew4Tall, 1, 4, 0, 1} : Shape{kFew4, 1, 4, 0, 1};
+    else if (tokens <= 4)
+        s = Shape{kOne4, 2, 4, 512, 1};
+    else if (tokens <= 8)
+        s = Shape{kOne8, 2, 8, 512, 1};
+    else if (tokens <= 16)
+        s = t.rows >= 8 * (size_t)cus ? Shape{kOne16Tall, 4, 16, 128, 1} : t.rows > (size_t)cus ? Shape{kOne16Wide, 2, 16, 512, 1} : Shape{kOne16, 1, 16, 1024, 1};
+    else if (tokens <= 32)
+        s = t.rows >= 4 * (size_t)cus ? Shape{kTwoTall, 4, 32, 256, 1} : Shape{kTwo, 4, 32, 512, 1};
+    else if ((t.rows + 15) / 16 * ((tokens + 63) / 64) >= (size_t)cus)
+        s = Shape{kFourTall, 16, 64, 128, 1};
+    if (s.form == kTwo || s.form == kFour) {
+        const size_t groups = (t.rows + s.row_tiles - 1) / s.row_tiles * ((tokens + s.tokens - 1) / s.tokens), chunks = w.cols / s.columns;
+        size_t splits = (size_t)cus / groups;
+        if (splits > chunks / 4) splits = chunks / 4;
+        s.splits = splits < 2 ? 1 : (unsigned)splits;
+    }
+    return s;
+}
+
+size_t workspace_of(const dq8_weights &w, size_t tokens, const Shape &s) { return s.splits > 1 ? s.splits * tokens * w.rows * sizeof(float) : 0; }
+
+template <typename T, int GROUP, int Q, int KW, int D>
+int few(const ProductArgs &k, hipStream_t stream)
+{
+    const size_t x = k.tokens * ((size_t)k.col_tiles * 2 * kTileCols + kRowPad), sums = KW * Q * 256;
+    hipLaunchKernelGGL((k_weights_product_few<T, GROUP, Q, KW, D>), dim3(k.row_tiles), dim3(KW * 64), x > sums ? x : sums, stream, k);
+    return dq8::after_launch_of("k_weights_product_few", stream);
+}
+
+template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC>
+int chunks(const ProductArgs &k, const SplitArgs &split, hipStream_t stream)
+{
+    constexpr uint32_t TOKENS = 4 * Q * MT;
+    hipLaunchKernelGGL((k_weights_product<T, GROUP, MT, Q, R, RW, KW, D, OCC>), dim3((k.row_tiles + R * RW - 1) / (R * RW), (k.tokens + TOKENS - 1) / TOKENS, split.splits),
+                       dim3(RW * KW * 64), 0, stream, k, split);
+    const int rc = dq8::after_launch_of("k_weights_product", stream);
+    if (rc || split.splits == 1) return rc;
+    hipLaunchKernelGGL(k_weights_join<T>, dim3((k.rows + 255) / 256, k.tokens), dim3(256), 0, stream, k, split);
+    return dq8::after_launch_of("k_weights_join", stream);
 }
 
 template <typename T, int GROUP>
-int product(const ProductArgs &k, hipStream_t stream)
+int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t stream)
 {
-    if (k.tokens <= 16) return product<T, GROUP, 1, 1>(k, stream);
-    if (k.tokens <= 32) return product<T, GROUP, 2, 1>(k, stream);
-    return product<T, GROUP, 4, 2>(k, stream);
+    switch (form) {
+    case kFew4: return few<T, GROUP, 1, 8, 4>(k, stream);
+    case kFew8: return few<T, GROUP, 2, 8, 2>(k, stream);
+    case kFew4Tall: return few<T, GROUP, 1, 4, 4>(k, stream);
+    case kOne4: return chunks<T, GROUP, 1, 1, 1, 2, 4, 4, 4>(k, split, stream);
+    case kOne8: return chunks<T, GROUP, 1, 2, 1, 2, 4, 4, 4>(k, split, stream);
+    case kOne16: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, split, stream);
+    case kOne16Wide: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
+    case kOne16Tall: return chunks<T, GROUP, 1, 4, 1, 4, 1, 4, 4>(k, split, stream);
+    case kTwo: return chunks<T, GROUP, 2, 4, 2, 2, 4, 2, 2>(k, split, stream);
+    case kTwoTall: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
+    case kFour: return chunks<T, GROUP, 4, 4, 2, 4, 1, 2, 2>(k, split, stream);
+    case kFourTall: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 2>(k, split, stream);
+    }
+    return DQ8_OK;
 }
 
 template <typename T>
-int product(int group, const ProductArgs &k, hipStream_t stream)
+int product(int group, const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t stream)
 {
-    return group == 32 ? product<T, 32>(k, stream) : group == 64 ? product<T, 64>(k, stream) : product<T, 128>(k, stream);
+    return group == 32 ? product<T, 32>(k, form, split, stream) : group == 64 ? product<T, 64>(k, form, split, stream) : product<T, 128>(k, form, split, stream);
+}
+
+// What looks at sizes and types.  No tokens or rows pass: such a call launches nothing.
+int check_product(const char *who, const dq8_weights *w, const dq8_product *in)
+{
+    const int rc = check_weights(who, w);
+    if (rc) return rc;
+    if (!in) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);
+    const dq8_product &p = *in;
+    if (p.type != DQ8_BFLOAT16 && p.type != DQ8_FLOAT16) return failed(DQ8_ERR_ARG, "%s: type %d is neither bfloat16 nor float16", who, p.type);
+    if (p.out_type != p.type && p.out_type != DQ8_FLOAT32) return failed(DQ8_ERR_ARG, "%s: out_type %d is neither type nor float32", who, p.out_type);
+    if (p.tokens > DQ8_WEIGHTS_MAX_TOKENS) return failed(DQ8_ERR_ARG, "%s: %zu tokens", who, p.tokens);
+    if (w->rows && p.tokens && w->cols == 0) return failed(DQ8_ERR_ARG, "%s: weights without columns", who);
+    return DQ8_OK;
 }
 
 }  // namespace
@@ -138,32 +225,46 @@ int dq8_weights_decode(const dq8_weights *in, int type, void *w, size_t row_stri
     return type == DQ8_BFLOAT16 ? decode<__bf16>(*in, w, row_stride, stream) : decode<_Float16>(*in, w, row_stride, stream);
 }
 
-int dq8_weights_product(const dq8_weights *w, const dq8_product *in, void *hip_stream)
+size_t dq8_weights_product_workspace_bytes(const dq8_weights *w, const dq8_product *p)
+{
+    if (check_product("dq8_weights_product_workspace_bytes", w, p) || w->rows == 0 || p->tokens <= 16) return 0;
+    dq8::DeviceTables dev;
+    if (dq8::device_tables(0, &dev)) return 0;
+    return workspace_of(*w, p->tokens, shape_of(*w, p->tokens, dev.cus));
+}
+
+int dq8_weights_product(const dq8_weights *w, const dq8_product *in, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     static const char who[] = "dq8_weights_product";
-    int rc = check_weights(who, w);
+    int rc = check_product(who, w, in);
     if (rc) return rc;
-    if (!in) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);
     const dq8_product &p = *in;
-    if (p.type != DQ8_BFLOAT16 && p.type != DQ8_FLOAT16) return failed(DQ8_ERR_ARG, "%s: type %d is neither bfloat16 nor float16", who, p.type);
-    if (p.out_type != p.type && p.out_type != DQ8_FLOAT32) return failed(DQ8_ERR_ARG, "%s: out_type %d is neither type nor float32", who, p.out_type);
-    if (p.tokens > DQ8_WEIGHTS_MAX_TOKENS) return failed(DQ8_ERR_ARG, "%s: %zu tokens", who, p.tokens);
     if (w->rows == 0 || p.tokens == 0) return DQ8_OK;
-    if (w->cols == 0) return failed(DQ8_ERR_ARG, "%s: weights without columns", who);
     rc = check_matrix(who, "x", *w, p.type, p.x, p.tokens, w->cols, p.x_stride, false);
     if (!rc) rc = check_matrix(who, "out", *w, p.out_type, p.out, p.tokens, w->rows, p.out_stride, true);
     if (rc) return rc;
-    if (((uintptr_t)p.bias & 3) != 0) return failed(DQ8_ERR_ARG, "%s: bias does not start at a multiple of 4 bytes", who);
+    if (((uintptr_t)p.bias & 3) != 0 || ((uintptr_t)workspace & 15) != 0)
+        return failed(DQ8_ERR_ARG, "%s: bias does not start at a multiple of 4 bytes or workspace of 16", who);
     const size_t n_out = ((p.tokens - 1) * p.out_stride + w->rows) * size_of(p.out_type), n_x = ((p.tokens - 1) * p.x_stride + w->cols) * 2;
-    if (dq8::meet(p.out, n_out, p.x, n_x) || (p.bias && dq8::meet(p.out, n_out, p.bias, w->rows * 4))) return failed(DQ8_ERR_ARG, "%s: out overlaps x or bias", who);
+    const size_t n_bias = p.bias ? w->rows * 4 : 0, n_work = workspace ? workspace_bytes : 0;
+    using dq8::meet;
+    if (meet(p.out, n_out, p.x, n_x) || meet(p.out, n_out, p.bias, n_bias) || meet(p.out, n_out, workspace, n_work) || meet(workspace, n_work, p.x, n_x) ||
+        meet(workspace, n_work, p.bias, n_bias) || meet(workspace, n_work, w->codes, code_bytes(*w)) || meet(workspace, n_work, w->scales, scale_bytes(*w)))
+        return failed(DQ8_ERR_ARG, "%s: out or workspace overlaps another array", who);
+    dq8::DeviceTables dev;
+    rc = dq8::device_tables(0, &dev);
+    if (rc) return rc;
     const Tiles t = tiles_of(*w);
     ProductArgs k;
     k.codes = w->codes, k.scales = static_cast<const uint16_t *>(w->scales), k.x = p.x, k.out = p.out, k.bias = p.bias;
     k.x_stride = p.x_stride, k.out_stride = p.out_stride;
     k.tokens = (uint32_t)p.tokens, k.rows = (uint32_t)w->rows, k.cols = (uint32_t)w->cols, k.row_tiles = (uint32_t)t.rows, k.col_tiles = (uint32_t)t.cols;
     k.wide = p.out_type == DQ8_FLOAT32;
+    const Shape s = shape_of(*w, p.tokens, dev.cus);
+    const bool some = s.splits > 1 && workspace && workspace_bytes >= workspace_of(*w, p.tokens, s);
+    const SplitArgs split = {some ? static_cast<float *>(workspace) : nullptr, some ? s.splits : 1};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return p.type == DQ8_BFLOAT16 ? product<__bf16>(w->group, k, stream) : product<_Float16>(w->group, k, stream);
+    return p.type == DQ8_BFLOAT16 ? product<__bf16>(w->group, k, s.form, split, stream) : product<_Float16>(w->group, k, s.form, split, stream);
 }
 
 }  // extern "C"

@@ -116,7 +116,9 @@ def lib():
         L.dq8_cache_attention_workspace_bytes.restype = sz
         L.dq8_weights_encode.argtypes = [ci, vp, sz, ctypes.POINTER(_Weights), vp]
         L.dq8_weights_decode.argtypes = [ctypes.POINTER(_Weights), ci, vp, sz, vp]
-        L.dq8_weights_product.argtypes = [ctypes.POINTER(_Weights), ctypes.POINTER(_Product), vp]
+        L.dq8_weights_product.argtypes = [ctypes.POINTER(_Weights), ctypes.POINTER(_Product), vp, sz, vp]
+        L.dq8_weights_product_workspace_bytes.argtypes = [ctypes.POINTER(_Weights), ctypes.POINTER(_Product)]
+        L.dq8_weights_product_workspace_bytes.restype = sz
         L.dq8_cache_plan.argtypes = [ctypes.POINTER(_Plan), vp]
         L.dq8_draft_verify.argtypes = [ctypes.POINTER(_Verify), vp, sz, vp]
         L.dq8_draft_verify_workspace_bytes.argtypes = [ctypes.POINTER(_Verify)]
@@ -143,7 +145,8 @@ _BOUND = ("dq8_absmax", "dq8_encode_ws", "dq8_workspace_bytes", "dq8_decode", "d
           "dq8_workspace_bytes_segments", "dq8_decode_segments",
           "dq8_decode_accumulate_avg", "dq8_decode_accumulate_avg_local", "dq8_decode_accumulate_avg_segments",
           "dq8_decode_avg_encode", "dq8_error_stats_ws", "dq8_workspace_bytes_stats", "dq8_cache_append", "dq8_cache_attention",
-          "dq8_cache_attention_workspace_bytes", "dq8_weights_encode", "dq8_weights_decode", "dq8_weights_product", "dq8_cache_plan",
+          "dq8_cache_attention_workspace_bytes", "dq8_weights_encode", "dq8_weights_decode", "dq8_weights_product", "dq8_weights_product_workspace_bytes",
+          "dq8_cache_plan",
           "dq8_draft_verify", "dq8_draft_verify_workspace_bytes", "dq8_last_error")
 
 
@@ -693,33 +696,55 @@ def weights_decode(codes, scales, rows=None, cols=None, dtype=torch.float32, out
     return out
 
 
-def weights_product(x, codes, scales, rows=None, bias=None, dtype=None, out=None):
-    """x [tokens, cols] (bfloat16 or float16) times compressed weights, out[m, n] = sum_k x[m, k] w[n, k] (+ bias[n], float32).
-
-    rows: of the weights, where these do not fill their last tile.  dtype: of the result, x's or float32.  For serving: as with every call
-    here no gradient passes through it."""
-    done = _native.weights_product(x, codes, scales, rows, bias, dtype, out)
-    if done is not None:
-        return done
-    at, stride = _matrix(x, "x", None, (torch.bfloat16, torch.float16), None, None)
+def _product(x, codes, scales, rows, dtype):
+    p = _Product()
+    p.x, p.x_stride = _matrix(x, "x", None, (torch.bfloat16, torch.float16), None, None)
     c = _weights(codes, scales, rows, x.shape[1])
     if codes.device != x.device:
         raise ValueError("x is on another device than codes")
-    if dtype is None:
-        dtype = x.dtype if out is None else out.dtype
     if dtype not in (x.dtype, torch.float32):
         raise TypeError("dtype must be %s or torch.float32, got %s" % (x.dtype, dtype))
+    p.type, p.out_type, p.tokens = _TYPES[x.dtype], _TYPES[dtype], x.shape[0]
+    return c, p
+
+
+def weights_product_workspace(x, codes, scales, rows=None):
+    """Bytes of scratch memory that weights_product can use for these arguments."""
+    c, p = _product(x, codes, scales, rows, x.dtype)
+    with torch.cuda.device(x.device):
+        return int(lib().dq8_weights_product_workspace_bytes(ctypes.byref(c), ctypes.byref(p)))
+
+
+def weights_product(x, codes, scales, rows=None, bias=None, dtype=None, out=None, workspace=None):
+    """x [tokens, cols] (bfloat16 or float16) times compressed weights, out[m, n] = sum_k x[m, k] w[n, k] (+ bias[n], float32).
+
+    rows: of the weights, where these do not fill their last tile.  dtype: of the result, x's or float32.  workspace: a uint8 tensor of
+    weights_product_workspace() bytes; None: taken from torch's allocator, and not while the stream is captured into a graph (hand one in there:
+    without it weights of few rows and more than 16 tokens take longer).  For serving: as with every call here no gradient passes through it."""
+    done = _native.weights_product(x, codes, scales, rows, bias, dtype, out, workspace)
+    if done is not None:
+        return done
+    if dtype is None:
+        dtype = x.dtype if out is None else out.dtype
+    c, p = _product(x, codes, scales, rows, dtype)
     if out is None:
         out = torch.empty((x.shape[0], c.rows), dtype=dtype, device=x.device)
-    p = _Product()
-    p.type, p.out_type, p.tokens, p.x, p.x_stride = _TYPES[x.dtype], _TYPES[dtype], x.shape[0], at, stride
     p.out, p.out_stride = _matrix(out, "out", x.device, (dtype,), x.shape[0], c.rows)
     if bias is not None:
         _dev(bias, torch.float32, "bias")
         if tuple(bias.shape) != (c.rows,) or bias.device != x.device:
             raise ValueError("bias must have shape [%d] on x's device" % c.rows)
         p.bias = bias.data_ptr()
-    _enqueue(lib().dq8_weights_product, x.get_device(), ctypes.byref(c), ctypes.byref(p))
+    if workspace is None:
+        with torch.cuda.device(x.device):
+            if not torch.cuda.is_current_stream_capturing():
+                workspace = torch.empty(int(lib().dq8_weights_product_workspace_bytes(ctypes.byref(c), ctypes.byref(p))), dtype=torch.uint8, device=x.device)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
+        if workspace.device != x.device:
+            raise ValueError("workspace is on another device than x")
+    _enqueue(lib().dq8_weights_product, x.get_device(), ctypes.byref(c), ctypes.byref(p),
+             workspace.data_ptr() if workspace is not None and workspace.numel() else None, 0 if workspace is None else workspace.numel())
     return out
 
 

@@ -24,7 +24,9 @@ def L():
     lib.dq8_last_error.restype = ctypes.c_char_p
     lib.dq8_weights_encode.argtypes = [ci, vp, sz, vp, vp]
     lib.dq8_weights_decode.argtypes = [vp, ci, vp, sz, vp]
-    lib.dq8_weights_product.argtypes = [vp, vp, vp]
+    lib.dq8_weights_product.argtypes = [vp, vp, vp, sz, vp]
+    lib.dq8_weights_product_workspace_bytes.argtypes = [vp, vp]
+    lib.dq8_weights_product_workspace_bytes.restype = sz
     lib.dq8_cache_plan.argtypes = [vp, vp]
     lib.dq8_draft_verify.argtypes = [vp, vp, sz, vp]
     lib.dq8_draft_verify_workspace_bytes.argtypes = [vp]
@@ -62,7 +64,7 @@ def verify(**change):
 
 
 @pytest.mark.parametrize("name,calls", [
-    ("dq8_weights.h", ["dq8_weights_decode", "dq8_weights_encode", "dq8_weights_product"]),
+    ("dq8_weights.h", ["dq8_weights_decode", "dq8_weights_encode", "dq8_weights_product", "dq8_weights_product_workspace_bytes"]),
     ("dq8_serve.h", ["dq8_cache_plan", "dq8_draft_verify", "dq8_draft_verify_workspace_bytes"])])
 def test_every_declared_call_is_exported(L, name, calls):
     header = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", name)).read(), flags=re.S)
@@ -91,7 +93,7 @@ def test_refused_weights(L, status, change):
     w, p = weights(**change), product()
     assert L.dq8_weights_encode(1, at(2), 300, ctypes.byref(w), None) == status and L.dq8_last_error()
     assert L.dq8_weights_decode(ctypes.byref(w), 1, at(2), 300, None) == status
-    assert L.dq8_weights_product(ctypes.byref(w), ctypes.byref(p), None) == status
+    assert L.dq8_weights_product(ctypes.byref(w), ctypes.byref(p), None, 0, None) == status
 
 
 def test_refused_matrices(L):
@@ -113,14 +115,14 @@ def test_refused_matrices(L):
     (3, {"out_stride": 19}), (3, {"out_stride": 1 << 45}), (3, {"out": at(2)}), (3, {"out": at(0)}), (3, {"out": at(1)}), (3, {"out": at(4)}), (3, {"x": at(0)})])
 def test_refused_products(L, status, change):
     w, p = weights(), product(**change)
-    assert L.dq8_weights_product(ctypes.byref(w), ctypes.byref(p), None) == status and L.dq8_last_error()
+    assert L.dq8_weights_product(ctypes.byref(w), ctypes.byref(p), None, 0, None) == status and L.dq8_last_error()
 
 
 def test_products_of_nothing(L):
-    assert L.dq8_weights_product(ctypes.byref(weights()), ctypes.byref(product(tokens=0, x=None, out=None)), None) == 0
-    assert L.dq8_weights_product(ctypes.byref(weights(rows=0, codes=None, scales=None)), ctypes.byref(product(out=None)), None) == 0
-    assert L.dq8_weights_product(ctypes.byref(weights(cols=0)), ctypes.byref(product()), None) == 3
-    assert L.dq8_weights_product(ctypes.byref(weights()), None, None) == 1
+    assert L.dq8_weights_product(ctypes.byref(weights()), ctypes.byref(product(tokens=0, x=None, out=None)), None, 0, None) == 0
+    assert L.dq8_weights_product(ctypes.byref(weights(rows=0, codes=None, scales=None)), ctypes.byref(product(out=None)), None, 0, None) == 0
+    assert L.dq8_weights_product(ctypes.byref(weights(cols=0)), ctypes.byref(product()), None, 0, None) == 3
+    assert L.dq8_weights_product(ctypes.byref(weights()), None, None, 0, None) == 1
     for w in (weights(rows=0, codes=None), weights(cols=0, scales=None)):
         assert L.dq8_weights_encode(1, None, 0, ctypes.byref(w), None) == 0 and L.dq8_weights_decode(ctypes.byref(w), 0, None, 0, None) == 0
 
@@ -161,6 +163,11 @@ def test_refused_workspaces(L):
     assert L.dq8_draft_verify(ctypes.byref(v), at(9, 8), 64, None) == 3
     for i in range(9):
         assert L.dq8_draft_verify(ctypes.byref(v), at(i), 64, None) == 3
+    for space in (at(9, 8), at(0), at(1), at(2), at(3), at(4)):
+        assert L.dq8_weights_product(ctypes.byref(weights()), ctypes.byref(product()), space, 64, None) == 3
+    assert L.dq8_weights_product_workspace_bytes(ctypes.byref(weights(group=1)), ctypes.byref(product(tokens=100))) == 0
+    assert L.dq8_weights_product_workspace_bytes(ctypes.byref(weights()), ctypes.byref(product(tokens=16))) == 0
+    assert L.dq8_weights_product_workspace_bytes(None, None) == 0
     assert L.dq8_draft_verify(None, None, 0, None) == 1 and L.dq8_draft_verify_workspace_bytes(None) == 0
     assert L.dq8_draft_verify(ctypes.byref(verify(batch=0)), None, 0, None) == 0
 
