@@ -9,16 +9,53 @@ namespace {
 constexpr uint32_t kPlanWg = 1024, kPlanMost = 4096;  // lanes of the plan's workgroup, sequences at most
 constexpr uint32_t kRun = kPlanMost / kPlanWg;         // sequences of a lane, at most
 
-// Sums over the lanes up to and with each.
-template <typename T>
-__device__ __forceinline__ T scan_wave(T v, uint32_t lane)
+// A number of another lane (data-parallel primitives: no LDS, 8 cycles; a shuffle takes a hundred), zero where the pattern has none for a lane.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T from_lane(T v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const T o = __shfl_up(v, d);
-        if (lane >= (uint32_t)d) v += o;
+    if constexpr (sizeof(T) == 8) {
+        uint64_t u;
+        __builtin_memcpy(&u, &v, 8);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xF, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xF, false);
+        u = (uint64_t)hi << 32 | lo;
+        __builtin_memcpy(&v, &u, 8);
+        return v;
+    } else {
+        return (T)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
     }
+}
+
+// Sums over the lanes up to and with each: 1, 2, 4, 8 lanes back inside rows of 16, then lane 15 of a row into the next and lane 31 into the upper half.
+template <typename T>
+__device__ __forceinline__ T scan_wave(T v)
+{
+    v += from_lane<0x111, 0xF>(v);
+    v += from_lane<0x112, 0xF>(v);
+    v += from_lane<0x114, 0xF>(v);
+    v += from_lane<0x118, 0xF>(v);
+    v += from_lane<0x142, 0xA>(v);
+    v += from_lane<0x143, 0xC>(v);
     return v;
+}
+
+// The number of a lane that is the same for all.
+template <typename T>
+__device__ __forceinline__ T of_lane(T v, int lane)
+{
+    uint64_t all = 0;
+    __builtin_memcpy(&all, &v, sizeof(T));
+    uint64_t u = (uint32_t)__builtin_amdgcn_readlane((int)all, lane);
+    if constexpr (sizeof(T) == 8) u |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(all >> 32), lane) << 32;
+    __builtin_memcpy(&v, &u, sizeof(T));
+    return v;
+}
+
+// The number of the lane before (zero for the first).
+template <typename T>
+__device__ __forceinline__ T before_lane(T v)
+{
+    return from_lane<0x138, 0xF>(v);
 }
 
 // Sums over the lanes before each in a workgroup of WAVES wavefronts; all: the sum of everything.  `spare` is LDS of WAVES numbers.
@@ -26,12 +63,11 @@ template <int WAVES, typename T>
 __device__ __forceinline__ T sum_before(T v, T *spare, T &all)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    v = scan_wave(v, lane);
+    const T upto = scan_wave(v);
     __syncthreads();
-    if (lane == 63) spare[wave] = v;
+    if (lane == 63) spare[wave] = upto;
     __syncthreads();
-    v = __shfl_up(v, 1);
-    if (lane == 0) v = 0;
+    v = before_lane(upto);
     T before = 0;
     all = 0;
 #pragma unroll
@@ -198,6 +234,11 @@ __global__ __launch_bounds__(kPlaceWg) void k_cache_place(PlanArgs a)
 }
 
 // ---------------------------------------------------------------- verification
+//
+// A sequence's drafts are judged by single numbers; only the row behind the accepted ones is read as a whole, the draft's too where one was
+// refused.  A row is cut into chunks; a wavefront adds up one at a time.  The chunk in which the sum passes its mark is found from the
+// chunks' sums and read once more by one wavefront, which finds the token in it.  All sums are binary64: their rounding, 2^-53 of the whole, moves no token's
+// border by as much as 2^-28 of the smallest step between two random numbers of 24 bits.
 
 struct VerifyArgs {
     const void *target, *draft;
@@ -208,8 +249,9 @@ struct VerifyArgs {
     int64_t *out;
     int32_t *accepted, *rejected;
     uint32_t tokens, batch, each, vocab;
-    uint32_t chunk, chunks;  // probabilities that a wavefront adds up, and how many such
-    double2 *sums;           // workspace [batch][chunks]: of the weights, and of the target alone (null: there is none)
+    uint32_t chunk, chunks;   // probabilities that a wavefront adds up at a time, and how many such
+    struct Verdict *verdicts; // workspace [batch] (null: there is none)
+    double *sums;             // workspace [batch][chunks]
 };
 
 // A probability: what is no positive number counts as none.
@@ -222,12 +264,11 @@ __device__ __forceinline__ float probability(T v)
 
 // Where a sequence ends: rows first .. first + n - 1, `row` of them accepted; refused: whether row `row` refused its draft `token`.
 struct Verdict {
-    uint32_t first, n, row;
-    bool refused;
+    uint32_t first, n, row, refused;
     int64_t token;
 };
 
-// Every wavefront that needs it finds it by itself: a lane per draft.
+// Every wavefront finds it by itself: a lane per draft.
 template <typename T>
 __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
 {
@@ -245,7 +286,7 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
     }
     v.n = end - v.first;
     v.row = v.n ? v.n - 1 : 0;
-    v.refused = false;
+    v.refused = 0;
     v.token = -1;
     for (uint32_t i0 = 0; i0 + 1 < v.n; i0 += 64) {
         const uint32_t i = i0 + lane;
@@ -253,25 +294,32 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
         int64_t d = -1;
         if (i + 1 < v.n) {
             const size_t row = v.first + i;
+            const float u = a.uniform[row];
             d = a.ids[row + 1];
             no = true;
             if (d >= 0 && d < (int64_t)a.vocab) {
                 const double p = probability(static_cast<const T *>(a.target)[row * a.target_stride + d]);
                 const double q = a.draft ? probability(static_cast<const T *>(a.draft)[row * a.draft_stride + d]) : 1.0f;
-                no = !((double)a.uniform[row] * q < p);  // 24 times 24 bits: exact
+                no = !((double)u * q < p);  // 24 times 24 bits: exact
             }
         }
         const uint64_t votes = __builtin_amdgcn_ballot_w64(no);
         if (votes) {
             const int l = __builtin_ctzll(votes);
             v.row = i0 + (uint32_t)l;
-            v.refused = true;
+            v.refused = 1;
             v.token = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(d >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)d, l));
             break;
         }
     }
+    v.first = (uint32_t)__builtin_amdgcn_readfirstlane((int)v.first);
+    v.n = (uint32_t)__builtin_amdgcn_readfirstlane((int)v.n);
+    v.row = (uint32_t)__builtin_amdgcn_readfirstlane((int)v.row);
     return v;
 }
+
+constexpr uint32_t kSumsWaves = 4, kAloneWaves = 16, kChunksMost = 2048, kChunk = 1024;
+constexpr int kPer = kChunk / 64;  // numbers of a lane: neighbours
 
 // The row from which a sequence's token is drawn.
 template <typename T>
@@ -287,160 +335,180 @@ struct Row {
         less = v.refused && !a.draft ? v.token : -1;
     }
 
-    __device__ __forceinline__ double weight(float pt, float qt, uint32_t t) const
+    // The weights of the lane's kPer tokens of kChunk from `begin` on, zeros behind `end`.  What a compute unit does for a number counts where it has a
+    // whole row, so each kind of row has its own steps.  (A branch around each load would make the next wait for it: 16 round trips to memory.)
+    __device__ __forceinline__ void weights(uint32_t begin, uint32_t end, double (&w)[kPer]) const
     {
-        const double w = (double)pt - (double)qt;
-        return (int64_t)t == less || !(w > 0.0) ? 0.0 : w;
+        typedef T V __attribute__((ext_vector_type(4)));
+        typedef V VA __attribute__((aligned(sizeof(T))));
+        const uint32_t t = begin + (threadIdx.x & 63) * kPer;
+        V x[kPer / 4], y[kPer / 4];
+        if (end - begin >= kChunk) {
+#pragma unroll
+            for (int k = 0; k < kPer / 4; ++k) x[k] = *reinterpret_cast<const VA *>(p + t + 4 * k);
+            if (q) {
+#pragma unroll
+                for (int k = 0; k < kPer / 4; ++k) y[k] = *reinterpret_cast<const VA *>(q + t + 4 * k);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) x[k / 4][k % 4] = p[t + k < end ? t + k : end - 1];
+            if (q) {
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) y[k / 4][k % 4] = q[t + k < end ? t + k : end - 1];
+            }
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (t + k >= end) x[k / 4][k % 4] = (T)0.0f;
+        }
+        if (q) {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const double d = (double)probability(x[k / 4][k % 4]) - (double)probability(y[k / 4][k % 4]);
+                w[k] = __builtin_fmax(d, 0.0);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) w[k] = (double)probability(x[k / 4][k % 4]);
+            if (less >= (int64_t)begin && less < (int64_t)end) {
+#pragma unroll
+                for (int k = 0; k < kPer; ++k)
+                    if ((int64_t)t + k == less) w[k] = 0.0;
+            }
+        }
     }
 };
 
-__device__ __forceinline__ double sum_wave(double v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-
-// A wavefront's sums over a chunk: of the weights and of the target's probabilities alone.
+// A wavefront's sum of the weights of a chunk, in its last lane.
 template <typename T>
-__device__ __forceinline__ double2 sum_chunk(const VerifyArgs &a, const Row<T> &row, uint32_t c)
+__device__ __forceinline__ double sum_chunk(const VerifyArgs &a, const Row<T> &row, uint32_t c)
 {
-    typedef T V __attribute__((ext_vector_type(4)));
-    typedef V VA __attribute__((aligned(sizeof(T))));
-    const uint32_t lane = threadIdx.x & 63, begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
-    double w = 0.0, all = 0.0;
-#pragma unroll 4
-    for (uint32_t t = begin + 4 * lane; t < end; t += 256) {
-        V p = {}, q = {};
-        if (t + 4 <= end) {
-            p = *reinterpret_cast<const VA *>(row.p + t);
-            if (row.q) q = *reinterpret_cast<const VA *>(row.q + t);
-        } else {
-            for (int e = 0; e < 4; ++e)
-                if (t + e < end) {
-                    p[e] = row.p[t + e];
-                    if (row.q) q[e] = row.q[t + e];
-                }
-        }
+    const uint32_t begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
+    double sum = 0.0;
+    for (uint32_t i = begin; i < end; i += kChunk) {
+        double w[kPer];
+        row.weights(i, end, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float f = probability(p[e]);
-            w += row.weight(f, probability(q[e]), t + e);
-            all += f;
-        }
+        for (int k = 0; k < kPer; ++k) sum += w[k];
     }
-    return double2{sum_wave(w), sum_wave(all)};
+    return scan_wave(sum);
 }
 
-constexpr uint32_t kVerifyWg = 256, kVerifyWaves = kVerifyWg / 64, kChunksMost = 2048, kChunk = 1024;
-
 template <typename T>
-__global__ __launch_bounds__(kVerifyWg) void k_verify_sums(VerifyArgs a)
+__global__ __launch_bounds__(kSumsWaves * 64) void k_verify_sums(VerifyArgs a)
 {
-    const uint32_t b = blockIdx.y, c = blockIdx.x * kVerifyWaves + (threadIdx.x >> 6);
+    const uint32_t b = blockIdx.y, c = blockIdx.x * kSumsWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (c >= a.chunks) return;
     const Verdict v = verdict_of<T>(a, b);
+    if (c == 0 && lane == 0) a.verdicts[b] = v;
     if (v.n == 0) return;
-    const double2 s = sum_chunk(a, Row<T>(a, v), c);
-    if ((threadIdx.x & 63) == 0) a.sums[(size_t)b * a.chunks + c] = s;
+    const double s = sum_chunk(a, Row<T>(a, v), c);
+    if (lane == 63) a.sums[(size_t)b * a.chunks + c] = s;
 }
 
-// One workgroup per sequence: the chunk in which the sum passes its mark, then the token in it.
-template <typename T>
-__global__ __launch_bounds__(kVerifyWg) void k_verify_pick(VerifyArgs a)
+// Numbers of a wavefront, `run` of a lane in the order of the lanes; next(i): the lane's number i.  The sum before the lane's first one, and of all.
+template <typename F>
+__device__ __forceinline__ double sums_of(uint32_t run, double &total, F next)
 {
-    __shared__ double2 sums[kChunksMost];
-    __shared__ double spare[kVerifyWaves];
-    __shared__ uint32_t found, last;
-    const uint32_t b = blockIdx.x, t = threadIdx.x, lane = t & 63;
-    const Verdict v = verdict_of<T>(a, b);
-    if (t == 0) {
+    double mine = 0.0;
+    for (uint32_t i = 0; i < run; ++i) mine += next(i);
+    const double upto = scan_wave(mine);
+    total = of_lane(upto, 63);
+    return before_lane(upto);
+}
+
+// The first of them up to and with which their sum is above the mark, or the last positive one where none is; `sum` is the sum before the
+// lane's first one, and then the one before that number.
+template <typename F>
+__device__ __forceinline__ uint32_t first_above(uint32_t run, double mark, double &sum, F next)
+{
+    uint32_t at = 0xFFFFFFFFu, last = 0xFFFFFFFFu;
+    double held = 0.0, held_last = 0.0;
+    for (uint32_t i = 0; i < run; ++i) {
+        const double x = next(i);
+        if (x > 0.0) {
+            last = i;
+            held_last = sum;
+            if (at == 0xFFFFFFFFu && sum + x > mark) {
+                at = i;
+                held = sum;
+            }
+        }
+        sum += x;
+    }
+    const uint64_t votes = __builtin_amdgcn_ballot_w64(at != 0xFFFFFFFFu), some = __builtin_amdgcn_ballot_w64(last != 0xFFFFFFFFu);
+    const int l = votes ? __builtin_ctzll(votes) : 63 - __builtin_clzll(some);
+    sum = of_lane(votes ? held : held_last, l);
+    return (uint32_t)l * run + (uint32_t)__builtin_amdgcn_readlane((int)(votes ? at : last), l);
+}
+
+// One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums.
+template <typename T, bool ALONE>
+__global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(VerifyArgs a)
+{
+    __shared__ double sums[kChunksMost];
+    const uint32_t b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float r = a.sample[b];
+    const Verdict v = ALONE ? verdict_of<T>(a, b) : a.verdicts[b];
+    if constexpr (!ALONE)
+        for (uint32_t c = lane; c < a.chunks; c += 64) sums[c] = a.sums[(size_t)b * a.chunks + c];
+    if (threadIdx.x == 0) {
         a.accepted[b] = v.n ? (int32_t)v.row : -1;
         a.rejected[b] = v.n ? (int32_t)(v.n - 1 - v.row) : 0;
     }
     if (v.n == 0) return;
-    const Row<T> row(a, v);
-    if (a.sums) {
-        for (uint32_t c = t; c < a.chunks; c += kVerifyWg) sums[c] = a.sums[(size_t)b * a.chunks + c];
-    } else {
-        for (uint32_t c = t >> 6; c < a.chunks; c += kVerifyWaves) {
-            const double2 s = sum_chunk(a, row, c);
-            if (lane == 0) sums[c] = s;
+    Row<T> row(a, v);
+    if constexpr (ALONE)
+        for (uint32_t c = wave; c < a.chunks; c += kAloneWaves) {
+            const double s = sum_chunk(a, row, c);
+            if (lane == 63) sums[c] = s;
         }
-    }
-    if (t == 0) {
-        found = 0xFFFFFFFFu;
-        last = 0;
-    }
     __syncthreads();
-    // a lane has a run of chunks
-    const uint32_t run = (a.chunks + kVerifyWg - 1) / kVerifyWg, c0 = t * run < a.chunks ? t * run : a.chunks, c1 = c0 + run < a.chunks ? c0 + run : a.chunks;
-    double w = 0.0, all = 0.0, total, total_all;
-    for (uint32_t c = c0; c < c1; ++c) {
-        w += sums[c].x;
-        all += sums[c].y;
-    }
-    const double before = sum_before<kVerifyWaves>(w, spare, total), before_all = sum_before<kVerifyWaves>(all, spare, total_all);
-    const bool plain = !(total > 0.0);  // the target's own
-    if (plain) total = total_all;
-    const float r = a.sample[b];
-    const double mark = (r > 0.0f ? (double)r : 0.0) * total;
-    // the first chunk that passes the mark, else the last with a weight
-    double sum = plain ? before_all : before;
-    for (uint32_t c = c0; c < c1; ++c) {
-        const double s = plain ? sums[c].y : sums[c].x, next = sum + s;
-        if (s > 0.0) {
-            atomicMax(&last, c);
-            if (next > mark) {
-                atomicMin(&found, c);
-                break;
-            }
+    if (wave != 0) return;
+    const uint32_t run = (a.chunks + 63) / 64;
+    auto chunk_sum = [&](uint32_t i) { return lane * run + i < a.chunks ? sums[lane * run + i] : 0.0; };
+    double total, sum = sums_of(run, total, chunk_sum);
+    if (!(total > 0.0)) {  // nothing is left of the difference: the target's own
+        row.q = nullptr;
+        row.less = -1;
+        for (uint32_t c = 0; c < a.chunks; ++c) {
+            const double s = sum_chunk(a, row, c);
+            if (lane == 63) sums[c] = s;
         }
-        sum = next;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        sum = sums_of(run, total, chunk_sum);
     }
-    __syncthreads();
     int64_t token = -1;
     if (total > 0.0) {
-        const uint32_t c = found != 0xFFFFFFFFu ? found : last;
-        __syncthreads();
-        if (t == 0) found = 0xFFFFFFFFu, last = 0;
-        // the sum before it, as that lane has it
-        if (c >= c0 && c < c1) {
-            double s = plain ? before_all : before;
-            for (uint32_t k = c0; k < c; ++k) s += plain ? sums[k].y : sums[k].x;
-            spare[0] = s;
-        }
-        __syncthreads();
-        double base = spare[0];
+        const double mark = (r > 0.0f ? (double)r : 0.0) * total;
+        const uint32_t c = first_above(run, mark, sum, chunk_sum);
         const uint32_t begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
-        for (uint32_t i0 = begin; i0 < end; i0 += kVerifyWg * 4) {
-            double x[4], mine = 0.0, some;
+        for (uint32_t i0 = begin; i0 < end; i0 += kChunk) {
+            double x[kPer], mine = 0.0;
+            row.weights(i0, end, x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t i = i0 + 4 * t + e;
-                x[e] = 0.0;
-                if (i < end) {
-                    const float p = probability(row.p[i]);
-                    x[e] = plain ? (double)p : row.weight(p, row.q ? probability(row.q[i]) : 0.0f, i);
-                }
-                mine += x[e];
-            }
-            double s = base + sum_before<kVerifyWaves>(mine, spare, some);
+            for (int k = 0; k < kPer; ++k) mine += x[k];
+            const double upto = scan_wave(mine);
+            double s = sum + before_lane(upto);
+            uint32_t at = 0xFFFFFFFFu, last = 0xFFFFFFFFu;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s += x[e];
-                if (x[e] > 0.0) {
-                    atomicMax(&last, i0 + 4 * t + e);
-                    if (s > mark) atomicMin(&found, i0 + 4 * t + e);
+            for (int k = 0; k < kPer; ++k) {
+                s += x[k];
+                if (x[k] > 0.0) {
+                    last = k;
+                    if (at == 0xFFFFFFFFu && s > mark) at = k;
                 }
             }
-            __syncthreads();
-            if (found != 0xFFFFFFFFu) break;
-            base += some;
+            const uint64_t votes = __builtin_amdgcn_ballot_w64(at != 0xFFFFFFFFu), some = __builtin_amdgcn_ballot_w64(last != 0xFFFFFFFFu);
+            if (some) {  // (the last one with a weight, if the rounding of sums leaves none above the mark)
+                const int l = votes ? __builtin_ctzll(votes) : 63 - __builtin_clzll(some);
+                token = i0 + (uint32_t)l * kPer + (uint32_t)__builtin_amdgcn_readlane((int)(votes ? at : last), l);
+            }
+            if (votes) break;
+            sum += of_lane(upto, 63);
         }
-        token = found != 0xFFFFFFFFu ? found : last;
     }
-    for (uint32_t i = t; i < v.n; i += kVerifyWg) a.out[v.first + i] = i < v.row ? a.ids[v.first + i + 1] : i == v.row ? token : -1;
+    for (uint32_t i = lane; i < v.n; i += 64) a.out[v.first + i] = i < v.row ? a.ids[v.first + i + 1] : i == v.row ? token : -1;
 }
 
 }  // namespace

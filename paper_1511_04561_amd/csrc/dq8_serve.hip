@@ -54,15 +54,28 @@ void cut(const dq8_verify &v, uint32_t &chunk, uint32_t &chunks)
     chunks = (uint32_t)((v.vocab + chunk - 1) / chunk);
 }
 
+// A row of up to this many bytes (with the draft's) is read by one workgroup.
+constexpr size_t kAloneBytes = 256 << 10;
+
+size_t workspace_of(const dq8_verify &v)
+{
+    uint32_t chunk, chunks;
+    cut(v, chunk, chunks);
+    if (v.vocab * (v.type == DQ8_FLOAT32 ? 4 : 2) * (v.draft ? 2 : 1) <= kAloneBytes) return 0;
+    return v.batch * (sizeof(Verdict) + chunks * sizeof(double));
+}
+
 template <typename T>
 int verify(const VerifyArgs &k, hipStream_t stream)
 {
-    if (k.sums) {
-        hipLaunchKernelGGL(k_verify_sums<T>, dim3((k.chunks + kVerifyWaves - 1) / kVerifyWaves, k.batch), dim3(kVerifyWg), 0, stream, k);
-        const int rc = dq8::after_launch_of("k_verify_sums", stream);
-        if (rc) return rc;
+    if (!k.sums) {
+        hipLaunchKernelGGL((k_verify_pick<T, true>), dim3(k.batch), dim3(kAloneWaves * 64), 0, stream, k);
+        return dq8::after_launch_of("k_verify_pick", stream);
     }
-    hipLaunchKernelGGL(k_verify_pick<T>, dim3(k.batch), dim3(kVerifyWg), 0, stream, k);
+    hipLaunchKernelGGL(k_verify_sums<T>, dim3((k.chunks + kSumsWaves - 1) / kSumsWaves, k.batch), dim3(kSumsWaves * 64), 0, stream, k);
+    const int rc = dq8::after_launch_of("k_verify_sums", stream);
+    if (rc) return rc;
+    hipLaunchKernelGGL((k_verify_pick<T, false>), dim3(k.batch), dim3(64), 0, stream, k);
     return dq8::after_launch_of("k_verify_pick", stream);
 }
 
@@ -112,9 +125,7 @@ int dq8_cache_plan(const dq8_plan *in, void *hip_stream)
 size_t dq8_draft_verify_workspace_bytes(const dq8_verify *v)
 {
     if (check_verify("dq8_draft_verify_workspace_bytes", v) || v->batch == 0 || v->tokens == 0) return 0;
-    uint32_t chunk, chunks;
-    cut(*v, chunk, chunks);
-    return v->batch * chunks * sizeof(double2);
+    return workspace_of(*v);
 }
 
 int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_bytes, void *hip_stream)
@@ -139,8 +150,10 @@ int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_byt
     k.ids = v.ids, k.uniform = v.uniform, k.sample = v.sample, k.starts = v.starts, k.out = v.out, k.accepted = v.accepted, k.rejected = v.rejected;
     k.tokens = (uint32_t)v.tokens, k.batch = (uint32_t)v.batch, k.each = v.starts ? 0 : (uint32_t)(v.tokens / v.batch), k.vocab = (uint32_t)v.vocab;
     cut(v, k.chunk, k.chunks);
-    k.sums = workspace && workspace_bytes >= v.batch * k.chunks * sizeof(double2) ? static_cast<double2 *>(workspace) : nullptr;
-    if (v.tokens == 0) k.sums = nullptr;
+    const size_t needed = v.tokens ? workspace_of(v) : 0;
+    const bool some = needed && workspace && workspace_bytes >= needed;
+    k.sums = some ? static_cast<double *>(workspace) : nullptr;
+    k.verdicts = some ? reinterpret_cast<Verdict *>(k.sums + v.batch * k.chunks) : nullptr;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (v.type == DQ8_FLOAT32) return verify<float>(k, stream);
     return v.type == DQ8_BFLOAT16 ? verify<__bf16>(k, stream) : verify<_Float16>(k, stream);

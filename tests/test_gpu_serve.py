@@ -189,7 +189,23 @@ def test_large_vocabularies(dtype, vocab):
     p, q = (torch.rand(5, vocab, generator=g).div_(vocab).mul_(3000 if dtype == torch.float16 else 1).to(dtype) for _ in range(2))
     ids = torch.randint(0, vocab, (5,), generator=g).numpy()
     for u in (0.0, 0.9):
-        both(p, q, ids, np.full(5, u, np.float32), [0.0, 0.37, 0.9999999], [0, 2, 4, 5])
+        for draft in (q, None):
+            both(p, draft, ids, np.full(5, u, np.float32), [0.0, 0.37, 0.9999999], [0, 2, 4, 5])
+            both(p, draft, ids, np.full(5, u, np.float32), [1.0, 0.5, 0.25, float("nan"), 0.75], [0, 1, 2, 3, 4, 5])
+
+
+def test_large_vocabularies_with_few_weights():
+    """Whole chunks without a weight, before, between and behind those that have some."""
+    vocab = 200000
+    for some in ([199999], [0], [1024, 1023], [5000, 150000, 150001], [2047, 2048, 199998], []):
+        p, q = torch.zeros(3, vocab), torch.zeros(3, vocab)
+        p[:, some] = 0.25
+        q[:, :70000] = 1e-6
+        q[1, some] = 0.25
+        for ids in ([0, 7, 100], [0, (some or [3])[0], 5]):
+            for r in (0.0, 0.3, 0.5, 0.99999994, 1.0):
+                both(p, q, np.array(ids), np.full(3, 0.5, np.float32), [r], [0, 3])
+                both(p, None, np.array(ids), np.full(3, 0.1, np.float32), [r, r], [0, 2, 3])
 
 
 def test_random_numbers_at_their_ends():
@@ -240,11 +256,11 @@ def test_verification_with_strides_and_even_rows():
 
 
 def test_verification_workspaces_and_graphs():
-    p, q, ids, uniform, rng = drafts(20, 5000, 2, torch.float32)
+    p, q, ids, uniform, rng = drafts(20, 50000, 2, torch.float32)
     args = [p.cuda(), dev(ids, I64), dev(uniform), dev(rng.random(5).astype(np.float32))]
     starts, draft = dev([0, 4, 8, 12, 16, 20], I32), q.cuda()
     n = dq8.draft_verify_workspace(*args, starts=starts, draft=draft)
-    assert n == 5 * 5 * 16
+    assert n == 5 * (24 + 49 * 8)
     want = dq8.draft_verify(*args, starts=starts, draft=draft)
     for bytes_ in (n, n - 1, n + 100):
         space = torch.full((n + 160,), 0xA5, dtype=torch.uint8, device="cuda")
