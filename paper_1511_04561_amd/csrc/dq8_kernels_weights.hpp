@@ -25,35 +25,146 @@ __device__ __forceinline__ float bf16_value(uint32_t bits16) { return __uint_as_
 
 // ---------------------------------------------------------------- compression and expansion
 
-// The nearest of eight magnitudes, the smaller of two as near, by comparisons with the borders between them times the scale.  These
-// products have 3 + 8 bits: they are exact, and the comparison is one of real numbers.
-struct Borders {
-    float b[7];
-    __device__ __forceinline__ explicit Borders(float s) : b{0.25f * s, 0.75f * s, 1.25f * s, 1.75f * s, 2.5f * s, 3.5f * s, 5.0f * s} {}
-    __device__ __forceinline__ uint32_t code(float a) const
+typedef uint16_t w2s __attribute__((ext_vector_type(2)));
+
+// The scale of a group whose largest absolute value has these bits as binary32: the nearest bfloat16 number to a sixth of it.
+__device__ __forceinline__ float scale_of(uint32_t most)
+{
+    const uint32_t bits = __float_as_uint(__uint_as_float(most) / 6.0f);
+    const float s = bf16_value((bits + 0x7FFFu + ((bits >> 16) & 1)) >> 16);
+    return s < kScaleTop ? s : kScaleTop;
+}
+
+__device__ __forceinline__ uint32_t most_of_row(uint32_t most)
+{
+#pragma unroll
+    for (int d = 16; d <= 32; d *= 2) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)most, d);
+        most = o > most ? o : most;
+    }
+    return most;
+}
+
+// A lane's eight elements of a run, and how they become codes.  binary32: the nearest of eight magnitudes, the smaller of two as near, by comparisons with the
+// borders between them times the scale.  These products have 3 + 8 bits: they are exact, and the comparison is one of real numbers.
+template <typename T>
+struct Eight {
+    float x[8];
+
+    __device__ __forceinline__ void load(const float *row, size_t k, size_t cols)
     {
-        const bool c2 = a > b[3];
-        const bool c1 = a > (c2 ? b[5] : b[1]);
-        const bool c0 = a > (c2 ? (c1 ? b[6] : b[4]) : (c1 ? b[2] : b[0]));
-        return (uint32_t)c2 * 4 + (uint32_t)c1 * 2 + (uint32_t)c0;
+        typedef float V __attribute__((ext_vector_type(8), aligned(4)));
+        if (k + 8 <= cols) {
+            const V v = *reinterpret_cast<const V *>(row + k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = k + e < cols ? row[k + e] : 0.0f;
+        }
+    }
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+    }
+
+    // The bits of the largest absolute value: infinities and NaN are above all others.
+    __device__ __forceinline__ uint32_t most() const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+            m = b > m ? b : m;
+        }
+        return m;
+    }
+
+    __device__ __forceinline__ uint32_t codes(float s) const
+    {
+        const float b0 = 0.25f * s, b1 = 0.75f * s, b2 = 1.25f * s, b3 = 1.75f * s, b4 = 2.5f * s, b5 = 3.5f * s, b6 = 5.0f * s;
+        uint32_t v = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = fabsf(x[e]);
+            const bool c2 = a > b3, c1 = a > (c2 ? b5 : b1), c0 = a > (c2 ? (c1 ? b6 : b4) : (c1 ? b2 : b0));
+            v |= ((__float_as_uint(x[e]) >> 31) * 8 + (uint32_t)c2 * 4 + (uint32_t)c1 * 2 + (uint32_t)c0) << (4 * e);
+        }
+        return v;
     }
 };
 
-// Eight elements of a row from column k on, zeros behind the last one.
+// 16 bits: the conversion to 4 bits rounds the quotient x / s to the nearest, and to even where it lies between two.  A border times the scale and x have 11
+// bits at most, so that x, where it is not on a border, is at least 2^-11 of itself away from it: quotients that are all made smaller by 2^-13 (their
+// own rounding is below 2^-22) lie on the same side of every border as the true ones, and those on a border below it.  The scale's exponent goes into the
+// conversion and one over the rest into a product, so that no reciprocal leaves binary32.
 template <typename T>
-__device__ __forceinline__ void eight_of(const T *row, size_t k, size_t cols, float (&x)[8])
-{
-    typedef T V __attribute__((ext_vector_type(8)));
-    typedef V VA __attribute__((aligned(sizeof(T))));
-    if (k + 8 <= cols) {
-        const V v = *reinterpret_cast<const VA *>(row + k);
+struct Eight16 {
+    w4u raw;
+
+    __device__ __forceinline__ void load(const T *row, size_t k, size_t cols)
+    {
+        typedef w4u WA __attribute__((aligned(2)));
+        if (k + 8 <= cols) {
+            raw = *reinterpret_cast<const WA *>(row + k);
+        } else {
+            typedef T V __attribute__((ext_vector_type(8)));
+            V v = {};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = k + e < cols ? (float)row[k + e] : 0.0f;
+            for (int e = 0; e < 8; ++e)
+                if (k + e < cols) v[e] = row[k + e];
+            __builtin_memcpy(&raw, &v, 16);
+        }
     }
-}
+
+    __device__ __forceinline__ void clear() { raw = w4u{0, 0, 0, 0}; }
+
+    __device__ __forceinline__ float at(int e) const
+    {
+        const uint32_t w = raw[e / 2];
+        if constexpr (__is_same(T, __bf16)) {
+            return __uint_as_float(e % 2 ? w & 0xFFFF0000u : w << 16);
+        } else {
+            const uint16_t u = (uint16_t)(e % 2 ? w >> 16 : w);
+            T h;
+            __builtin_memcpy(&h, &u, 2);
+            return (float)h;
+        }
+    }
+
+    __device__ __forceinline__ uint32_t most() const
+    {
+        w2s m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = raw[i] & 0x7FFF7FFFu;
+            w2s h;
+            __builtin_memcpy(&h, &u, 4);
+            m = __builtin_elementwise_max(m, h);
+        }
+        const uint16_t u = m.x > m.y ? m.x : m.y;
+        T h;
+        __builtin_memcpy(&h, &u, 2);
+        return __float_as_uint((float)h);
+    }
+
+    __device__ __forceinline__ uint32_t codes(float s) const
+    {
+        const uint32_t e = __float_as_uint(s) & 0x7F800000u, power = e ? e : 0x00800000u;  // 2^exponent, of the smallest normal number at least
+        const float two = __uint_as_float(power), part = __builtin_amdgcn_ldexpf(s, 127 - (int)(power >> 23)), f = (1.0f - 0x1p-13f) / part;
+        uint32_t v = 0;
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, at(0) * f, at(1) * f, two, 0);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, at(2) * f, at(3) * f, two, 1);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, at(4) * f, at(5) * f, two, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, at(6) * f, at(7) * f, two, 3);
+    }
+};
+template <>
+struct Eight<__bf16> : Eight16<__bf16> {};
+template <>
+struct Eight<_Float16> : Eight16<_Float16> {};
 
 // A wavefront per tile: lane 16 g + n has of row n the four runs of eight columns that its piece holds.
 template <typename T, int GROUP>
@@ -65,51 +176,39 @@ __global__ __launch_bounds__(256) void k_weights_encode(const T *__restrict__ w,
     const size_t tile = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (tile >= tiles) return;
     const size_t rt = tile / col_tiles, ct = tile - rt * col_tiles, row = rt * kTileRows + n;
-    float x[4][8];
+    Eight<T> x[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-        if (row < rows)
-            eight_of(w + row * stride, ct * kTileCols + 32 * s + 8 * g, cols, x[s]);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[s][e] = 0.0f;
+        x[s].clear();
+        if (row < rows) x[s].load(w + row * stride, ct * kTileCols + 32 * s + 8 * g, cols);
     }
-    uint32_t word[4], scale[PER];
+    w4u word;
+    uint32_t scale[PER];
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        uint32_t most = 0;  // of the absolute values' bits: infinities and NaN are above all others
+        uint32_t most = 0;
 #pragma unroll
-        for (int s = p * RUNS; s < (p + 1) * RUNS; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t b = __float_as_uint(x[s][e]) & 0x7FFFFFFFu;
-                most = b > most ? b : most;
-            }
-#pragma unroll
-        for (int d = 16; d <= 32; d *= 2) {
-            const uint32_t o = (uint32_t)__shfl_xor((int)most, d);
-            most = o > most ? o : most;
+        for (int s = p * RUNS; s < (p + 1) * RUNS; ++s) {
+            const uint32_t m = x[s].most();
+            most = m > most ? m : most;
         }
+        most = most_of_row(most);
         const bool bad = most >= 0x7F800000u;
-        const float q = __uint_as_float(most) / 6.0f;
-        const uint32_t bits = __float_as_uint(q);
-        float s = bf16_value((bits + 0x7FFFu + ((bits >> 16) & 1)) >> 16);
-        s = s < kScaleTop ? s : kScaleTop;
+        const float s = scale_of(most);
         scale[p] = bad ? 0x7FC0u : __float_as_uint(s) >> 16;
-        const bool none = bad || s == 0.0f;
-        const Borders borders(s);
+        const uint32_t keep = bad ? 0u : s == 0.0f ? 0x88888888u : 0xFFFFFFFFu;
 #pragma unroll
-        for (int r = p * RUNS; r < (p + 1) * RUNS; ++r) {
-            uint32_t v = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v |= (none ? 0u : borders.code(fabsf(x[r][e]))) << (4 * e) | (bad ? 0u : __float_as_uint(x[r][e]) >> 31) << (4 * e + 3);
-            word[r] = v;
-        }
+        for (int r = p * RUNS; r < (p + 1) * RUNS; ++r) word[r] = x[r].codes(s == 0.0f ? 1.0f : s) & keep;
     }
-    *reinterpret_cast<w4u *>(codes + tile * kTileBytes + lane * 16) = w4u{word[0], word[1], word[2], word[3]};
+    reinterpret_cast<w4u *>(codes + tile * kTileBytes)[lane] = word;
     if (g == 0) {
-#pragma unroll
-        for (int p = 0; p < PER; ++p) scales[(tile * kTileRows + n) * PER + p] = (uint16_t)scale[p];
+        uint16_t *to = scales + (tile * kTileRows + n) * PER;
+        if constexpr (PER == 4)
+            *reinterpret_cast<uint2 *>(to) = uint2{scale[0] | scale[1] << 16, scale[2] | scale[3] << 16};
+        else if constexpr (PER == 2)
+            *reinterpret_cast<uint32_t *>(to) = scale[0] | scale[1] << 16;
+        else
+            *to = (uint16_t)scale[0];
     }
 }
 

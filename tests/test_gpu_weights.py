@@ -73,6 +73,46 @@ def test_encode_on_and_next_to_every_border():
     assert np.array_equal(c.cpu().numpy(), codes) and np.array_equal(array(s), scales)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("group", [32, 128])
+def test_encode_16_bits_on_and_next_to_borders(dtype, group):
+    """Every 16-bit number next to every border of many scales: mantissas of the scale, exponents to the ends of the type."""
+    borders = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    rng = np.random.default_rng(5)
+    exps = [-133, -130, -126, -120, -1, 0, 5, 100, 118] if dtype == torch.bfloat16 else [-26, -24, -15, -3, 0, 6, 12]
+    rows = []
+    for e in exps:
+        for m in [1.0, 255 / 128, 129 / 128, 170 / 128] + list(rng.integers(128, 256, 20) / 128):
+            s = m * 2.0 ** e
+            top = torch.tensor(6 * s, dtype=torch.float64).float().to(dtype)  # the group's largest makes the scale
+            if not torch.isfinite(top):
+                continue
+            scale = float(ref.bf16(np.float32(float(top.float())) / np.float32(6)))
+            near = torch.from_numpy(borders * scale).float().to(dtype).view(torch.int16)
+            row = torch.cat([near - 1, near, near + 1]).clamp(min=0).view(dtype)
+            row = torch.where(torch.arange(21) % 2 == 0, row, -row)
+            row = torch.where(row.abs() > top, top, row)
+            rows.append(torch.cat([top.view(1), row, torch.zeros(group - 22, dtype=dtype)]))
+    w = torch.stack(rows)
+    codes, scales = ref.encode(w.float().numpy(), group)
+    c, s = dq8.weights_encode(w.cuda(), group)
+    assert np.array_equal(array(s), scales) and np.array_equal(c.cpu().numpy(), codes)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_encode_16_bits_extremes(dtype):
+    top = torch.finfo(dtype).max
+    w = torch.zeros((16, 256), dtype=dtype)
+    w[0, :5] = torch.tensor([top, -top, top / 2, 1.0, -0.0])
+    w[1, 3], w[1, 40], w[1, 70], w[1, 100] = float("inf"), float("-inf"), float("nan"), 1.0
+    w[2, :] = -0.0
+    w[3, :3] = torch.tensor([1, -32767, 3], dtype=torch.int16).view(dtype)  # subnormal numbers
+    w[4, :64:2] = torch.arange(1, 33, dtype=torch.int16).view(dtype)
+    codes, scales = ref.encode(w.float().numpy(), 32)
+    c, s = dq8.weights_encode(w.cuda(), 32)
+    assert np.array_equal(c.cpu().numpy(), codes) and np.array_equal(array(s), scales, equal_nan=True)
+
+
 def test_encode_extremes():
     top = np.finfo(np.float32).max
     w = np.zeros((16, 256), np.float32)
