@@ -776,7 +776,7 @@ def cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop=None, slo
     stays as it was (granted -1).  tokens: rows of the step, padding among them.
 
     Returns (slots int64 [tokens], positions int64 [tokens], starts int32 [sequences + 1], lens_out, granted, n_free_out): -1 in slots and positions
-    for padding and refused sequences; lens_out may be lens and n_free_out may be n_free."""
+    for padding and refused sequences; lens_out may be lens and n_free_out may be n_free.  (Those that are not handed in may share one allocation.)"""
     done = _native.cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop, slots, positions, starts, lens_out, granted, n_free_out)
     if done is not None:
         return done
