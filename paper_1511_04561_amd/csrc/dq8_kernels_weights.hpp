@@ -467,8 +467,8 @@ constexpr uint32_t kRowPad = 16;  // bytes between the rows of activations in LD
 
 // Up to 4 Q tokens whose rows fit LDS: staged once, and no wavefront waits for another until the end.  A workgroup has a row tile, its
 // wavefronts every KW-th column tile of it, D of them in flight.
-// 28672 x 8192 weights, group 128, one token: 19.8 us, 6.1 TB/s, what loads alone reach; 4096 x 4096, group 32: 4.0 us (kernel start and end, three round trips
-// to memory).  With activations staged in pieces, as below, 21.5 and 4.8.
+// 28672 x 8192 weights, group 128, one token: 19.4 us, 6.2 TB/s, what loads alone reach; 4096 x 4096, group 32: 3.3 us in a graph (kernel start and end, three
+// round trips to memory).  With activations staged in chunks, as below, 21.5 and 4.0.  With more tokens every workgroup stages more than its weights.
 template <typename T, int GROUP, int Q, int KW, int D>
 __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs a)
 {

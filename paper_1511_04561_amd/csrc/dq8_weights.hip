@@ -86,16 +86,14 @@ int decode(const dq8_weights &o, void *w, size_t stride, hipStream_t stream)
     return o.group == 32 ? decode<T, 32>(o, w, stride, stream) : o.group == 64 ? decode<T, 64>(o, w, stride, stream) : decode<T, 128>(o, w, stride, stream);
 }
 
-// What a product launches.
+// What a product launches.  The number behind a name: row tiles of a workgroup.
 enum Form {
-    kFew4, kFew8,      // rows of activations staged whole, up to 4 or 8 tokens; a wavefront has every eighth column tile, ...
-    kFew4Tall,         // ... every fourth where there are many row tiles
-    kOne4, kOne8,      // staged in chunks, up to 4, 8 or ...
-    kOne16,            // ... 16 tokens: one row tile per workgroup, eight wavefronts along the columns,
-    kOne16Wide,        // two row tiles,
-    kOne16Tall,        // four
-    kTwo, kTwoTall,    // up to 32 tokens
-    kFour, kFourTall   // 64 tokens a workgroup
+    kFew16, kFew8, kFew4,          // up to 2 tokens, whole rows of activations staged; 16, 8, 4 wavefronts along the columns
+    kToken4x1, kToken4x2, kToken4x2Short,  // in chunks: up to 4 tokens; 8, 4, 2 wavefronts along the columns
+    kToken8x1, kToken8x2, kToken8x4,       // up to 8; 8, 4, 2
+    kToken16x1, kToken16x2, kToken16x4, kToken16x8,  // up to 16; 8, 4, 2, 1
+    kToken32x4, kToken32x4Short, kToken32x8,         // up to 32; 4, 2, 1
+    kToken64x4, kToken64x8, kToken64x16, kToken64x32 // 64 a workgroup; 2, 1, 1, 1
 };
 
 struct Shape {
@@ -107,26 +105,42 @@ struct Shape {
 
 constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 
-Shape shape_of(const dq8_weights &w, size_t tokens, int cus)
+// With few row tiles wavefronts share one, or compute units stay idle; with many a workgroup has several, for it reads its tokens' activations once for all
+// of them.  us, groups of 32, bfloat16 (in parentheses with other forms):
+//   1 token, 4096 x 8192 kFew16 5.7 (kFew8 6.2), 8192 x 4096 kFew8 5.4 (kFew16 5.9), 28672 x 8192 kFew4 21.6 (kFew8 22.5, in chunks 23.9);
+//   4 tokens, 4096 x 8192 kToken4x1 6.8 (kToken4x2 8.2), 8192 x 8192 kToken4x2 9.0 (10.1, kToken4x2Short 10.7, whole rows staged 9.9), 28672 x 8192
+//   kToken4x2Short 24.3 (kToken4x2 26, whole rows 26); 8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 50016 x 4096 kToken8x4 25.5 (kToken8x2 28);
+//   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 16384 x 4096 kToken16x4 11 (kToken16x2 12.5), 50016 x 4096
+//   kToken16x8 25.9 (kToken16x4 27.5);
+//   32 tokens, 4096 x 4096 kToken32x4 over four splits 10.7 (undivided 18), 16384 x 4096 kToken32x4Short 13.1 (kToken32x4 13.4, kToken32x8 22), 50016 x 4096
+//   kToken32x8 30.8 (kToken32x4Short 42);
+//   64 tokens, 4096 x 4096 kToken64x4 over four splits 12.6 (kToken64x8 14), 28672 x 8192 kToken64x8 50 (kToken64x4 57); 500 tokens, 8192 x 4096 kToken64x16 43
+//   (kToken64x8 54); 2048 tokens kToken64x32 148 (kToken64x16 165).
+Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
 {
-    const Tiles t = tiles_of(w);
-    const size_t few = tokens * (t.cols * 2 * kTileCols + kRowPad);
-    Shape s = {kFour, 8, 64, 128, 1};
-    if (tokens <= 8 && few <= kFewBytes)
-        s = tokens > 4 ? Shape{kFew8, 1, 8, 0, 1} : t.rows > 4 * (size_t)cus ? Shape{kFew4Tall, 1, 4, 0, 1} : Shape{kFew4, 1, 4, 0, 1};
+    const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64;
+    Shape s;
+    if (tokens <= 2 && tokens * (tiles_of(w).cols * 2 * kTileCols + kRowPad) <= kFewBytes)
+        s = rows <= cus ? Shape{kFew16, 1, 4, 0, 1} : rows <= 4 * cus ? Shape{kFew8, 1, 4, 0, 1} : Shape{kFew4, 1, 4, 0, 1};
     else if (tokens <= 4)
-        s = Shape{kOne4, 2, 4, 512, 1};
+        s = rows <= cus ? Shape{kToken4x1, 1, 4, 1024, 1} : rows <= 2 * cus ? Shape{kToken4x2, 2, 4, 512, 1} : Shape{kToken4x2Short, 2, 4, 256, 1};
     else if (tokens <= 8)
-        s = Shape{kOne8, 2, 8, 512, 1};
+        s = rows <= cus ? Shape{kToken8x1, 1, 8, 1024, 1} : rows <= 2 * cus ? Shape{kToken8x2, 2, 8, 512, 1} : Shape{kToken8x4, 4, 8, 256, 1};
     else if (tokens <= 16)
-        s = t.rows >= 8 * (size_t)cus ? Shape{kOne16Tall, 4, 16, 128, 1} : t.rows > (size_t)cus ? Shape{kOne16Wide, 2, 16, 512, 1} : Shape{kOne16, 1, 16, 1024, 1};
+        s = rows <= cus       ? Shape{kToken16x1, 1, 16, 1024, 1}
+            : rows <= 2 * cus ? Shape{kToken16x2, 2, 16, 512, 1}
+            : rows <= 8 * cus ? Shape{kToken16x4, 4, 16, 256, 1}
+                              : Shape{kToken16x8, 8, 16, 128, 1};
     else if (tokens <= 32)
-        s = t.rows >= 4 * (size_t)cus ? Shape{kTwoTall, 4, 32, 256, 1} : Shape{kTwo, 4, 32, 512, 1};
-    else if ((t.rows + 15) / 16 * ((tokens + 63) / 64) >= (size_t)cus)
-        s = Shape{kFourTall, 16, 64, 128, 1};
-    if (s.form == kTwo || s.form == kFour) {
-        const size_t groups = (t.rows + s.row_tiles - 1) / s.row_tiles * ((tokens + s.tokens - 1) / s.tokens), chunks = w.cols / s.columns;
-        size_t splits = (size_t)cus / groups;
+        s = rows <= 2 * cus ? Shape{kToken32x4, 4, 32, 512, 1} : rows <= 4 * cus ? Shape{kToken32x4Short, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
+    else
+        s = (rows + 31) / 32 * blocks >= cus   ? Shape{kToken64x32, 32, 64, 128, 1}
+            : (rows + 15) / 16 * blocks >= cus ? Shape{kToken64x16, 16, 64, 128, 1}
+            : (rows + 3) / 4 * blocks > cus    ? Shape{kToken64x8, 8, 64, 128, 1}
+                                               : Shape{kToken64x4, 4, 64, 256, 1};
+    if (s.form == kToken32x4 || s.form == kToken64x4) {
+        const size_t groups = (rows + s.row_tiles - 1) / s.row_tiles * ((tokens + s.tokens - 1) / s.tokens), chunks = w.cols / s.columns;
+        size_t splits = cus / groups;
         if (splits > chunks / 4) splits = chunks / 4;
         s.splits = splits < 2 ? 1 : (unsigned)splits;
     }
@@ -159,18 +173,26 @@ template <typename T, int GROUP>
 int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t stream)
 {
     switch (form) {
-    case kFew4: return few<T, GROUP, 1, 8, 4>(k, stream);
-    case kFew8: return few<T, GROUP, 2, 8, 2>(k, stream);
-    case kFew4Tall: return few<T, GROUP, 1, 4, 4>(k, stream);
-    case kOne4: return chunks<T, GROUP, 1, 1, 1, 2, 4, 4, 4>(k, split, stream);
-    case kOne8: return chunks<T, GROUP, 1, 2, 1, 2, 4, 4, 4>(k, split, stream);
-    case kOne16: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, split, stream);
-    case kOne16Wide: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
-    case kOne16Tall: return chunks<T, GROUP, 1, 4, 1, 4, 1, 4, 4>(k, split, stream);
-    case kTwo: return chunks<T, GROUP, 2, 4, 2, 2, 4, 2, 2>(k, split, stream);
-    case kTwoTall: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
-    case kFour: return chunks<T, GROUP, 4, 4, 2, 4, 1, 2, 2>(k, split, stream);
-    case kFourTall: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 2>(k, split, stream);
+    case kFew16: return few<T, GROUP, 1, 16, 2>(k, stream);
+    case kFew8: return few<T, GROUP, 1, 8, 2>(k, stream);
+    case kFew4: return few<T, GROUP, 1, 4, 4>(k, stream);
+    case kToken4x1: return chunks<T, GROUP, 1, 1, 1, 1, 8, 2, 4>(k, split, stream);
+    case kToken4x2: return chunks<T, GROUP, 1, 1, 1, 2, 4, 4, 4>(k, split, stream);
+    case kToken4x2Short: return chunks<T, GROUP, 1, 1, 1, 2, 2, 4, 4>(k, split, stream);
+    case kToken8x1: return chunks<T, GROUP, 1, 2, 1, 1, 8, 2, 4>(k, split, stream);
+    case kToken8x2: return chunks<T, GROUP, 1, 2, 1, 2, 4, 4, 4>(k, split, stream);
+    case kToken8x4: return chunks<T, GROUP, 1, 2, 1, 4, 2, 4, 4>(k, split, stream);
+    case kToken16x1: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, split, stream);
+    case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
+    case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 4>(k, split, stream);
+    case kToken16x8: return chunks<T, GROUP, 1, 4, 1, 8, 1, 4, 4>(k, split, stream);
+    case kToken32x4: return chunks<T, GROUP, 2, 4, 2, 2, 4, 2, 2>(k, split, stream);
+    case kToken32x4Short: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
+    case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, split, stream);
+    case kToken64x4: return chunks<T, GROUP, 4, 4, 1, 4, 2, 2, 2>(k, split, stream);
+    case kToken64x8: return chunks<T, GROUP, 4, 4, 1, 8, 1, 2, 2>(k, split, stream);
+    case kToken64x16: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 2>(k, split, stream);
+    case kToken64x32: return chunks<T, GROUP, 4, 4, 4, 8, 1, 2, 1>(k, split, stream);
     }
     return DQ8_OK;
 }

@@ -181,6 +181,62 @@ def test_large_products(rows, cols, group, tokens):
             within(array(dq8.weights_product(x, codes, scales, rows=rows, dtype=to)), array(want), array(size), group, cols, to)
 
 
+@pytest.mark.parametrize("rows", [4096 + 7, 8192 + 16, 16384 + 1, 4 * 4096 + 33, 32768 + 17])
+def test_products_on_both_sides_of_the_choices(rows):
+    """Row counts on the sides of every choice between forms, tokens too; a rest of the columns in most forms' last chunk."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    for cols in (200, 1310):
+        codes, scales = dq8.weights_encode(torch.randn(rows, cols, generator=g, device="cuda"), 32)
+        w = dq8.weights_decode(codes, scales, rows, cols).double()
+        for tokens in (1, 2, 3, 4, 7, 8, 11, 16, 30, 33, 70, 190):
+            x = torch.randn(tokens, cols, generator=g, device="cuda").half()
+            want, size = x.double() @ w.T, x.double().abs() @ w.abs().T
+            within(array(dq8.weights_product(x, codes, scales, rows=rows, dtype=torch.float32)), array(want), array(size), 32, cols, torch.float32)
+
+
+def test_long_rows():
+    """Rows of activations around what is staged whole, and columns divided over workgroups with a rest."""
+    for rows, cols, tokens in ((20, 32760, 1), (20, 32768, 1), (33, 16300, 2), (33, 16400, 2), (40, 40001, 20), (70, 9999, 64), (16, 70000, 1), (300, 5000, 100)):
+        codes, scales = dq8.weights_encode(torch.randn(rows, cols, device="cuda"), 64)
+        w = dq8.weights_decode(codes, scales, rows, cols).double()
+        x = torch.randn(tokens, cols, device="cuda").bfloat16()
+        want, size = array(x.double() @ w.T), array(x.double().abs() @ w.abs().T)
+        within(array(dq8.weights_product(x, codes, scales, rows=rows, dtype=torch.float32)), want, size, 64, cols, torch.float32)
+        none = torch.empty(0, dtype=torch.uint8, device="cuda")
+        within(array(dq8.weights_product(x, codes, scales, rows=rows, dtype=torch.float32, workspace=none)), want, size, 64, cols, torch.float32)
+
+
+def test_workspaces_of_products():
+    codes, scales, w = compressed(200, 9000, 32, 4)
+    x = torch.randn(40, 9000, device="cuda").half()
+    bias = torch.randn(200, device="cuda")
+    n = dq8.weights_product_workspace(x, codes, scales, rows=200)
+    assert n and n % (200 * 40 * 4) == 0 and dq8.weights_product_workspace(x[:16], codes, scales, rows=200) == 0
+    want = dq8.weights_product(x, codes, scales, rows=200, bias=bias)
+    alone = dq8.weights_product(x, codes, scales, rows=200, bias=bias, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    for bytes_, same in ((n, want), (n - 1, alone), (n + 100, want)):
+        space = torch.full((n + 160,), 0xFF, dtype=torch.uint8, device="cuda")
+        got = dq8.weights_product(x, codes, scales, rows=200, bias=bias, workspace=space[16 : 16 + bytes_])
+        assert torch.equal(got, same)
+        assert (space[:16] == 0xFF).all() and (space[16 + n :] == 0xFF).all()
+    # two graphs with a workspace each, one without, replayed in turn
+    graphs = []
+    for space in (torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.uint8, device="cuda"), None):
+        out = torch.zeros_like(want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dq8.weights_product(x, codes, scales, rows=200, bias=bias, out=out, workspace=space)
+        graphs.append((graph, out, space))
+    for seed in range(4):
+        x.copy_(torch.randn(40, 9000, generator=torch.Generator().manual_seed(seed)).half())
+        want = dq8.weights_product(x, codes, scales, rows=200, bias=bias)
+        alone = dq8.weights_product(x, codes, scales, rows=200, bias=bias, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+        for graph, _, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert [torch.equal(out, alone if space is None else want) for _, out, space in graphs] == [True] * 3
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("tokens", [1, 3, 20, 70])
 def test_products_with_strides_and_guards(dtype, tokens):
