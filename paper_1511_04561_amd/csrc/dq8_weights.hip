@@ -92,7 +92,7 @@ enum Form {
     kToken4x1, kToken4x2, kToken4x2Short,  // in chunks: up to 4 tokens; 8, 4, 2 wavefronts along the columns
     kToken8x1, kToken8x2, kToken8x4,       // up to 8; 8, 4, 2
     kToken16x1, kToken16x2, kToken16x4, kToken16x8,  // up to 16; 8, 4, 2, 1
-    kToken32x4, kToken32x4Short, kToken32x8,         // up to 32; 4, 2, 1
+    kToken32x4, kToken32x4Deep, kToken32x8,          // up to 32; 2 (the second with more loads ahead), 1
     kToken64x4, kToken64x8, kToken64x16, kToken64x32 // 64 a workgroup; 2, 1, 1, 1
 };
 
@@ -112,8 +112,8 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 //   kToken4x2Short 24.3 (kToken4x2 26, whole rows 26); 8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 50016 x 4096 kToken8x4 25.5 (kToken8x2 28);
 //   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 16384 x 4096 kToken16x4 11 (kToken16x2 12.5), 50016 x 4096
 //   kToken16x8 25.9 (kToken16x4 27.5);
-//   32 tokens, 4096 x 4096 kToken32x4 over four splits 10.7 (undivided 18), 16384 x 4096 kToken32x4Short 13.1 (kToken32x4 13.4, kToken32x8 22), 50016 x 4096
-//   kToken32x8 30.8 (kToken32x4Short 42);
+//   32 tokens, 4096 x 4096 kToken32x4 over four splits 9.3 (two 9.8), 8192 x 8192 over two 15.3 (kToken32x4Deep 15.6), 16384 x 4096 kToken32x4Deep 13.1
+//   (kToken32x8 22), 50016 x 4096 kToken32x8 30.8 (kToken32x4Deep 42);
 //   64 tokens, 4096 x 4096 kToken64x4 over four splits 12.6 (kToken64x8 14), 28672 x 8192 kToken64x8 50 (kToken64x4 57); 500 tokens, 8192 x 4096 kToken64x16 43
 //   (kToken64x8 54); 2048 tokens kToken64x32 148 (kToken64x16 165).
 Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
@@ -132,7 +132,7 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
             : rows <= 8 * cus ? Shape{kToken16x4, 4, 16, 256, 1}
                               : Shape{kToken16x8, 8, 16, 128, 1};
     else if (tokens <= 32)
-        s = rows <= 2 * cus ? Shape{kToken32x4, 4, 32, 512, 1} : rows <= 4 * cus ? Shape{kToken32x4Short, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
+        s = rows <= 2 * cus ? Shape{kToken32x4, 4, 32, 256, 1} : rows <= 4 * cus ? Shape{kToken32x4Deep, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
     else
         s = (rows + 31) / 32 * blocks >= cus   ? Shape{kToken64x32, 32, 64, 128, 1}
             : (rows + 15) / 16 * blocks >= cus ? Shape{kToken64x16, 16, 64, 128, 1}
@@ -186,8 +186,8 @@ int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t
     case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
     case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 4>(k, split, stream);
     case kToken16x8: return chunks<T, GROUP, 1, 4, 1, 8, 1, 4, 4>(k, split, stream);
-    case kToken32x4: return chunks<T, GROUP, 2, 4, 2, 2, 4, 2, 2>(k, split, stream);
-    case kToken32x4Short: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
+    case kToken32x4: return chunks<T, GROUP, 2, 4, 1, 4, 2, 2, 4>(k, split, stream);
+    case kToken32x4Deep: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
     case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, split, stream);
     case kToken64x4: return chunks<T, GROUP, 4, 4, 1, 4, 2, 2, 2>(k, split, stream);
     case kToken64x8: return chunks<T, GROUP, 4, 4, 1, 8, 1, 2, 2>(k, split, stream);
