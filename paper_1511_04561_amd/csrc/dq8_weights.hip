@@ -191,7 +191,7 @@ int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t
     case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, split, stream);
     case kToken64x4: return chunks<T, GROUP, 4, 4, 1, 4, 2, 2, 2>(k, split, stream);
     case kToken64x8: return chunks<T, GROUP, 4, 4, 1, 8, 1, 2, 2>(k, split, stream);
-    case kToken64x16: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 2>(k, split, stream);
+    case kToken64x16: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 1>(k, split, stream);
     case kToken64x32: return chunks<T, GROUP, 4, 4, 4, 8, 1, 2, 1>(k, split, stream);
     }
     return DQ8_OK;
