@@ -110,8 +110,8 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 //   1 token, 4096 x 8192 kFew16 5.7 (kFew8 6.2), 8192 x 4096 kFew8 5.4 (kFew16 5.9), 28672 x 8192 kFew4 21.6 (kFew8 22.5, in chunks 23.9);
 //   4 tokens, 4096 x 8192 kToken4x1 6.8 (kToken4x2 8.2), 8192 x 8192 kToken4x2 9.0 (10.1, kToken4x2Short 10.7, whole rows staged 9.9), 28672 x 8192
 //   kToken4x2Short 24.3 (kToken4x2 26, whole rows 26); 8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 50016 x 4096 kToken8x4 25.5 (kToken8x2 28);
-//   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 16384 x 4096 kToken16x4 11 (kToken16x2 12.5), 50016 x 4096
-//   kToken16x8 25.9 (kToken16x4 27.5);
+//   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 14336 x 4096 kToken16x4 10 (kToken16x8 13), 50016 x 4096
+//   kToken16x8 24.6 (kToken16x4 27);
 //   32 tokens, 4096 x 4096 kToken32x4 over four splits 9.3 (two 9.8), 8192 x 8192 over two 15.3 (kToken32x4Deep 15.6), 16384 x 4096 kToken32x4Deep 13.1
 //   (kToken32x8 22), 50016 x 4096 kToken32x8 30.8 (kToken32x4Deep 42);
 //   64 tokens, 4096 x 4096 kToken64x4 over four splits 12.6 (kToken64x8 14), 28672 x 8192 kToken64x8 50 (kToken64x4 57); 500 tokens, 8192 x 4096 kToken64x16 43
@@ -184,8 +184,8 @@ int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t
     case kToken8x4: return chunks<T, GROUP, 1, 2, 1, 4, 2, 4, 4>(k, split, stream);
     case kToken16x1: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, split, stream);
     case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
-    case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 4>(k, split, stream);
-    case kToken16x8: return chunks<T, GROUP, 1, 4, 1, 8, 1, 4, 4>(k, split, stream);
+    case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 5>(k, split, stream);
+    case kToken16x8: return chunks<T, GROUP, 1, 4, 1, 8, 1, 2, 8>(k, split, stream);
     case kToken32x4: return chunks<T, GROUP, 2, 4, 1, 4, 2, 2, 4>(k, split, stream);
     case kToken32x4Deep: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
     case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, split, stream);
