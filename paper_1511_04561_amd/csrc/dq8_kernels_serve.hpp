@@ -142,7 +142,9 @@ __device__ __forceinline__ void place_token(const PlanArgs &a, uint32_t i, const
 }
 
 // One workgroup: three sums over the sequences (new tokens; pages given back and taken), then the pages that move, one lane each whatever
-// sequence they belong to.
+// sequence they belong to, then slots and positions of up to a few thousand tokens.  256 sequences of five new tokens: 6.7 us, of which five dependent round
+// trips to memory (requests; pages given back; pages taken; page numbers of the tokens; stores) are the most.  More tokens are placed by k_cache_place: a second launch
+// costs 3 us, one workgroup 0.5 us per thousand tokens.
 __global__ __launch_bounds__(kPlanWg) void k_cache_plan(PlanArgs a)
 {
     __shared__ uint32_t ends[kPlanMost], gone_upto[kPlanMost], need_upto[kPlanMost], had_pages[kPlanMost];
@@ -443,6 +445,8 @@ __device__ __forceinline__ uint32_t first_above(uint32_t run, double mark, doubl
 }
 
 // One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums.
+// 32000 probabilities, ALONE: 7 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
+// needs), then 4.5.  The border between the two (kAloneBytes): a second launch and its verdicts take as long as a compute unit has for 256 KiB.
 template <typename T, bool ALONE>
 __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(VerifyArgs a)
 {

@@ -167,6 +167,7 @@ template <>
 struct Eight<_Float16> : Eight16<_Float16> {};
 
 // A wavefront per tile: lane 16 g + n has of row n the four runs of eight columns that its piece holds.
+// 14336 x 4096 bfloat16, groups of 32: 150 MB in 26 us (memory; 49 us with the bisection of binary32, which is bound by the vector unit).
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void k_weights_encode(const T *__restrict__ w, size_t stride, size_t rows, size_t cols, uint32_t col_tiles, size_t tiles,
                                                         uint8_t *__restrict__ codes, uint16_t *__restrict__ scales)
@@ -221,6 +222,7 @@ __device__ __forceinline__ void two_values(uint32_t word, float &a, float &b)
     b = (float)v.y;
 }
 
+// The reverse, bound by its writes: 26 us.
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void k_weights_decode(const uint8_t *__restrict__ codes, const uint16_t *__restrict__ scales, size_t rows, size_t cols,
                                                         uint32_t col_tiles, size_t tiles, T *__restrict__ w, size_t stride)
@@ -515,6 +517,9 @@ __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs 
 // weights are on their way to registers: both by the same distance, for loads are waited for in the order of their issue.  What a
 // compute unit gets from L2 is about 25 bytes a cycle, of HBM's weights 12: with few row tiles in a workgroup, activations cost more than weights.
 // With `parts` (workspace) the chunks are divided over the workgroups of grid z as well, and k_weights_join adds up their sums.
+// 50021 x 4096, 13 tokens: 25 us of 16.5 that its bytes take (weights' loads alone 21.6; everything else alone 17.9); 4096 x 14336, 20 tokens over four splits: 10.5 us
+// (chunks one after the other: a barrier, LDS, four dependent matrix instructions) and 3 of the join; 8192 x 4096, 500 tokens: 43 us, 780 TFLOP/s (matrix and
+// vector instructions of two wavefronts a SIMD in turn; 32 us without loads).
 struct SplitArgs {
     float *parts;  // [splits][tokens][rows]
     uint32_t splits;
