@@ -39,6 +39,9 @@ __device__ __forceinline__ T scan_wave(T v)
     return v;
 }
 
+// A lane's wavefront, in a scalar register.
+__device__ __forceinline__ uint32_t wave_of(uint32_t thread) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(thread >> 6)); }
+
 // The number of a lane that is the same for all.
 template <typename T>
 __device__ __forceinline__ T of_lane(T v, int lane)
@@ -124,27 +127,42 @@ __device__ __forceinline__ Request request_of(const PlanArgs &a, uint32_t b)
 
 __device__ __forceinline__ uint32_t pages_of(const PlanArgs &a, uint32_t tokens) { return (tokens + (1u << a.page_shift) - 1) >> a.page_shift; }
 
-// Token i of the step: its sequence is the first whose end is behind it.
-__device__ __forceinline__ void place_token(const PlanArgs &a, uint32_t i, const uint32_t *ends, const int32_t *lens, bool ok_by_len)
+// Tokens i0, i0 + step .. of the step, N of them at once: their searches and loads run side by side.  A token's sequence is the first whose end is behind it.
+// len(b): its length after the step, -1 where it is refused.
+template <int N, typename F>
+__device__ __forceinline__ void place_tokens(const PlanArgs &a, uint32_t i0, uint32_t step, const uint32_t *ends, F len)
 {
-    int64_t slot = -1, position = -1;
-    const uint32_t b = not_above(ends, a.batch, i);
-    if (b < a.batch) {
-        const int32_t len = ok_by_len ? lens[b] : a.granted[b] < 0 ? -1 : lens[b];
-        if (len >= 0) {
-            const uint32_t p = (uint32_t)len - (ends[b] - i);
-            position = p;
-            slot = ((int64_t)a.pages[(size_t)b * a.max_pages + (p >> a.page_shift)] << a.page_shift) + (p & ((1u << a.page_shift) - 1));
+    uint32_t b[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) b[k] = 0;
+    for (uint32_t s = 1u << (31 - __builtin_clz(a.batch)); s != 0; s >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const uint32_t at = b[k] + s;
+            if (at <= a.batch && ends[at - 1] <= i0 + k * step) b[k] = at;
         }
+    int64_t position[N];
+    int32_t page[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint32_t c = b[k] < a.batch ? b[k] : a.batch - 1;
+        const int32_t n = len(c);
+        const bool there = b[k] < a.batch && n >= 0;
+        position[k] = there ? (int64_t)n - (ends[c] - (i0 + k * step)) : -1;
+        page[k] = a.pages[(size_t)c * a.max_pages + (there ? (uint32_t)position[k] >> a.page_shift : 0)];
     }
-    a.slots[i] = slot;
-    a.positions[i] = position;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint32_t i = i0 + k * step;
+        if (i >= a.tokens) continue;
+        a.slots[i] = position[k] < 0 ? -1 : ((int64_t)page[k] << a.page_shift) + (position[k] & ((1u << a.page_shift) - 1));
+        a.positions[i] = position[k];
+    }
 }
 
 // One workgroup: three sums over the sequences (new tokens; pages given back and taken), then the pages that move, one lane each whatever
 // sequence they belong to, then slots and positions of up to a few thousand tokens.  256 sequences of five new tokens: 6.7 us, of which five dependent round
-// trips to memory (requests; pages given back; pages taken; page numbers of the tokens; stores) are the most.  More tokens are placed by k_cache_place: a second launch
-// costs 3 us, one workgroup 0.5 us per thousand tokens.
+// trips to memory (requests; pages given back; pages taken; page numbers of the tokens; stores) are the most.  Many tokens are placed by k_cache_place.
 __global__ __launch_bounds__(kPlanWg) void k_cache_plan(PlanArgs a)
 {
     __shared__ uint32_t ends[kPlanMost], gone_upto[kPlanMost], need_upto[kPlanMost], had_pages[kPlanMost];
@@ -217,22 +235,20 @@ __global__ __launch_bounds__(kPlanWg) void k_cache_plan(PlanArgs a)
     if (t == 0) *a.n_free_out = (int32_t)(stock - take);
     if (!a.finish) return;
     __syncthreads();
-    for (uint32_t i = t; i < a.tokens; i += kPlanWg) place_token(a, i, ends, lens, true);
+    for (uint32_t i = t; i < a.tokens; i += kPlanWg) place_tokens<1>(a, i, kPlanWg, ends, [&](uint32_t b) { return lens[b]; });
 }
 
 // Slots and positions of many tokens, behind k_cache_plan.
-constexpr uint32_t kPlaceWg = 256, kPlacePer = 4;
+constexpr uint32_t kPlaceWg = 256;
+constexpr int kPlacePer = 4;  // tokens of a lane
 
 __global__ __launch_bounds__(kPlaceWg) void k_cache_place(PlanArgs a)
 {
     __shared__ uint32_t ends[kPlanMost];
     for (uint32_t b = threadIdx.x; b < a.batch; b += kPlaceWg) ends[b] = (uint32_t)a.starts[b + 1];
     __syncthreads();
-#pragma unroll
-    for (uint32_t k = 0; k < kPlacePer; ++k) {
-        const uint32_t i = (blockIdx.x * kPlacePer + k) * kPlaceWg + threadIdx.x;
-        if (i < a.tokens) place_token(a, i, ends, a.lens_out, false);
-    }
+    const uint32_t i = blockIdx.x * kPlacePer * kPlaceWg + threadIdx.x;
+    if (i < a.tokens) place_tokens<kPlacePer>(a, i, kPlaceWg, ends, [&](uint32_t b) { return a.granted[b] < 0 ? -1 : a.lens_out[b]; });
 }
 
 // ---------------------------------------------------------------- verification
@@ -261,7 +277,7 @@ template <typename T>
 __device__ __forceinline__ float probability(T v)
 {
     const float f = (float)v;
-    return f > 0.0f && f < __builtin_inff() ? f : 0.0f;
+    return __builtin_amdgcn_classf(f, 0x180) ? f : 0.0f;  // positive, subnormal or normal
 }
 
 // Where a sequence ends: rows first .. first + n - 1, `row` of them accepted; refused: whether row `row` refused its draft `token`.
@@ -391,7 +407,10 @@ __device__ __forceinline__ double sum_chunk(const VerifyArgs &a, const Row<T> &r
         double w[kPer];
         row.weights(i, end, w);
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) sum += w[k];
+        for (int d = kPer / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int k = 0; k < d; ++k) w[k] += w[k + d];
+        sum += w[0];
     }
     return scan_wave(sum);
 }
@@ -399,13 +418,16 @@ __device__ __forceinline__ double sum_chunk(const VerifyArgs &a, const Row<T> &r
 template <typename T>
 __global__ __launch_bounds__(kSumsWaves * 64) void k_verify_sums(VerifyArgs a)
 {
-    const uint32_t b = blockIdx.y, c = blockIdx.x * kSumsWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (c >= a.chunks) return;
+    const uint32_t b = blockIdx.y, first = blockIdx.x * kSumsWaves + wave_of(threadIdx.x), lane = threadIdx.x & 63;
+    if (first >= a.chunks) return;
     const Verdict v = verdict_of<T>(a, b);
-    if (c == 0 && lane == 0) a.verdicts[b] = v;
+    if (first == 0 && lane == 0) a.verdicts[b] = v;
     if (v.n == 0) return;
-    const double s = sum_chunk(a, Row<T>(a, v), c);
-    if (lane == 63) a.sums[(size_t)b * a.chunks + c] = s;
+    const Row<T> row(a, v);
+    for (uint32_t c = first; c < a.chunks; c += gridDim.x * kSumsWaves) {
+        const double s = sum_chunk(a, row, c);
+        if (lane == 63) a.sums[(size_t)b * a.chunks + c] = s;
+    }
 }
 
 // Numbers of a wavefront, `run` of a lane in the order of the lanes; next(i): the lane's number i.  The sum before the lane's first one, and of all.
@@ -446,12 +468,12 @@ __device__ __forceinline__ uint32_t first_above(uint32_t run, double mark, doubl
 
 // One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums.
 // 32000 probabilities, ALONE: 7 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
-// needs), then 4.5.  The border between the two (kAloneBytes): a second launch and its verdicts take as long as a compute unit has for 256 KiB.
+// needs), then 4.5. 
 template <typename T, bool ALONE>
 __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(VerifyArgs a)
 {
     __shared__ double sums[kChunksMost];
-    const uint32_t b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t b = blockIdx.x, lane = threadIdx.x & 63, wave = wave_of(threadIdx.x);
     const float r = a.sample[b];
     const Verdict v = ALONE ? verdict_of<T>(a, b) : a.verdicts[b];
     if constexpr (!ALONE)

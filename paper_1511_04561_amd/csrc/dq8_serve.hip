@@ -12,8 +12,9 @@ using dq8::kCacheLimit;
 
 static_assert(kPlanMost == DQ8_PLAN_MAX_BATCH, "LDS of the plan");
 
-// Tokens up to which the plan's own workgroup writes slots and positions.
-constexpr size_t kPlanTokens = 4096;
+// Tokens up to which the plan's own workgroup writes slots and positions; more take a second launch.  us, 16 sequences of 256 tokens each: 6.5 in one (two: 8.7), of 512 8.8
+// (9.1); 256 sequences of 16 9.3 (12.6), of 32 14 (12.9).
+constexpr size_t kPlanTokens = 6144;
 
 struct Array {
     const void *p;
@@ -54,25 +55,31 @@ void cut(const dq8_verify &v, uint32_t &chunk, uint32_t &chunks)
     chunks = (uint32_t)((v.vocab + chunk - 1) / chunk);
 }
 
-// A row of up to this many bytes (with the draft's) is read by one workgroup.
-constexpr size_t kAloneBytes = 256 << 10;
+// Whether one workgroup reads a sequence's whole row, in one launch, or the whole chip and then a wavefront per sequence, in two.  What a compute unit needs for a row
+// grows with its numbers, what the chip needs with the batch.  us, in one | in two launches, binary32 with the draft's probabilities (bfloat16 without):
+//   1 sequence, 32768 probabilities 6.9 | 6.9 (6.0 | 6.7), 65536 10.4 | 7.3 (8.4 | 6.7);  16 of 65536 13.3 | 8.6 (8.7 | 7.1);  64 of 131072 21.9 | 15.9 (14.5 | 11.5);
+//   100 of 131072 22.2 | 19.4 (14.6 | 13.2), of 98304 bfloat16 (12.0 | 12.2);  256 of 131072 36.8 | 36.8 (15.6 | 30).
+bool alone(const dq8_verify &v, int cus) { return v.vocab <= 32768 + 768 * v.batch || v.batch >= (size_t)cus; }
 
 size_t workspace_of(const dq8_verify &v)
 {
     uint32_t chunk, chunks;
     cut(v, chunk, chunks);
-    if (v.vocab * (v.type == DQ8_FLOAT32 ? 4 : 2) * (v.draft ? 2 : 1) <= kAloneBytes) return 0;
     return v.batch * (sizeof(Verdict) + chunks * sizeof(double));
 }
 
 template <typename T>
-int verify(const VerifyArgs &k, hipStream_t stream)
+int verify(const VerifyArgs &k, int cus, hipStream_t stream)
 {
     if (!k.sums) {
         hipLaunchKernelGGL((k_verify_pick<T, true>), dim3(k.batch), dim3(kAloneWaves * 64), 0, stream, k);
         return dq8::after_launch_of("k_verify_pick", stream);
     }
-    hipLaunchKernelGGL(k_verify_sums<T>, dim3((k.chunks + kSumsWaves - 1) / kSumsWaves, k.batch), dim3(kSumsWaves * 64), 0, stream, k);
+    // wavefronts for the whole chip, a chunk at least for each
+    unsigned groups = (k.chunks + kSumsWaves - 1) / kSumsWaves;
+    const unsigned most = (unsigned)cus * 32 / (kSumsWaves * k.batch) + 1;
+    if (groups > most) groups = most;
+    hipLaunchKernelGGL(k_verify_sums<T>, dim3(groups, k.batch), dim3(kSumsWaves * 64), 0, stream, k);
     const int rc = dq8::after_launch_of("k_verify_sums", stream);
     if (rc) return rc;
     hipLaunchKernelGGL((k_verify_pick<T, false>), dim3(k.batch), dim3(64), 0, stream, k);
@@ -125,7 +132,8 @@ int dq8_cache_plan(const dq8_plan *in, void *hip_stream)
 size_t dq8_draft_verify_workspace_bytes(const dq8_verify *v)
 {
     if (check_verify("dq8_draft_verify_workspace_bytes", v) || v->batch == 0 || v->tokens == 0) return 0;
-    return workspace_of(*v);
+    dq8::DeviceTables dev;
+    return dq8::device_tables(0, &dev) || alone(*v, dev.cus) ? 0 : workspace_of(*v);
 }
 
 int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_bytes, void *hip_stream)
@@ -150,13 +158,15 @@ int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_byt
     k.ids = v.ids, k.uniform = v.uniform, k.sample = v.sample, k.starts = v.starts, k.out = v.out, k.accepted = v.accepted, k.rejected = v.rejected;
     k.tokens = (uint32_t)v.tokens, k.batch = (uint32_t)v.batch, k.each = v.starts ? 0 : (uint32_t)(v.tokens / v.batch), k.vocab = (uint32_t)v.vocab;
     cut(v, k.chunk, k.chunks);
-    const size_t needed = v.tokens ? workspace_of(v) : 0;
-    const bool some = needed && workspace && workspace_bytes >= needed;
+    dq8::DeviceTables dev;
+    const int found = dq8::device_tables(0, &dev);
+    if (found) return found;
+    const bool some = v.tokens && workspace && !alone(v, dev.cus) && workspace_bytes >= workspace_of(v);
     k.sums = some ? static_cast<double *>(workspace) : nullptr;
     k.verdicts = some ? reinterpret_cast<Verdict *>(k.sums + v.batch * k.chunks) : nullptr;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (v.type == DQ8_FLOAT32) return verify<float>(k, stream);
-    return v.type == DQ8_BFLOAT16 ? verify<__bf16>(k, stream) : verify<_Float16>(k, stream);
+    if (v.type == DQ8_FLOAT32) return verify<float>(k, dev.cus, stream);
+    return v.type == DQ8_BFLOAT16 ? verify<__bf16>(k, dev.cus, stream) : verify<_Float16>(k, dev.cus, stream);
 }
 
 }  // extern "C"

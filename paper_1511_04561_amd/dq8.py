@@ -826,7 +826,9 @@ def _draft(target, ids, uniform, sample, starts, draft):
 
 def draft_verify_workspace(target, ids, uniform, sample, starts=None, draft=None):
     """Bytes of scratch memory that draft_verify can use for these arguments."""
-    return int(lib().dq8_draft_verify_workspace_bytes(ctypes.byref(_draft(target, ids, uniform, sample, starts, draft))))
+    v = _draft(target, ids, uniform, sample, starts, draft)
+    with torch.cuda.device(target.device):
+        return int(lib().dq8_draft_verify_workspace_bytes(ctypes.byref(v)))
 
 
 def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None, accepted=None, rejected=None, workspace=None):
