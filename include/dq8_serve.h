@@ -36,7 +36,7 @@ extern "C" {
  * order of the sequences, positions[i], the place in its sequence, and slots[i] = page * page_size + place in the page; both are -1 for tokens of
  * refused sequences and behind the last one.  pages and free_pages change in place; entries that nobody needs stay as they were.
  * lens_out may be lens and n_free_out may be n_free: the state then moves on in place.  All other arrays must be apart from each other.
- * page_size: a power of two from 16 to DQ8_CACHE_MAX_PAGE; batch up to DQ8_PLAN_MAX_BATCH; batch * max_pages, max_pages * page_size, tokens and
+ * page_size: a power of two from 16 to DQ8_CACHE_MAX_PAGE; batch from 1 to DQ8_PLAN_MAX_BATCH; batch * max_pages, max_pages * page_size, tokens and
  * free_capacity below 2^31.
  */
 typedef struct {

@@ -9,6 +9,9 @@ namespace {
 
 using dq8::failed;
 
+// Grids of 256 lanes a row tile, or a tile in four, count their lanes in 32 bits.
+constexpr size_t kRowLimit = (size_t)1 << 28, kTileLimit = (size_t)1 << 25;
+
 size_t size_of(int type) { return type == DQ8_FLOAT32 ? 4 : 2; }
 
 struct Tiles {
@@ -31,7 +34,7 @@ int check_weights(const char *who, const dq8_weights *w)
 {
     if (!w) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);
     if (w->group != 32 && w->group != 64 && w->group != 128) return failed(DQ8_ERR_ARG, "%s: group %d is not 32, 64 or 128", who, w->group);
-    if (w->rows >= dq8::kCacheLimit || w->cols >= dq8::kCacheLimit || tiles_of(*w).all >= dq8::kCacheLimit)
+    if (w->rows >= kRowLimit || w->cols >= dq8::kCacheLimit || tiles_of(*w).all >= kTileLimit)
         return failed(DQ8_ERR_ARG, "%s: %zu x %zu weights are too many", who, w->rows, w->cols);
     if (w->rows == 0 || w->cols == 0) return DQ8_OK;
     if (!w->codes || !w->scales) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);

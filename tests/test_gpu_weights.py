@@ -287,6 +287,14 @@ def test_products_of_the_largest_and_smallest_activations():
         x[1, ::2] *= -1
         got = array(dq8.weights_product(x, c, s, dtype=torch.float32))
         within(got, array(x) @ w.T, np.abs(array(x)) @ w.T, 128, cols, torch.float32)
+    # the smallest: an activation times a magnitude is a multiple of 2^-134, and 2^-10 of that one of 2^-144: exact in binary32's subnormal numbers
+    for size in (2.0 ** -125, 2.0 ** -129, 2.0 ** -133):
+        x = torch.full((2, cols), size, dtype=torch.bfloat16, device="cuda")
+        x[1, ::2] *= 3
+        for scale in (1.0, 2.0 ** 60):
+            s2 = torch.full(s.shape, scale).to(torch.bfloat16).cuda()
+            w2 = ref.decode(codes, array(s2), rows, cols)
+            within(array(dq8.weights_product(x, c, s2, dtype=torch.float32)), array(x) @ w2.T, np.abs(array(x)) @ np.abs(w2).T, 128, cols, torch.float32)
     # scales at the ends of their range
     for scale in (170 * 2.0 ** 118, 2.0 ** -133):
         s2 = torch.full(s.shape, scale, dtype=torch.float64).to(torch.bfloat16).cuda()
