@@ -27,6 +27,20 @@ __device__ __forceinline__ float bf16_value(uint32_t bits16) { return __uint_as_
 
 typedef uint16_t w2s __attribute__((ext_vector_type(2)));
 
+// The last elements of a row, fewer than eight, from column k on, zeros behind them: all loads at once (with a branch around each, one would wait for the other).
+template <typename T>
+__device__ __forceinline__ w4u last_eight(const T *row, size_t k, size_t cols)
+{
+    static_assert(sizeof(T) == 2, "bfloat16 or binary16");
+    const uint16_t *bits = reinterpret_cast<const uint16_t *>(row);
+    uint32_t v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = bits[k + e < cols ? k + e : cols - 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k + e < cols ? v[e] : 0;
+    return w4u{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+}
+
 // The scale of a group whose largest absolute value has these bits as binary32: the nearest bfloat16 number to a sixth of it.
 __device__ __forceinline__ float scale_of(uint32_t most)
 {
@@ -58,9 +72,13 @@ struct Eight {
             const V v = *reinterpret_cast<const V *>(row + k);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = v[e];
-        } else {
+        } else if (k < cols) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = k + e < cols ? row[k + e] : 0.0f;
+            for (int e = 0; e < 8; ++e) x[e] = row[k + e < cols ? k + e : cols - 1];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = k + e < cols ? x[e] : 0.0f;
+        } else {
+            clear();
         }
     }
 
@@ -109,13 +127,10 @@ struct Eight16 {
         typedef w4u WA __attribute__((aligned(2)));
         if (k + 8 <= cols) {
             raw = *reinterpret_cast<const WA *>(row + k);
+        } else if (k < cols) {
+            raw = last_eight(row, k, cols);
         } else {
-            typedef T V __attribute__((ext_vector_type(8)));
-            V v = {};
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (k + e < cols) v[e] = row[k + e];
-            __builtin_memcpy(&raw, &v, 16);
+            clear();
         }
     }
 
@@ -456,13 +471,8 @@ __device__ __forceinline__ w4u eight_columns(const T *row, size_t k, uint32_t co
 {
     typedef w4u WA __attribute__((aligned(2)));
     if (k + 8 <= cols) return *reinterpret_cast<const WA *>(row + k);
-    typename Operand<T>::type v = {};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (k + e < cols) v[e] = row[k + e];
-    w4u w;
-    __builtin_memcpy(&w, &v, 16);
-    return w;
+    if (k >= cols) return w4u{0, 0, 0, 0};
+    return last_eight(row, k, cols);
 }
 
 constexpr uint32_t kRowPad = 16;  // bytes between the rows of activations in LDS, so that 16 rows' pieces lie in different banks
