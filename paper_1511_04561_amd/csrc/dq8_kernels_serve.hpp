@@ -161,8 +161,9 @@ __device__ __forceinline__ void place_tokens(const PlanArgs &a, uint32_t i0, uin
 }
 
 // One workgroup: three sums over the sequences (new tokens; pages given back and taken), then the pages that move, one lane each whatever
-// sequence they belong to, then slots and positions of up to a few thousand tokens.  256 sequences of five new tokens: 6.7 us, of which five dependent round
-// trips to memory (requests; pages given back; pages taken; page numbers of the tokens; stores) are the most.  Many tokens are placed by k_cache_place.
+// sequence they belong to, then slots and positions of up to a few thousand tokens.  256 sequences of five new tokens: 6.7 us, of which start, end and
+// four dependent round trips to memory (requests; pages given back; pages taken; page numbers of the tokens) are 4.6, and the instructions of the tokens' searches and stores the
+// rest: one compute unit, 0.6 to 1.2 us per thousand tokens.  So k_cache_place has many.  (512 lanes: 8.1 us; the top of the stack loaded ahead: 7.0.)
 __global__ __launch_bounds__(kPlanWg) void k_cache_plan(PlanArgs a)
 {
     __shared__ uint32_t ends[kPlanMost], gone_upto[kPlanMost], need_upto[kPlanMost], had_pages[kPlanMost];
@@ -245,10 +246,15 @@ constexpr int kPlacePer = 4;  // tokens of a lane
 __global__ __launch_bounds__(kPlaceWg) void k_cache_place(PlanArgs a)
 {
     __shared__ uint32_t ends[kPlanMost];
-    for (uint32_t b = threadIdx.x; b < a.batch; b += kPlaceWg) ends[b] = (uint32_t)a.starts[b + 1];
+    __shared__ int32_t lens[kPlanMost];
+    for (uint32_t b = threadIdx.x; b < a.batch; b += kPlaceWg) {
+        ends[b] = (uint32_t)a.starts[b + 1];
+        const int32_t granted = a.granted[b], len = a.lens_out[b];
+        lens[b] = granted < 0 ? -1 : len;
+    }
     __syncthreads();
     const uint32_t i = blockIdx.x * kPlacePer * kPlaceWg + threadIdx.x;
-    if (i < a.tokens) place_tokens<kPlacePer>(a, i, kPlaceWg, ends, [&](uint32_t b) { return a.granted[b] < 0 ? -1 : a.lens_out[b]; });
+    if (i < a.tokens) place_tokens<kPlacePer>(a, i, kPlaceWg, ends, [&](uint32_t b) { return lens[b]; });
 }
 
 // ---------------------------------------------------------------- verification

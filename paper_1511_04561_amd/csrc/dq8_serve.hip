@@ -12,8 +12,8 @@ using dq8::kCacheLimit;
 
 static_assert(kPlanMost == DQ8_PLAN_MAX_BATCH, "LDS of the plan");
 
-// Tokens up to which the plan's own workgroup writes slots and positions; more take a second launch.  us, 16 sequences of 256 tokens each: 6.5 in one (two: 8.7), of 512 8.8
-// (9.1); 256 sequences of 16 9.3 (12.6), of 32 14 (12.9).
+// Tokens up to which the plan's own workgroup writes slots and positions; more take a second launch.  us, 16 sequences of 256 tokens each: 6.8 in one (two: 7.7), of 512 9
+// (8.1); 256 sequences of 16 9.4 (10.5), of 32 14 (11).
 constexpr size_t kPlanTokens = 6144;
 
 struct Array {
