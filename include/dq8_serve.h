@@ -34,7 +34,8 @@ extern "C" {
  * Written: starts[batch + 1], the sums of new tokens before each sequence, refused ones counted (at most `tokens`); granted[b]: new tokens
  * granted, -1 where refused; lens_out[b]: the length after the step; n_free_out[0]; and for tokens i = 0 .. `tokens` - 1 of the step, packed in the
  * order of the sequences, positions[i], the place in its sequence, and slots[i] = page * page_size + place in the page; both are -1 for tokens of
- * refused sequences and behind the last one.  pages and free_pages change in place; entries that nobody needs stay as they were.
+ * refused sequences and behind the last one (dq8_cache_append stores nothing for such tokens, and their queries and outputs mean nothing).  pages and
+ * free_pages change in place; entries that nobody needs stay as they were.
  * lens_out may be lens and n_free_out may be n_free: the state then moves on in place.  All other arrays must be apart from each other.
  * page_size: a power of two from 16 to DQ8_CACHE_MAX_PAGE; batch from 1 to DQ8_PLAN_MAX_BATCH; batch * max_pages, max_pages * page_size, tokens and
  * free_capacity below 2^31.
@@ -63,6 +64,7 @@ int dq8_cache_plan(const dq8_plan *p, void *hip_stream);
  * a weight where none does (sample[b] of 1 and more; NaN and negative count as 0).  Differences and sums in binary64.
  * Written: out, for each row of a sequence: the accepted tokens, the drawn one, then -1 (the drawn one is -1 too if all its weights are 0); accepted[b]: how
  * many drafts were accepted, -1 for a sequence without rows; rejected[b]: how many were not.  Rows behind the last sequence stay as they were.
+ * batch up to 65535, tokens below 2^31, vocab from 1 to below 2^31 - 4096.
  * starts outside 0 .. tokens count as the nearer end; they must not descend (a sequence whose do has no rows, and rows that two claim hold
  * tokens of either).
  * workspace: dq8_draft_verify_workspace_bytes bytes at a multiple of 16, whose contents are of no meaning before and after; calls that
