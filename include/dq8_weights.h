@@ -27,7 +27,7 @@ extern "C" {
  * multiple of 16 bytes; piece 16 g + n of its 64 pieces of 16 bytes is of row n, and word s of its four words holds the columns 32 s + 8 g ..
  * + 7, four bits each from the lowest on.  scales: bfloat16 [row tiles][column tiles][16 rows][128 / group], at a multiple of 8 bytes.
  * (A wavefront's 64 loads of 16 bytes are one tile, and each of the four words one operand of a matrix instruction whose products share a scale.)
- * rows below 2^28, cols below 2^31, ceil(rows / 16) * ceil(cols / 128) tiles below 2^25.
+ * rows up to 2^28 - 16, cols below 2^31, ceil(rows / 16) * ceil(cols / 128) tiles below 2^25.
  */
 typedef struct {
     uint8_t *codes;

@@ -533,6 +533,7 @@ __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs 
 struct SplitArgs {
     float *parts;  // [splits][tokens][rows]
     uint32_t splits;
+    uint32_t each = 0, more = 0;  // whole chunks of a split, one more in the first `more`
 };
 
 template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC>
@@ -545,7 +546,7 @@ __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductAr
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t kw = wave % KW, row_tile = (blockIdx.x * RW + wave / KW) * R, first = blockIdx.y * TOKENS;
     // this workgroup's whole chunks; the last one has the columns behind them too
-    const uint32_t whole = a.cols / COLS, c0 = (uint32_t)((uint64_t)whole * blockIdx.z / split.splits), c1 = (uint32_t)((uint64_t)whole * (blockIdx.z + 1) / split.splits);
+    const uint32_t whole = a.cols / COLS, z = blockIdx.z, c0 = z * split.each + (z < split.more ? z : split.more), c1 = c0 + split.each + (z < split.more ? 1 : 0);
     const bool rest = whole * COLS < a.cols && blockIdx.z == split.splits - 1;
     const TileSource<GROUP, R> source(a, row_tile);
     float sum[MT][R][Q];

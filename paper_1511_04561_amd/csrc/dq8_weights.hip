@@ -10,7 +10,7 @@ namespace {
 using dq8::failed;
 
 // Grids of 256 lanes a row tile, or a tile in four, count their lanes in 32 bits.
-constexpr size_t kRowLimit = (size_t)1 << 28, kTileLimit = (size_t)1 << 25;
+constexpr size_t kRowLimit = ((size_t)1 << 28) - 16, kTileLimit = (size_t)1 << 25;
 
 size_t size_of(int type) { return type == DQ8_FLOAT32 ? 4 : 2; }
 
@@ -34,7 +34,7 @@ int check_weights(const char *who, const dq8_weights *w)
 {
     if (!w) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);
     if (w->group != 32 && w->group != 64 && w->group != 128) return failed(DQ8_ERR_ARG, "%s: group %d is not 32, 64 or 128", who, w->group);
-    if (w->rows >= kRowLimit || w->cols >= dq8::kCacheLimit || tiles_of(*w).all >= kTileLimit)
+    if (w->rows > kRowLimit || w->cols >= dq8::kCacheLimit || tiles_of(*w).all >= kTileLimit)
         return failed(DQ8_ERR_ARG, "%s: %zu x %zu weights are too many", who, w->rows, w->cols);
     if (w->rows == 0 || w->cols == 0) return DQ8_OK;
     if (!w->codes || !w->scales) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);
@@ -117,11 +117,15 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 //   kToken16x8 24.6 (kToken16x4 27);
 //   32 tokens, 4096 x 4096 kToken32x4 over four splits 9.3 (two 9.8), 8192 x 8192 over two 15.3 (kToken32x4Deep 15.6), 16384 x 4096 kToken32x4Deep 13.1
 //   (kToken32x8 22), 50016 x 4096 kToken32x8 30.8 (kToken32x4Deep 42);
-//   64 tokens, 4096 x 4096 kToken64x4 over four splits 12.6 (kToken64x8 14), 28672 x 8192 kToken64x8 50 (kToken64x4 57); 500 tokens, 8192 x 4096 kToken64x16 43
-//   (kToken64x8 54); 2048 tokens kToken64x32 148 (kToken64x16 165).
+//   64 tokens, 4096 x 4096 kToken64x4 over four splits 12.6 (kToken64x8 14), 28672 x 8192 kToken64x8 50 (kToken64x4 57).
+// From there on what counts is how often the compute units take a workgroup: with 2048 columns kToken64x8 takes 12.5 us a turn and 4.5 once, kToken64x16 24.5 a
+// turn, kToken64x32 43 (groups of 128: 12, 21, 39), and the form whose turns cost least runs: 500 tokens, 8192 rows one turn of kToken64x16 27.6 (two of kToken64x8
+// 28.3, half a one of kToken64x32 42); 700 tokens, 8192 rows kToken64x8 38.7 (kToken64x16 48.5, kToken64x32 42.5); 300, 14336 kToken64x8 37.9 (45.9, 42.1); 200, 28672
+// kToken64x32 43.7 (49.8, 49.3); 1500, 8192 kToken64x16 72.5 (73, kToken64x32 83); 2048, 28672 kToken64x32 306 (380, 347).
 Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
 {
     const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64;
+    auto turns = [&](size_t tiles) { return ((rows + tiles - 1) / tiles * blocks + cus - 1) / cus; };
     Shape s;
     if (tokens <= 2 && tokens * (tiles_of(w).cols * 2 * kTileCols + kRowPad) <= kFewBytes)
         s = rows <= cus ? Shape{kFew16, 1, 4, 0, 1} : rows <= 4 * cus ? Shape{kFew8, 1, 4, 0, 1} : Shape{kFew4, 1, 4, 0, 1};
@@ -136,11 +140,12 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
                               : Shape{kToken16x8, 8, 16, 128, 1};
     else if (tokens <= 32)
         s = rows <= 2 * cus ? Shape{kToken32x4, 4, 32, 256, 1} : rows <= 4 * cus ? Shape{kToken32x4Deep, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
-    else
-        s = (rows + 31) / 32 * blocks >= cus   ? Shape{kToken64x32, 32, 64, 128, 1}
-            : (rows + 15) / 16 * blocks >= cus ? Shape{kToken64x16, 16, 64, 128, 1}
-            : (rows + 3) / 4 * blocks > cus    ? Shape{kToken64x8, 8, 64, 128, 1}
-                                               : Shape{kToken64x4, 4, 64, 256, 1};
+    else if ((rows + 3) / 4 * blocks <= cus)
+        s = Shape{kToken64x4, 4, 64, 256, 1};
+    else {
+        const size_t t8 = 25 * turns(8) + 9, t16 = 49 * turns(16), t32 = 86 * turns(32);
+        s = t32 <= t16 && t32 <= t8 ? Shape{kToken64x32, 32, 64, 128, 1} : t16 <= t8 ? Shape{kToken64x16, 16, 64, 128, 1} : Shape{kToken64x8, 8, 64, 128, 1};
+    }
     if (s.form == kToken32x4 || s.form == kToken64x4) {
         const size_t groups = (rows + s.row_tiles - 1) / s.row_tiles * ((tokens + s.tokens - 1) / s.tokens), chunks = w.cols / s.columns;
         size_t splits = cus / groups;
@@ -287,7 +292,9 @@ int dq8_weights_product(const dq8_weights *w, const dq8_product *in, void *works
     k.wide = p.out_type == DQ8_FLOAT32;
     const Shape s = shape_of(*w, p.tokens, dev.cus);
     const bool some = s.splits > 1 && workspace && workspace_bytes >= workspace_of(*w, p.tokens, s);
-    const SplitArgs split = {some ? static_cast<float *>(workspace) : nullptr, some ? s.splits : 1};
+    SplitArgs split;
+    split.parts = some ? static_cast<float *>(workspace) : nullptr, split.splits = some ? s.splits : 1;
+    if (s.columns) split.each = (uint32_t)(w->cols / s.columns / split.splits), split.more = (uint32_t)(w->cols / s.columns % split.splits);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return p.type == DQ8_BFLOAT16 ? product<__bf16>(w->group, k, s.form, split, stream) : product<_Float16>(w->group, k, s.form, split, stream);
 }

@@ -194,6 +194,17 @@ def test_products_on_both_sides_of_the_choices(rows):
             within(array(dq8.weights_product(x, codes, scales, rows=rows, dtype=torch.float32)), array(want), array(size), 32, cols, torch.float32)
 
 
+@pytest.mark.parametrize("rows,tokens", [(28400, 200), (8200, 300), (8200, 700), (14300, 300), (5000, 1000), (5000, 2000)])
+def test_products_of_many_tokens(rows, tokens):
+    """Each of the forms that the turns of the compute units choose between; a rest of the columns, rows and tokens behind the last tile."""
+    for cols, group in ((300, 32), (640, 128)):
+        codes, scales = dq8.weights_encode(torch.randn(rows, cols, device="cuda"), group)
+        w = dq8.weights_decode(codes, scales, rows, cols).double()
+        x = torch.randn(tokens, cols, device="cuda").bfloat16()
+        want, size = array(x.double() @ w.T), array(x.double().abs() @ w.abs().T)
+        within(array(dq8.weights_product(x, codes, scales, rows=rows)), want, size, group, cols, torch.bfloat16)
+
+
 def test_long_rows():
     """Rows of activations around what is staged whole, and columns divided over workgroups with a rest."""
     for rows, cols, tokens in ((20, 32640, 1), (20, 32760, 1), (4100, 32512, 1), (17000, 16256, 2), (20, 32768, 1), (33, 16300, 2), (33, 16400, 2), (40, 40001, 20), (70, 9999, 64), (16, 70000, 1), (300, 5000, 100)):
