@@ -95,7 +95,7 @@ enum Form {
     kToken4x1, kToken4x2, kToken4x2Short,  // in chunks: up to 4 tokens; 8, 4, 2 wavefronts along the columns
     kToken8x1, kToken8x2, kToken8x4,       // up to 8; 8, 4, 2
     kToken16x1, kToken16x2, kToken16x4, kToken16x8,  // up to 16; 8, 4, 2, 1
-    kToken32x4, kToken32x4Deep, kToken32x8,          // up to 32; 2 (the second with more loads ahead), 1
+    kToken32x2, kToken32x4, kToken32x4Deep, kToken32x8,  // 32 a workgroup; 4, 2 (the last with more loads ahead), 1
     kToken64x4, kToken64x8, kToken64x16, kToken64x32 // 64 a workgroup; 2, 1, 1, 1
 };
 
@@ -115,16 +115,20 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 //   kToken4x2Short 24.3 (kToken4x2 26, whole rows 26); 8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 50016 x 4096 kToken8x4 25.5 (kToken8x2 28);
 //   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 14336 x 4096 kToken16x4 10 (kToken16x8 13), 50016 x 4096
 //   kToken16x8 24.6 (kToken16x4 27);
-//   32 tokens, 4096 x 4096 kToken32x4 over four splits 9.3 (two 9.8), 8192 x 8192 over two 15.3 (kToken32x4Deep 15.6), 16384 x 4096 kToken32x4Deep 13.1
-//   (kToken32x8 22), 50016 x 4096 kToken32x8 30.8 (kToken32x4Deep 42);
-//   64 tokens, 4096 x 4096 kToken64x4 over four splits 12.6 (kToken64x8 14), 28672 x 8192 kToken64x8 50 (kToken64x4 57).
+//   32 tokens, 8192 x 4096 kToken32x2 9.9 (kToken32x4 11.8), 16384 x 4096 kToken32x4Deep 13.1 (kToken32x8 22), 14336 x 8192 20.2 (kToken32x4 21.0), 50016 x 4096
+//   kToken32x8 30.8 (kToken32x4Deep 42);
+//   64 tokens, 4096 x 4096 kToken32x2 9.3 (kToken32x4 11.5, kToken64x4 16.8), 8192 x 8192 kToken32x4 19.8 (kToken32x2 26.6, kToken64x4 28.7): two workgroups that
+//   read the same weights cost less than one whose chunks take twice as long; 96 tokens, 6144 x 8192 kToken64x4 28.8 (kToken32x4 29.4), 2048 columns 10.8 (11.1).
+// Where kToken32x2 leaves half the compute units idle, columns from 6144 on are divided, and from 12288 on for kToken32x4: 32 tokens, 4096 x 8192 over two splits
+// 11.7 (one 13.3; kToken32x4 over four 11.4), 4096 x 4096 9.3 (8.6); 2048 x 8192 over four 9.7 (two 10.8, one 12.8); 4096 x 14336 kToken32x4 over four 15.3 (kToken32x2
+// over two 16.0), 2048 x 28672 over eight 15.6 (over four 16.4).
 // From there on what counts is how often the compute units take a workgroup: with 2048 columns kToken64x8 takes 12.5 us a turn and 4.5 once, kToken64x16 24.5 a
 // turn, kToken64x32 43 (groups of 128: 12, 21, 39), and the form whose turns cost least runs: 500 tokens, 8192 rows one turn of kToken64x16 27.6 (two of kToken64x8
 // 28.3, half a one of kToken64x32 42); 700 tokens, 8192 rows kToken64x8 38.7 (kToken64x16 48.5, kToken64x32 42.5); 300, 14336 kToken64x8 37.9 (45.9, 42.1); 200, 28672
 // kToken64x32 43.7 (49.8, 49.3); 1500, 8192 kToken64x16 72.5 (73, kToken64x32 83); 2048, 28672 kToken64x32 306 (380, 347).
 Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
 {
-    const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64;
+    const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64, blocks32 = (tokens + 31) / 32, pairs = (rows + 1) / 2 * blocks32;
     auto turns = [&](size_t tiles) { return ((rows + tiles - 1) / tiles * blocks + cus - 1) / cus; };
     Shape s;
     if (tokens <= 2 && tokens * (tiles_of(w).cols * 2 * kTileCols + kRowPad) <= kFewBytes)
@@ -138,19 +142,21 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
             : rows <= 2 * cus ? Shape{kToken16x2, 2, 16, 512, 1}
             : rows <= 8 * cus ? Shape{kToken16x4, 4, 16, 256, 1}
                               : Shape{kToken16x8, 8, 16, 128, 1};
+    else if (pairs <= cus)
+        s = pairs <= cus / 2 && w.cols >= 12288 ? Shape{kToken32x4, 4, 32, 256, 1} : Shape{kToken32x2, 2, 32, 512, 1};
     else if (tokens <= 32)
-        s = rows <= 2 * cus ? Shape{kToken32x4, 4, 32, 256, 1} : rows <= 4 * cus ? Shape{kToken32x4Deep, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
+        s = rows <= 4 * cus ? Shape{kToken32x4Deep, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
+    else if ((rows + 3) / 4 * blocks32 <= cus)
+        s = Shape{kToken32x4, 4, 32, 256, 1};
     else if ((rows + 3) / 4 * blocks <= cus)
         s = Shape{kToken64x4, 4, 64, 256, 1};
     else {
         const size_t t8 = 25 * turns(8) + 9, t16 = 49 * turns(16), t32 = 86 * turns(32);
         s = t32 <= t16 && t32 <= t8 ? Shape{kToken64x32, 32, 64, 128, 1} : t16 <= t8 ? Shape{kToken64x16, 16, 64, 128, 1} : Shape{kToken64x8, 8, 64, 128, 1};
     }
-    if (s.form == kToken32x4 || s.form == kToken64x4) {
-        const size_t groups = (rows + s.row_tiles - 1) / s.row_tiles * ((tokens + s.tokens - 1) / s.tokens), chunks = w.cols / s.columns;
-        size_t splits = cus / groups;
-        if (splits > chunks / 4) splits = chunks / 4;
-        s.splits = splits < 2 ? 1 : (unsigned)splits;
+    if (tokens > 16 && pairs <= cus / 2 && w.cols >= 6144) {
+        const size_t idle = cus / ((rows + s.row_tiles - 1) / s.row_tiles * blocks32), most = w.cols / 1024;
+        s.splits = (unsigned)(idle < most ? idle : most);
     }
     return s;
 }
@@ -194,6 +200,7 @@ int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t
     case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
     case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 5>(k, split, stream);
     case kToken16x8: return chunks<T, GROUP, 1, 4, 1, 8, 1, 2, 8>(k, split, stream);
+    case kToken32x2: return chunks<T, GROUP, 2, 4, 1, 2, 4, 2, 4>(k, split, stream);
     case kToken32x4: return chunks<T, GROUP, 2, 4, 1, 4, 2, 2, 4>(k, split, stream);
     case kToken32x4Deep: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
     case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, split, stream);
