@@ -522,12 +522,12 @@ __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs 
     });
 }
 
-// Any number of tokens, 4 Q MT of them in a workgroup (grid y), RW R row tiles; the column tiles are cut into chunks of KW, a wavefront has one tile of a chunk
+// Any number of tokens, 4 Q MT of them in a workgroup (grid y), RW R row tiles (from LEAST R on, by the launch); the column tiles are cut into chunks of KW, a wavefront has one tile of a chunk
 // of R row tiles.  A chunk of the activations is staged in LDS for all wavefronts, one ahead of its use, and D more chunks of activations and
 // weights are on their way to registers: both by the same distance, for loads are waited for in the order of their issue.  What a
 // compute unit gets from L2 is about 25 bytes a cycle, of HBM's weights 12: with few row tiles in a workgroup, activations cost more than weights.
 // With `parts` (workspace) the chunks are divided over the workgroups of grid z as well, and k_weights_join adds up their sums.
-// 50021 x 4096, 13 tokens: 25 us of 16.5 that its bytes take (weights' loads alone 21.6; everything else alone 17.9); 4096 x 14336, 20 tokens over four splits: 10.5 us
+// 50021 x 4096, 13 tokens: 22 us of 16.5 that its bytes take (weights' loads alone 18.8); 4096 x 14336, 20 tokens over four splits: 10.5 us
 // (chunks one after the other: a barrier, LDS, four dependent matrix instructions) and 3 of the join; 8192 x 4096, 500 tokens: 43 us, 780 TFLOP/s (matrix and
 // vector instructions of two wavefronts a SIMD in turn; 32 us without loads).
 struct SplitArgs {
@@ -536,15 +536,16 @@ struct SplitArgs {
     uint32_t each = 0, more = 0;  // whole chunks of a split, one more in the first `more`
 };
 
-template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC>
+template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC, int LEAST>
 __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductArgs a, SplitArgs split)
 {
-    constexpr uint32_t WG = RW * KW * 64, TOKENS = 4 * Q * MT, COLS = KW * kTileCols, BYTES = 2 * COLS, STRIDE = BYTES + kRowPad;
-    constexpr uint32_t PIECES = TOKENS * BYTES / 16, MINE = (PIECES + WG - 1) / WG;
+    constexpr uint32_t TOKENS = 4 * Q * MT, COLS = KW * kTileCols, BYTES = 2 * COLS, STRIDE = BYTES + kRowPad;
+    constexpr uint32_t PIECES = TOKENS * BYTES / 16, FEWEST = LEAST * KW * 64, MINE = (PIECES + FEWEST - 1) / FEWEST;
+    const uint32_t WG = LEAST == RW ? RW * KW * 64 : blockDim.x, rw = LEAST == RW ? RW : WG / (KW * 64);
     constexpr uint32_t STAGED = 2 * TOKENS * STRIDE, JOINED = KW > 1 ? RW * KW * MT * R * Q * 256 : 0;
     __shared__ __align__(16) char lds[STAGED > JOINED ? STAGED : JOINED];
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const uint32_t kw = wave % KW, row_tile = (blockIdx.x * RW + wave / KW) * R, first = blockIdx.y * TOKENS;
+    const uint32_t kw = wave % KW, row_tile = (blockIdx.x * rw + wave / KW) * R, first = blockIdx.y * TOKENS;
     // this workgroup's whole chunks; the last one has the columns behind them too
     const uint32_t whole = a.cols / COLS, z = blockIdx.z, c0 = z * split.each + (z < split.more ? z : split.more), c1 = c0 + split.each + (z < split.more ? 1 : 0);
     const bool rest = whole * COLS < a.cols && blockIdx.z == split.splits - 1;
@@ -576,7 +577,7 @@ __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductAr
     auto place_x = [&](uint32_t buffer, const Pieces &p) {
 #pragma unroll
         for (uint32_t i = 0; i < MINE; ++i)
-            if (PIECES % WG == 0 || threadIdx.x + i * WG < PIECES) *reinterpret_cast<w4u *>(lds + buffer * TOKENS * STRIDE + to[i]) = p.v[i];
+            if ((LEAST == RW && PIECES % FEWEST == 0) || threadIdx.x + i * WG < PIECES) *reinterpret_cast<w4u *>(lds + buffer * TOKENS * STRIDE + to[i]) = p.v[i];
     };
     const uint32_t x = n / (4 / Q) * STRIDE + kw * 2 * kTileCols + g * 16;
     auto work = [&](const TileWords<GROUP, R> &t, uint32_t buffer) { add_tile<T, GROUP, MT, Q, R, 4 * Q * STRIDE>(lds + buffer * TOKENS * STRIDE + x, t, sum); };

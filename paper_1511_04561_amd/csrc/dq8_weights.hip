@@ -89,21 +89,21 @@ int decode(const dq8_weights &o, void *w, size_t stride, hipStream_t stream)
     return o.group == 32 ? decode<T, 32>(o, w, stride, stream) : o.group == 64 ? decode<T, 64>(o, w, stride, stream) : decode<T, 128>(o, w, stride, stream);
 }
 
-// What a product launches.  The number behind a name: row tiles of a workgroup.
+// What a product launches.  The number behind a name: row tiles of a workgroup; with 7 and 13 the most.
 enum Form {
     kFew16, kFew8, kFew4,          // up to 2 tokens, whole rows of activations staged; 16, 8, 4 wavefronts along the columns
-    kToken4x1, kToken4x2, kToken4x2Short,  // in chunks: up to 4 tokens; 8, 4, 2 wavefronts along the columns
-    kToken8x1, kToken8x2, kToken8x4,       // up to 8; 8, 4, 2
-    kToken16x1, kToken16x2, kToken16x4, kToken16x8,  // up to 16; 8, 4, 2, 1
-    kToken32x2, kToken32x4, kToken32x4Deep, kToken32x8,  // 32 a workgroup; 4, 2 (the last with more loads ahead), 1
-    kToken64x4, kToken64x8, kToken64x16, kToken64x32 // 64 a workgroup; 2, 1, 1, 1
+    kToken4x1, kToken4x2, kToken4x2Short, kToken4x7, kToken4x13,  // in chunks: up to 4 tokens; 8, 4, 2, 2, 1 wavefronts along the columns
+    kToken8x1, kToken8x2, kToken8x4, kToken8x7, kToken8x13,       // up to 8; 8, 4, 2, 2, 1
+    kToken16x1, kToken16x2, kToken16x4, kToken16x7, kToken16x13,  // up to 16; 8, 4, 2, 2, 1
+    kToken32x2, kToken32x4, kToken32x4Deep, kToken32x8, kToken32x13,  // 32 a workgroup; 4, 2, 2 (with more loads ahead), 1, 1
+    kToken64x4, kToken64x8, kToken64x16, kToken64x32              // 64 a workgroup; 2, 1, 1, 1
 };
 
 struct Shape {
     Form form;
-    unsigned row_tiles, tokens;  // of a workgroup
-    unsigned columns;            // of a chunk
-    unsigned splits;             // workgroups along the columns, where there is workspace for their sums
+    unsigned row_tiles;  // of a workgroup
+    unsigned columns;    // of a chunk
+    unsigned splits;     // workgroups along the columns, where there is workspace for their sums
 };
 
 constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
@@ -112,11 +112,13 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 // of them.  us, groups of 32, bfloat16 (in parentheses with other forms):
 //   1 token, 4096 x 8192 kFew16 5.7 (kFew8 6.2), 8192 x 4096 kFew8 5.4 (kFew16 5.9), 28672 x 8192 kFew4 21.6 (kFew8 22.5, in chunks 23.9);
 //   4 tokens, 4096 x 8192 kToken4x1 6.8 (kToken4x2 8.2), 8192 x 8192 kToken4x2 9.0 (10.1, kToken4x2Short 10.7, whole rows staged 9.9), 28672 x 8192
-//   kToken4x2Short 24.3 (kToken4x2 26, whole rows 26); 8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 50016 x 4096 kToken8x4 25.5 (kToken8x2 28);
-//   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 14336 x 4096 kToken16x4 10 (kToken16x8 13), 50016 x 4096
-//   kToken16x8 24.6 (kToken16x4 27);
+//   kToken4x7 26.4 (kToken4x2Short 27.7), 50016 x 4096 kToken4x13 22.5 (23.4);
+//   8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 28672 x 8192 kToken8x7 26.5 (kToken8x4 28), 50016 x 4096 kToken8x13 22.9 (26.8);
+//   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 14336 x 4096 kToken16x4 10.2 (kToken16x7 with 7 row tiles 11.8),
+//   20480 x 4096 kToken16x7 with 5 13.0 (kToken16x4 16.2), 32000 x 4096 with 4 15.7 (8 16.6), 50021 x 4096 kToken16x13 23.7 (workgroups of 8 row tiles 26.1);
 //   32 tokens, 8192 x 4096 kToken32x2 9.9 (kToken32x4 11.8), 16384 x 4096 kToken32x4Deep 13.1 (kToken32x8 22), 14336 x 8192 20.2 (kToken32x4 21.0), 50016 x 4096
-//   kToken32x8 30.8 (kToken32x4Deep 42);
+//   kToken32x13 28.3 (kToken32x8 32, kToken32x4Deep 42), 128256 x 4096 kToken32x8 67.5 (kToken32x13 73).
+// A workgroup of 7 or 13 row tiles at most gets as many as make all of a turn alike: some compute units with two and others with one cost what they idle.
 //   64 tokens, 4096 x 4096 kToken32x2 9.3 (kToken32x4 11.5, kToken64x4 16.8), 8192 x 8192 kToken32x4 19.8 (kToken32x2 26.6, kToken64x4 28.7): two workgroups that
 //   read the same weights cost less than one whose chunks take twice as long; 96 tokens, 6144 x 8192 kToken64x4 28.8 (kToken32x4 29.4), 2048 columns 10.8 (11.1).
 // Where kToken32x2 leaves half the compute units idle, columns from 6144 on are divided, and from 12288 on for kToken32x4: 32 tokens, 4096 x 8192 over two splits
@@ -130,29 +132,45 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
 {
     const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64, blocks32 = (tokens + 31) / 32, pairs = (rows + 1) / 2 * blocks32;
     auto turns = [&](size_t tiles) { return ((rows + tiles - 1) / tiles * blocks + cus - 1) / cus; };
+    // row tiles of a workgroup, so that all workgroups of a turn have as many: at most `most` of them
+    auto even = [&](size_t most) {
+        const size_t turn = cus * ((rows + most * cus - 1) / (most * cus));
+        return (unsigned)((rows + turn - 1) / turn);
+    };
     Shape s;
     if (tokens <= 2 && tokens * (tiles_of(w).cols * 2 * kTileCols + kRowPad) <= kFewBytes)
-        s = rows <= cus ? Shape{kFew16, 1, 4, 0, 1} : rows <= 4 * cus ? Shape{kFew8, 1, 4, 0, 1} : Shape{kFew4, 1, 4, 0, 1};
+        s = rows <= cus ? Shape{kFew16, 1, 0, 1} : rows <= 4 * cus ? Shape{kFew8, 1, 0, 1} : Shape{kFew4, 1, 0, 1};
     else if (tokens <= 4)
-        s = rows <= cus ? Shape{kToken4x1, 1, 4, 1024, 1} : rows <= 2 * cus ? Shape{kToken4x2, 2, 4, 512, 1} : Shape{kToken4x2Short, 2, 4, 256, 1};
+        s = rows <= cus       ? Shape{kToken4x1, 1, 1024, 1}
+            : rows <= 2 * cus ? Shape{kToken4x2, 2, 512, 1}
+            : rows <= 4 * cus ? Shape{kToken4x2Short, 2, 256, 1}
+            : rows <= 8 * cus ? Shape{kToken4x7, even(7), 256, 1}
+                              : Shape{kToken4x13, even(13), 128, 1};
     else if (tokens <= 8)
-        s = rows <= cus ? Shape{kToken8x1, 1, 8, 1024, 1} : rows <= 2 * cus ? Shape{kToken8x2, 2, 8, 512, 1} : Shape{kToken8x4, 4, 8, 256, 1};
+        s = rows <= cus       ? Shape{kToken8x1, 1, 1024, 1}
+            : rows <= 2 * cus ? Shape{kToken8x2, 2, 512, 1}
+            : rows <= 4 * cus ? Shape{kToken8x4, 4, 256, 1}
+            : rows <= 8 * cus ? Shape{kToken8x7, even(7), 256, 1}
+                              : Shape{kToken8x13, even(13), 128, 1};
     else if (tokens <= 16)
-        s = rows <= cus       ? Shape{kToken16x1, 1, 16, 1024, 1}
-            : rows <= 2 * cus ? Shape{kToken16x2, 2, 16, 512, 1}
-            : rows <= 8 * cus ? Shape{kToken16x4, 4, 16, 256, 1}
-                              : Shape{kToken16x8, 8, 16, 128, 1};
+        s = rows <= cus       ? Shape{kToken16x1, 1, 1024, 1}
+            : rows <= 2 * cus ? Shape{kToken16x2, 2, 512, 1}
+            : rows <= 4 * cus ? Shape{kToken16x4, 4, 256, 1}
+            : rows <= 8 * cus ? Shape{kToken16x7, even(7), 256, 1}
+                              : Shape{kToken16x13, even(13), 128, 1};
     else if (pairs <= cus)
-        s = pairs <= cus / 2 && w.cols >= 12288 ? Shape{kToken32x4, 4, 32, 256, 1} : Shape{kToken32x2, 2, 32, 512, 1};
+        s = pairs <= cus / 2 && w.cols >= 12288 ? Shape{kToken32x4, 4, 256, 1} : Shape{kToken32x2, 2, 512, 1};
     else if (tokens <= 32)
-        s = rows <= 4 * cus ? Shape{kToken32x4Deep, 4, 32, 256, 1} : Shape{kToken32x8, 8, 32, 128, 1};
+        s = rows <= 4 * cus                          ? Shape{kToken32x4Deep, 4, 256, 1}
+            : rows <= 8 * cus || rows > 13 * cus ? Shape{kToken32x8, 8, 128, 1}
+                                                 : Shape{kToken32x13, even(13), 128, 1};
     else if ((rows + 3) / 4 * blocks32 <= cus)
-        s = Shape{kToken32x4, 4, 32, 256, 1};
+        s = Shape{kToken32x4, 4, 256, 1};
     else if ((rows + 3) / 4 * blocks <= cus)
-        s = Shape{kToken64x4, 4, 64, 256, 1};
+        s = Shape{kToken64x4, 4, 256, 1};
     else {
         const size_t t8 = 25 * turns(8) + 9, t16 = 49 * turns(16), t32 = 86 * turns(32);
-        s = t32 <= t16 && t32 <= t8 ? Shape{kToken64x32, 32, 64, 128, 1} : t16 <= t8 ? Shape{kToken64x16, 16, 64, 128, 1} : Shape{kToken64x8, 8, 64, 128, 1};
+        s = t32 <= t16 && t32 <= t8 ? Shape{kToken64x32, 32, 128, 1} : t16 <= t8 ? Shape{kToken64x16, 16, 128, 1} : Shape{kToken64x8, 8, 128, 1};
     }
     if (tokens > 16 && pairs <= cus / 2 && w.cols >= 6144) {
         const size_t idle = cus / ((rows + s.row_tiles - 1) / s.row_tiles * blocks32), most = w.cols / 1024;
@@ -171,12 +189,12 @@ int few(const ProductArgs &k, hipStream_t stream)
     return dq8::after_launch_of("k_weights_product_few", stream);
 }
 
-template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC>
-int chunks(const ProductArgs &k, const SplitArgs &split, hipStream_t stream)
+template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC, int LEAST = RW>
+int chunks(const ProductArgs &k, uint32_t row_tiles, const SplitArgs &split, hipStream_t stream)
 {
     constexpr uint32_t TOKENS = 4 * Q * MT;
-    hipLaunchKernelGGL((k_weights_product<T, GROUP, MT, Q, R, RW, KW, D, OCC>), dim3((k.row_tiles + R * RW - 1) / (R * RW), (k.tokens + TOKENS - 1) / TOKENS, split.splits),
-                       dim3(RW * KW * 64), 0, stream, k, split);
+    hipLaunchKernelGGL((k_weights_product<T, GROUP, MT, Q, R, RW, KW, D, OCC, LEAST>),
+                       dim3((k.row_tiles + row_tiles - 1) / row_tiles, (k.tokens + TOKENS - 1) / TOKENS, split.splits), dim3(row_tiles / R * KW * 64), 0, stream, k, split);
     const int rc = dq8::after_launch_of("k_weights_product", stream);
     if (rc || split.splits == 1) return rc;
     hipLaunchKernelGGL(k_weights_join<T>, dim3((k.rows + 255) / 256, k.tokens), dim3(256), 0, stream, k, split);
@@ -184,38 +202,45 @@ int chunks(const ProductArgs &k, const SplitArgs &split, hipStream_t stream)
 }
 
 template <typename T, int GROUP>
-int product(const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t stream)
+int product(const ProductArgs &k, const Shape &s, const SplitArgs &split, hipStream_t stream)
 {
-    switch (form) {
+    const uint32_t n = s.row_tiles;
+    switch (s.form) {
     case kFew16: return few<T, GROUP, 1, 16, 2>(k, stream);
     case kFew8: return few<T, GROUP, 1, 8, 2>(k, stream);
     case kFew4: return few<T, GROUP, 1, 4, 4>(k, stream);
-    case kToken4x1: return chunks<T, GROUP, 1, 1, 1, 1, 8, 2, 4>(k, split, stream);
-    case kToken4x2: return chunks<T, GROUP, 1, 1, 1, 2, 4, 4, 4>(k, split, stream);
-    case kToken4x2Short: return chunks<T, GROUP, 1, 1, 1, 2, 2, 4, 4>(k, split, stream);
-    case kToken8x1: return chunks<T, GROUP, 1, 2, 1, 1, 8, 2, 4>(k, split, stream);
-    case kToken8x2: return chunks<T, GROUP, 1, 2, 1, 2, 4, 4, 4>(k, split, stream);
-    case kToken8x4: return chunks<T, GROUP, 1, 2, 1, 4, 2, 4, 4>(k, split, stream);
-    case kToken16x1: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, split, stream);
-    case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, split, stream);
-    case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 5>(k, split, stream);
-    case kToken16x8: return chunks<T, GROUP, 1, 4, 1, 8, 1, 2, 8>(k, split, stream);
-    case kToken32x2: return chunks<T, GROUP, 2, 4, 1, 2, 4, 2, 4>(k, split, stream);
-    case kToken32x4: return chunks<T, GROUP, 2, 4, 1, 4, 2, 2, 4>(k, split, stream);
-    case kToken32x4Deep: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, split, stream);
-    case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, split, stream);
-    case kToken64x4: return chunks<T, GROUP, 4, 4, 1, 4, 2, 2, 2>(k, split, stream);
-    case kToken64x8: return chunks<T, GROUP, 4, 4, 1, 8, 1, 2, 2>(k, split, stream);
-    case kToken64x16: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 1>(k, split, stream);
-    case kToken64x32: return chunks<T, GROUP, 4, 4, 4, 8, 1, 2, 1>(k, split, stream);
+    case kToken4x1: return chunks<T, GROUP, 1, 1, 1, 1, 8, 2, 4>(k, n, split, stream);
+    case kToken4x2: return chunks<T, GROUP, 1, 1, 1, 2, 4, 4, 4>(k, n, split, stream);
+    case kToken4x2Short: return chunks<T, GROUP, 1, 1, 1, 2, 2, 4, 4>(k, n, split, stream);
+    case kToken4x7: return chunks<T, GROUP, 1, 1, 1, 7, 2, 2, 4, 4>(k, n, split, stream);
+    case kToken4x13: return chunks<T, GROUP, 1, 1, 1, 13, 1, 2, 4, 7>(k, n, split, stream);
+    case kToken8x1: return chunks<T, GROUP, 1, 2, 1, 1, 8, 2, 4>(k, n, split, stream);
+    case kToken8x2: return chunks<T, GROUP, 1, 2, 1, 2, 4, 4, 4>(k, n, split, stream);
+    case kToken8x4: return chunks<T, GROUP, 1, 2, 1, 4, 2, 4, 4>(k, n, split, stream);
+    case kToken8x7: return chunks<T, GROUP, 1, 2, 1, 7, 2, 2, 4, 4>(k, n, split, stream);
+    case kToken8x13: return chunks<T, GROUP, 1, 2, 1, 13, 1, 2, 4, 7>(k, n, split, stream);
+    case kToken16x1: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, n, split, stream);
+    case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, n, split, stream);
+    case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 5>(k, n, split, stream);
+    case kToken16x7: return chunks<T, GROUP, 1, 4, 1, 7, 2, 2, 4, 4>(k, n, split, stream);
+    case kToken16x13: return chunks<T, GROUP, 1, 4, 1, 13, 1, 2, 4, 7>(k, n, split, stream);
+    case kToken32x2: return chunks<T, GROUP, 2, 4, 1, 2, 4, 2, 4>(k, n, split, stream);
+    case kToken32x4: return chunks<T, GROUP, 2, 4, 1, 4, 2, 2, 4>(k, n, split, stream);
+    case kToken32x4Deep: return chunks<T, GROUP, 2, 4, 1, 4, 2, 4, 2>(k, n, split, stream);
+    case kToken32x8: return chunks<T, GROUP, 2, 4, 1, 8, 1, 4, 2>(k, n, split, stream);
+    case kToken32x13: return chunks<T, GROUP, 2, 4, 1, 13, 1, 2, 4, 8>(k, n, split, stream);
+    case kToken64x4: return chunks<T, GROUP, 4, 4, 1, 4, 2, 2, 2>(k, n, split, stream);
+    case kToken64x8: return chunks<T, GROUP, 4, 4, 1, 8, 1, 2, 2>(k, n, split, stream);
+    case kToken64x16: return chunks<T, GROUP, 4, 4, 2, 8, 1, 2, 1>(k, n, split, stream);
+    case kToken64x32: return chunks<T, GROUP, 4, 4, 4, 8, 1, 2, 1>(k, n, split, stream);
     }
     return DQ8_OK;
 }
 
 template <typename T>
-int product(int group, const ProductArgs &k, Form form, const SplitArgs &split, hipStream_t stream)
+int product(int group, const ProductArgs &k, const Shape &s, const SplitArgs &split, hipStream_t stream)
 {
-    return group == 32 ? product<T, 32>(k, form, split, stream) : group == 64 ? product<T, 64>(k, form, split, stream) : product<T, 128>(k, form, split, stream);
+    return group == 32 ? product<T, 32>(k, s, split, stream) : group == 64 ? product<T, 64>(k, s, split, stream) : product<T, 128>(k, s, split, stream);
 }
 
 // What looks at sizes and types.  No tokens or rows pass: such a call launches nothing.
@@ -303,7 +328,7 @@ int dq8_weights_product(const dq8_weights *w, const dq8_product *in, void *works
     split.parts = some ? static_cast<float *>(workspace) : nullptr, split.splits = some ? s.splits : 1;
     if (s.columns) split.each = (uint32_t)(w->cols / s.columns / split.splits), split.more = (uint32_t)(w->cols / s.columns % split.splits);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return p.type == DQ8_BFLOAT16 ? product<__bf16>(w->group, k, s.form, split, stream) : product<_Float16>(w->group, k, s.form, split, stream);
+    return p.type == DQ8_BFLOAT16 ? product<__bf16>(w->group, k, s, split, stream) : product<_Float16>(w->group, k, s, split, stream);
 }
 
 }  // extern "C"

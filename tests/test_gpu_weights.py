@@ -205,6 +205,22 @@ def test_products_of_many_tokens(rows, tokens):
         within(array(dq8.weights_product(x, codes, scales, rows=rows)), want, size, group, cols, torch.bfloat16)
 
 
+@pytest.mark.parametrize("rows", [24600, 30001, 45000, 53300, 70001])
+def test_products_of_evenly_divided_rows(rows):
+    """Workgroups with any number of row tiles from 5 to 13, and behind the last row."""
+    cols = 330
+    codes, scales = dq8.weights_encode(torch.randn(rows, cols, device="cuda"), 32)
+    w = dq8.weights_decode(codes, scales, rows, cols).double()
+    bias = torch.randn(rows, device="cuda")
+    for tokens in (3, 8, 15, 32):
+        x = torch.randn(tokens, cols, device="cuda").half()
+        out = torch.full((tokens + 1, rows + 3), 7.0, device="cuda")
+        dq8.weights_product(x, codes, scales, rows=rows, bias=bias, out=out[:tokens, :rows])
+        want, size = array(x.double() @ w.T) + array(bias), array(x.double().abs() @ w.abs().T)
+        within(array(out[:tokens, :rows]), want, size, 32, cols, torch.float32, array(bias))
+        assert (out[tokens] == 7).all() and (out[:, rows:] == 7).all()
+
+
 def test_long_rows():
     """Rows of activations around what is staged whole, and columns divided over workgroups with a rest."""
     for rows, cols, tokens in ((20, 32640, 1), (20, 32760, 1), (4100, 32512, 1), (17000, 16256, 2), (20, 32768, 1), (33, 16300, 2), (33, 16400, 2), (40, 40001, 20), (70, 9999, 64), (16, 70000, 1), (300, 5000, 100)):
