@@ -536,7 +536,7 @@ struct SplitArgs {
     uint32_t each = 0, more = 0;  // whole chunks of a split, one more in the first `more`
 };
 
-template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC, int LEAST>
+template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC, int LEAST = RW>
 __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductArgs a, SplitArgs split)
 {
     constexpr uint32_t TOKENS = 4 * Q * MT, COLS = KW * kTileCols, BYTES = 2 * COLS, STRIDE = BYTES + kRowPad;

@@ -17,6 +17,7 @@ template __global__ void k_weights_product_few<__bf16, 128, 1, 4, 4>(ProductArgs
 template __global__ void k_weights_product_few<__bf16, 32, 1, 8, 2>(ProductArgs);
 template __global__ void k_weights_product<__bf16, 32, 1, 4, 1, 4, 2, 4, 5>(ProductArgs, SplitArgs);
 template __global__ void k_weights_product<__bf16, 32, 4, 4, 2, 8, 1, 2, 1>(ProductArgs, SplitArgs);
+template __global__ void k_weights_product<__bf16, 32, 1, 4, 1, 13, 1, 2, 4, 7>(ProductArgs, SplitArgs);
 """
 
 
@@ -79,7 +80,8 @@ def test_tiles_ahead_stay_on_their_way(start, tiles):
     assert left and min(left) >= 2 * tiles, left
 
 
-@pytest.mark.parametrize("start,least", [("k_weights_productIDF16bLi32ELi1ELi4ELi1ELi4ELi2ELi4ELi5E", 6), ("k_weights_productIDF16bLi32ELi4ELi4ELi2ELi8ELi1ELi2ELi1E", 4)])
+@pytest.mark.parametrize("start,least", [("k_weights_productIDF16bLi32ELi1ELi4ELi1ELi4ELi2ELi4ELi5E", 6), ("k_weights_productIDF16bLi32ELi4ELi4ELi2ELi8ELi1ELi2ELi1E", 4),
+                                         ("k_weights_productIDF16bLi32ELi1ELi4ELi1ELi13ELi1ELi2ELi4E", 3)])
 def test_chunks_ahead_stay_on_their_way(start, least):
     """Where a chunk of activations goes to LDS, behind a barrier in the loop, later chunks' loads are on their way."""
     left = []
