@@ -84,15 +84,13 @@ def test_tiles_ahead_stay_on_their_way(start, tiles):
                                          ("k_weights_productIDF16bLi32ELi1ELi4ELi1ELi13ELi1ELi2ELi4E", 3)])
 def test_chunks_ahead_stay_on_their_way(start, least):
     """Where a chunk of activations goes to LDS, behind a barrier in the loop, later chunks' loads are on their way."""
-    left = []
-    for b in named(start):
-        for i, x in enumerate(b):
-            if x == "s_barrier":
-                waits = [int(m.group(1)) for y in b[i : i + 12] for m in re.finditer(r"vmcnt\((\d+)\)", y)]
-                writes = any(y.startswith("ds_write_b128") for y in b[i : i + 14])
-                if waits and writes and any(y.startswith("global_load") for y in b[i:]):
-                    left.append(waits[0])
-    assert left and min(left) >= least, left
+    left, code = [], [i for b in named(start) for i in b]
+    barriers = [i for i, x in enumerate(code) if x == "s_barrier"] + [len(code)]
+    for first, end in zip(barriers, barriers[1:]):
+        part = code[first:end]
+        if any(y.startswith("v_mfma") for y in part) and any(y.startswith("ds_write_b128") for y in part) and any(y.startswith("global_load") for y in part):
+            left += [int(m.group(1)) for y in part for m in re.finditer(r"vmcnt\((\d+)\)", y)][:1]
+    assert len(left) >= 2 and min(left) >= least, left
 
 
 def test_no_spills():
