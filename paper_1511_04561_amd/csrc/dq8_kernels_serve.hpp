@@ -359,45 +359,50 @@ struct Row {
         less = v.refused && !a.draft ? v.token : -1;
     }
 
-    // The weights of the lane's kPer tokens of kChunk from `begin` on, zeros behind `end`.  What a compute unit does for a number counts where it has a
+    // The weights of the lane's kPer tokens of kChunk from `begin` on, zeros behind `end`: neighbours, or where only their sum counts (APART) 16 bytes from each of
+    // the loads, whose lanes then lie side by side (a row of 32000 in one compute unit: 7.9 -> 7.15 us).  What a compute unit does for a number counts where it has a
     // whole row, so each kind of row has its own steps.  (A branch around each load would make the next wait for it: 16 round trips to memory.)
+    template <bool APART>
     __device__ __forceinline__ void weights(uint32_t begin, uint32_t end, double (&w)[kPer]) const
     {
-        typedef T V __attribute__((ext_vector_type(4)));
+        constexpr int W = 16 / sizeof(T);  // numbers of a load
+        typedef T V __attribute__((ext_vector_type(W)));
         typedef V VA __attribute__((aligned(sizeof(T))));
-        const uint32_t t = begin + (threadIdx.x & 63) * kPer;
-        V x[kPer / 4], y[kPer / 4];
+        constexpr uint32_t STEP = APART ? 64 * W : W;
+        const uint32_t t = begin + (threadIdx.x & 63) * (APART ? W : kPer);
+        auto at = [&](int k) { return t + (uint32_t)(k / W) * STEP + (uint32_t)(k % W); };
+        V x[kPer / W], y[kPer / W];
         if (end - begin >= kChunk) {
 #pragma unroll
-            for (int k = 0; k < kPer / 4; ++k) x[k] = *reinterpret_cast<const VA *>(p + t + 4 * k);
+            for (int k = 0; k < kPer; k += W) x[k / W] = *reinterpret_cast<const VA *>(p + at(k));
             if (q) {
 #pragma unroll
-                for (int k = 0; k < kPer / 4; ++k) y[k] = *reinterpret_cast<const VA *>(q + t + 4 * k);
+                for (int k = 0; k < kPer; k += W) y[k / W] = *reinterpret_cast<const VA *>(q + at(k));
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) x[k / 4][k % 4] = p[t + k < end ? t + k : end - 1];
+            for (int k = 0; k < kPer; ++k) x[k / W][k % W] = p[at(k) < end ? at(k) : end - 1];
             if (q) {
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) y[k / 4][k % 4] = q[t + k < end ? t + k : end - 1];
+                for (int k = 0; k < kPer; ++k) y[k / W][k % W] = q[at(k) < end ? at(k) : end - 1];
             }
 #pragma unroll
             for (int k = 0; k < kPer; ++k)
-                if (t + k >= end) x[k / 4][k % 4] = (T)0.0f;
+                if (at(k) >= end) x[k / W][k % W] = (T)0.0f;
         }
         if (q) {
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
-                const double d = (double)probability(x[k / 4][k % 4]) - (double)probability(y[k / 4][k % 4]);
+                const double d = (double)probability(x[k / W][k % W]) - (double)probability(y[k / W][k % W]);
                 w[k] = __builtin_fmax(d, 0.0);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) w[k] = (double)probability(x[k / 4][k % 4]);
+            for (int k = 0; k < kPer; ++k) w[k] = (double)probability(x[k / W][k % W]);
             if (less >= (int64_t)begin && less < (int64_t)end) {
 #pragma unroll
                 for (int k = 0; k < kPer; ++k)
-                    if ((int64_t)t + k == less) w[k] = 0.0;
+                    if ((int64_t)at(k) == less) w[k] = 0.0;
             }
         }
     }
@@ -411,7 +416,7 @@ __device__ __forceinline__ double sum_chunk(const VerifyArgs &a, const Row<T> &r
     double sum = 0.0;
     for (uint32_t i = begin; i < end; i += kChunk) {
         double w[kPer];
-        row.weights(i, end, w);
+        row.template weights<true>(i, end, w);
 #pragma unroll
         for (int d = kPer / 2; d > 0; d /= 2)
 #pragma unroll
@@ -473,8 +478,8 @@ __device__ __forceinline__ uint32_t first_above(uint32_t run, double mark, doubl
 }
 
 // One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums.
-// 32000 probabilities, ALONE: 7 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
-// needs), then 4.5. 
+// 32000 probabilities, ALONE: 6.0 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
+// needs), then 4.5.
 template <typename T, bool ALONE>
 __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(VerifyArgs a)
 {
@@ -517,7 +522,7 @@ __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(V
         const uint32_t begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
         for (uint32_t i0 = begin; i0 < end; i0 += kChunk) {
             double x[kPer], mine = 0.0;
-            row.weights(i0, end, x);
+            row.template weights<false>(i0, end, x);
 #pragma unroll
             for (int k = 0; k < kPer; ++k) mine += x[k];
             const double upto = scan_wave(mine);
