@@ -91,7 +91,7 @@ int decode(const dq8_weights &o, void *w, size_t stride, hipStream_t stream)
 
 // What a product launches.  The number behind a name: row tiles of a workgroup; with 7 and 13 the most.
 enum Form {
-    kFew16, kFew8, kFew4,          // up to 2 tokens, whole rows of activations staged; 16, 8, 4 wavefronts along the columns
+    kFew16, kFew8, kFew4,          // one token or two, whole rows of activations staged; 16, 8, 4 wavefronts along the columns
     kToken4x1, kToken4x2, kToken4x2Short, kToken4x7, kToken4x13,  // in chunks: up to 4 tokens; 8, 4, 2, 2, 1 wavefronts along the columns
     kToken8x1, kToken8x2, kToken8x4, kToken8x7, kToken8x13,       // up to 8; 8, 4, 2, 2, 1
     kToken16x1, kToken16x2, kToken16x4, kToken16x7, kToken16x13,  // up to 16; 8, 4, 2, 2, 1
@@ -106,11 +106,13 @@ struct Shape {
     unsigned splits;     // workgroups along the columns, where there is workspace for their sums
 };
 
-constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
+constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows; half of it where workgroups share a compute unit
 
 // With few row tiles wavefronts share one, or compute units stay idle; with many a workgroup has several, for it reads its tokens' activations once for all
 // of them.  us, groups of 32, bfloat16 (in parentheses with other forms):
-//   1 token, 4096 x 8192 kFew16 5.7 (kFew8 6.2), 8192 x 4096 kFew8 5.4 (kFew16 5.9), 28672 x 8192 kFew4 21.6 (kFew8 22.5, in chunks 23.9);
+//   1 token, 4096 x 8192 kFew16 5.7 (kFew8 6.2), 8192 x 4096 kFew8 5.4 (kFew16 5.9), 28672 x 8192 kFew4 21.6 (kFew8 22.5, in chunks 22.7), 14336 x 14336 20.5 (21.3),
+//   4096 x 28672 kFew16 12.8 (14.6); in chunks 8192 x 28672 21.4 (kFew8 23.3), 20000 x 28672 59 (kFew4 62); 2 tokens, 4096 x 4096 kFew16 4.3 (in chunks 4.5), in
+//   chunks 28672 x 8192 24.7 (kFew4 27.8), 8192 x 14336 12.3 (kFew8 14.3);
 //   4 tokens, 4096 x 8192 kToken4x1 6.8 (kToken4x2 8.2), 8192 x 8192 kToken4x2 9.0 (10.1, kToken4x2Short 10.7, whole rows staged 9.9), 28672 x 8192
 //   kToken4x7 26.4 (kToken4x2Short 27.7), 50016 x 4096 kToken4x13 22.5 (23.4);
 //   8 tokens, 4096 x 4096 kToken8x1 5.1 (kToken8x2 6.1), 28672 x 8192 kToken8x7 26.5 (kToken8x4 28), 50016 x 4096 kToken8x13 22.9 (26.8);
@@ -127,7 +129,7 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows
 // From there on what counts is how often the compute units take a workgroup: with 2048 columns kToken64x8 takes 12.5 us a turn and 4.5 once, kToken64x16 24.5 a
 // turn, kToken64x32 43 (groups of 128: 12, 21, 39), and the form whose turns cost least runs: 500 tokens, 8192 rows one turn of kToken64x16 27.6 (two of kToken64x8
 // 28.3, half a one of kToken64x32 42); 700 tokens, 8192 rows kToken64x8 38.7 (kToken64x16 48.5, kToken64x32 42.5); 300, 14336 kToken64x8 37.9 (45.9, 42.1); 200, 28672
-// kToken64x32 43.7 (49.8, 49.3); 1500, 8192 kToken64x16 72.5 (73, kToken64x32 83); 2048, 28672 kToken64x32 306 (380, 347).
+// kToken64x32 43.7 (49.8, 49.3); 1500, 8192 kToken64x16 72.5 (73, kToken64x32 83); 2048, 28672 kToken64x32 306 (380, 347); 1024, 28672 x 8192 551 (kToken64x16 597).
 Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
 {
     const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64, blocks32 = (tokens + 31) / 32, pairs = (rows + 1) / 2 * blocks32;
@@ -138,7 +140,8 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
         return (unsigned)((rows + turn - 1) / turn);
     };
     Shape s;
-    if (tokens <= 2 && tokens * (tiles_of(w).cols * 2 * kTileCols + kRowPad) <= kFewBytes)
+    const size_t whole = tokens * (tiles_of(w).cols * 2 * kTileCols + kRowPad);
+    if (rows <= cus ? tokens <= 2 && whole <= kFewBytes : tokens == 1 && whole <= kFewBytes / 2)
         s = rows <= cus ? Shape{kFew16, 1, 0, 1} : rows <= 4 * cus ? Shape{kFew8, 1, 0, 1} : Shape{kFew4, 1, 0, 1};
     else if (tokens <= 4)
         s = rows <= cus       ? Shape{kToken4x1, 1, 1024, 1}
@@ -169,7 +172,7 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
     else if ((rows + 3) / 4 * blocks <= cus)
         s = Shape{kToken64x4, 4, 256, 1};
     else {
-        const size_t t8 = 25 * turns(8) + 9, t16 = 49 * turns(16), t32 = 86 * turns(32);
+        const size_t t8 = 25 * turns(8) + 9, t16 = 49 * turns(16), t32 = 85 * turns(32);
         s = t32 <= t16 && t32 <= t8 ? Shape{kToken64x32, 32, 128, 1} : t16 <= t8 ? Shape{kToken64x16, 16, 128, 1} : Shape{kToken64x8, 8, 128, 1};
     }
     if (tokens > 16 && pairs <= cus / 2 && w.cols >= 6144) {
