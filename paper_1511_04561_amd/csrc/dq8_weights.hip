@@ -125,14 +125,18 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows; half of it where
 //   read the same weights cost less than one whose chunks take twice as long; 96 tokens, 6144 x 8192 kToken64x4 28.8 (kToken32x4 29.4), 2048 columns 10.8 (11.1).
 // Where kToken32x2 leaves half the compute units idle, columns from 6144 on are divided, and from 12288 on for kToken32x4: 32 tokens, 4096 x 8192 over two splits
 // 11.7 (one 13.3; kToken32x4 over four 11.4), 4096 x 4096 9.3 (8.6); 2048 x 8192 over four 9.7 (two 10.8, one 12.8); 4096 x 14336 kToken32x4 over four 15.3 (kToken32x2
-// over two 16.0), 2048 x 28672 over eight 15.6 (over four 16.4).
+// over two 16.0), 2048 x 28672 over eight 15.6 (over four 16.4).  Of 9 to 16 tokens those from 12288 on, for kToken16x4: 4096 x 14336 over four 13.6 (kToken16x1 14.5),
+// 8192 x 14336 over two 17.2 (kToken16x2 19.7), 1024 x 28672 over eight 12.4 (kToken16x1 23.3); 4096 x 8192 10.5 (kToken16x1 9.9).
 // From there on what counts is how often the compute units take a workgroup: with 2048 columns kToken64x8 takes 12.5 us a turn and 4.5 once, kToken64x16 24.5 a
 // turn, kToken64x32 43 (groups of 128: 12, 21, 39), and the form whose turns cost least runs: 500 tokens, 8192 rows one turn of kToken64x16 27.6 (two of kToken64x8
 // 28.3, half a one of kToken64x32 42); 700 tokens, 8192 rows kToken64x8 38.7 (kToken64x16 48.5, kToken64x32 42.5); 300, 14336 kToken64x8 37.9 (45.9, 42.1); 200, 28672
 // kToken64x32 43.7 (49.8, 49.3); 1500, 8192 kToken64x16 72.5 (73, kToken64x32 83); 2048, 28672 kToken64x32 306 (380, 347); 1024, 28672 x 8192 551 (kToken64x16 597).
-Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
+// split: whether there is workspace for divided columns.
+Shape shape_of(const dq8_weights &w, size_t tokens, int cus_, bool split)
 {
-    const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64, blocks32 = (tokens + 31) / 32, pairs = (rows + 1) / 2 * blocks32;
+    const size_t cus = (size_t)cus_, rows = tiles_of(w).rows, blocks = (tokens + 63) / 64, blocks32 = (tokens + 31) / 32;
+    const size_t pairs = (rows + 1) / 2 * blocks32, fours = (rows + 3) / 4 * blocks32;
+    const bool divide = split && (tokens > 16 ? pairs <= cus / 2 && w.cols >= 6144 : tokens > 8 && fours <= cus / 2 && w.cols >= 12288);
     auto turns = [&](size_t tiles) { return ((rows + tiles - 1) / tiles * blocks + cus - 1) / cus; };
     // row tiles of a workgroup, so that all workgroups of a turn have as many: at most `most` of them
     auto even = [&](size_t most) {
@@ -156,18 +160,19 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
             : rows <= 8 * cus ? Shape{kToken8x7, even(7), 256, 1}
                               : Shape{kToken8x13, even(13), 128, 1};
     else if (tokens <= 16)
-        s = rows <= cus       ? Shape{kToken16x1, 1, 1024, 1}
+        s = divide            ? Shape{kToken16x4, 4, 256, 1}
+            : rows <= cus     ? Shape{kToken16x1, 1, 1024, 1}
             : rows <= 2 * cus ? Shape{kToken16x2, 2, 512, 1}
             : rows <= 4 * cus ? Shape{kToken16x4, 4, 256, 1}
             : rows <= 8 * cus ? Shape{kToken16x7, even(7), 256, 1}
                               : Shape{kToken16x13, even(13), 128, 1};
     else if (pairs <= cus)
-        s = pairs <= cus / 2 && w.cols >= 12288 ? Shape{kToken32x4, 4, 256, 1} : Shape{kToken32x2, 2, 512, 1};
+        s = divide && w.cols >= 12288 ? Shape{kToken32x4, 4, 256, 1} : Shape{kToken32x2, 2, 512, 1};
     else if (tokens <= 32)
-        s = rows <= 4 * cus                          ? Shape{kToken32x4Deep, 4, 256, 1}
+        s = rows <= 4 * cus                      ? Shape{kToken32x4Deep, 4, 256, 1}
             : rows <= 8 * cus || rows > 13 * cus ? Shape{kToken32x8, 8, 128, 1}
                                                  : Shape{kToken32x13, even(13), 128, 1};
-    else if ((rows + 3) / 4 * blocks32 <= cus)
+    else if (fours <= cus)
         s = Shape{kToken32x4, 4, 256, 1};
     else if ((rows + 3) / 4 * blocks <= cus)
         s = Shape{kToken64x4, 4, 256, 1};
@@ -175,7 +180,7 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_)
         const size_t t8 = 25 * turns(8) + 9, t16 = 49 * turns(16), t32 = 85 * turns(32);
         s = t32 <= t16 && t32 <= t8 ? Shape{kToken64x32, 32, 128, 1} : t16 <= t8 ? Shape{kToken64x16, 16, 128, 1} : Shape{kToken64x8, 8, 128, 1};
     }
-    if (tokens > 16 && pairs <= cus / 2 && w.cols >= 6144) {
+    if (divide) {
         const size_t idle = cus / ((rows + s.row_tiles - 1) / s.row_tiles * blocks32), most = w.cols / 1024;
         s.splits = (unsigned)(idle < most ? idle : most);
     }
@@ -292,10 +297,10 @@ int dq8_weights_decode(const dq8_weights *in, int type, void *w, size_t row_stri
 
 size_t dq8_weights_product_workspace_bytes(const dq8_weights *w, const dq8_product *p)
 {
-    if (check_product("dq8_weights_product_workspace_bytes", w, p) || w->rows == 0 || p->tokens <= 16) return 0;
+    if (check_product("dq8_weights_product_workspace_bytes", w, p) || w->rows == 0 || p->tokens <= 8) return 0;
     dq8::DeviceTables dev;
     if (dq8::device_tables(0, &dev)) return 0;
-    return workspace_of(*w, p->tokens, shape_of(*w, p->tokens, dev.cus));
+    return workspace_of(*w, p->tokens, shape_of(*w, p->tokens, dev.cus, true));
 }
 
 int dq8_weights_product(const dq8_weights *w, const dq8_product *in, void *workspace, size_t workspace_bytes, void *hip_stream)
@@ -325,11 +330,11 @@ int dq8_weights_product(const dq8_weights *w, const dq8_product *in, void *works
     k.x_stride = p.x_stride, k.out_stride = p.out_stride;
     k.tokens = (uint32_t)p.tokens, k.rows = (uint32_t)w->rows, k.cols = (uint32_t)w->cols, k.row_tiles = (uint32_t)t.rows, k.col_tiles = (uint32_t)t.cols;
     k.wide = p.out_type == DQ8_FLOAT32;
-    const Shape s = shape_of(*w, p.tokens, dev.cus);
-    const bool some = s.splits > 1 && workspace && workspace_bytes >= workspace_of(*w, p.tokens, s);
+    Shape s = shape_of(*w, p.tokens, dev.cus, workspace != nullptr);
+    if (workspace_bytes < workspace_of(*w, p.tokens, s)) s = shape_of(*w, p.tokens, dev.cus, false);
     SplitArgs split;
-    split.parts = some ? static_cast<float *>(workspace) : nullptr, split.splits = some ? s.splits : 1;
-    if (s.columns) split.each = (uint32_t)(w->cols / s.columns / split.splits), split.more = (uint32_t)(w->cols / s.columns % split.splits);
+    split.parts = s.splits > 1 ? static_cast<float *>(workspace) : nullptr, split.splits = s.splits;
+    if (s.columns) split.each = (uint32_t)(w->cols / s.columns / s.splits), split.more = (uint32_t)(w->cols / s.columns % s.splits);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return p.type == DQ8_BFLOAT16 ? product<__bf16>(w->group, k, s, split, stream) : product<_Float16>(w->group, k, s, split, stream);
 }

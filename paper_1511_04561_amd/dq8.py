@@ -720,7 +720,7 @@ def weights_product(x, codes, scales, rows=None, bias=None, dtype=None, out=None
 
     rows: of the weights, where these do not fill their last tile.  dtype: of the result, x's or float32.  workspace: a uint8 tensor of
     weights_product_workspace() bytes; None: taken from torch's allocator, and not while the stream is captured into a graph (hand one in there:
-    without it weights of few rows and more than 16 tokens take longer).  For serving: as with every call here no gradient passes through it."""
+    without it weights of few rows and more than 8 tokens take longer).  For serving: as with every call here no gradient passes through it."""
     done = _native.weights_product(x, codes, scales, rows, bias, dtype, out, workspace)
     if done is not None:
         return done

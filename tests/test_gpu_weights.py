@@ -223,7 +223,7 @@ def test_products_of_evenly_divided_rows(rows):
 
 def test_long_rows():
     """Rows of activations around what is staged whole, and columns divided over workgroups with a rest."""
-    for rows, cols, tokens in ((20, 32640, 1), (20, 32760, 1), (4100, 32512, 1), (17000, 16256, 2), (20, 32768, 1), (33, 16300, 2), (33, 16400, 2), (40, 40001, 20), (70, 9999, 64), (16, 70000, 1), (300, 5000, 100)):
+    for rows, cols, tokens in ((20, 32640, 1), (20, 32760, 1), (4100, 32512, 1), (17000, 16256, 2), (20, 32768, 1), (33, 16300, 2), (33, 16400, 2), (40, 40001, 20), (70, 9999, 64), (40, 40001, 16), (3000, 12300, 9), (16, 70000, 1), (300, 5000, 100)):
         codes, scales = dq8.weights_encode(torch.randn(rows, cols, device="cuda"), 64)
         w = dq8.weights_decode(codes, scales, rows, cols).double()
         x = torch.randn(tokens, cols, device="cuda").bfloat16()
