@@ -384,12 +384,12 @@ struct TileSource {
     }
 };
 
-// A tile's products: x points at the lane's 16 bytes of its row of activations in LDS, 64 bytes from one step to the next and TOKENS_APART bytes
+// A tile's products: the lane's 16 bytes of its row of activations in LDS for each of the four steps are at x + step[.], TOKENS_APART bytes
 // from one token tile to the next.  Products have tokens as rows and weight rows as columns, so that a lane's sums share the scale of its weight
 // row.  A lane has four of the 16 tokens of a token tile; with Q = 2 or 1 every token is there 2 or 4 times, and only one of them is scaled
 // and added up (16 multiply-adds of a tile with groups of 32 become 4: a third of the vector instructions).
 template <typename T, int GROUP, int MT, int Q, int R, int TOKENS_APART>
-__device__ __forceinline__ void add_tile(const char *x, const TileWords<GROUP, R> &t, float (&sum)[MT][R][Q])
+__device__ __forceinline__ void add_tile(const char *x, const uint32_t (&step)[4], const TileWords<GROUP, R> &t, float (&sum)[MT][R][Q])
 {
     constexpr int PER = kTileCols / GROUP, RUNS = 4 / PER;
     typedef Operand<T> Op;
@@ -400,7 +400,7 @@ __device__ __forceinline__ void add_tile(const char *x, const TileWords<GROUP, R
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int k = 0; k < RUNS; ++k) v[m][k] = *reinterpret_cast<const V *>(x + m * TOKENS_APART + (p * RUNS + k) * 64);
+            for (int k = 0; k < RUNS; ++k) v[m][k] = *reinterpret_cast<const V *>(x + m * TOKENS_APART + step[p * RUNS + k]);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             w4f d[MT];
@@ -525,12 +525,13 @@ __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs 
     uint32_t token = n / (4 / Q);
     token = token < a.tokens ? token : a.tokens - 1;
     const char *x = lds + token * stride + g * 16;
+    const uint32_t step[4] = {0, 64, 128, 192};
     __syncthreads();
     for (uint32_t ct = wave; ct < a.col_tiles; ct += D * KW) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
             const uint32_t now = ct + d * KW;
-            if (now < a.col_tiles) add_tile<T, GROUP, 1, Q, 1, 0>(x + now * 2 * kTileCols, t[d], sum);
+            if (now < a.col_tiles) add_tile<T, GROUP, 1, Q, 1, 0>(x + now * 2 * kTileCols, step, t[d], sum);
             source.fetch(inside(now + D * KW), lane, t[d]);  // (without a condition: a branch around loads makes the waits for others wait for all)
         }
     }
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs 
 // compute unit gets from L2 is about 25 bytes a cycle, of HBM's weights 12: with few row tiles in a workgroup, activations cost more than weights.
 // With `parts` (workspace) the chunks are divided over the workgroups of grid z as well, and k_weights_join adds up their sums.
 // 50021 x 4096, 13 tokens: 22 us of 16.5 that its bytes take (weights' loads alone 18.8); 4096 x 14336, 20 tokens over four splits: 10.5 us
-// (chunks one after the other: a barrier, LDS, four dependent matrix instructions) and 3 of the join; 8192 x 4096, 500 tokens: 43 us, 780 TFLOP/s (matrix and
+// (chunks one after the other: a barrier, LDS, four dependent matrix instructions) and 3 of the join; 8192 x 4096, 500 tokens: 42 us, 800 TFLOP/s (matrix and
 // vector instructions of two wavefronts a SIMD in turn; 32 us without loads).
 struct SplitArgs {
     float *parts;  // [splits][tokens][rows]
@@ -557,8 +558,8 @@ struct SplitArgs {
 template <typename T, int GROUP, int MT, int Q, int R, int RW, int KW, int D, int OCC, int LEAST = RW>
 __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductArgs a, SplitArgs split)
 {
-    constexpr uint32_t TOKENS = 4 * Q * MT, COLS = KW * kTileCols, BYTES = 2 * COLS, STRIDE = BYTES + kRowPad;
-    constexpr uint32_t PIECES = TOKENS * BYTES / 16, FEWEST = LEAST * KW * 64, MINE = (PIECES + FEWEST - 1) / FEWEST;
+    constexpr uint32_t TOKENS = 4 * Q * MT, COLS = KW * kTileCols, STRIDE = 2 * COLS;
+    constexpr uint32_t PIECES = TOKENS * STRIDE / 16, FEWEST = LEAST * KW * 64, MINE = (PIECES + FEWEST - 1) / FEWEST;
     const uint32_t WG = LEAST == RW ? RW * KW * 64 : blockDim.x, rw = LEAST == RW ? RW : WG / (KW * 64);
     constexpr uint32_t STAGED = 2 * TOKENS * STRIDE, JOINED = KW > 1 ? RW * KW * MT * R * Q * 256 : 0;
     __shared__ __align__(16) char lds[STAGED > JOINED ? STAGED : JOINED];
@@ -575,14 +576,18 @@ __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductAr
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int q = 0; q < Q; ++q) sum[m][r][q] = 0.0f;
+    // Of a row's pieces in LDS every 16 change places by the row: rows lie 256 bytes or a multiple apart, and the 16 lanes that are served together are of all the
+    // rows of a token tile, some with one g and the others with the next, so that each finds banks of its own (with rows 16 bytes further apart instead 38 to 46 % of the LDS
+    // cycles were conflicts; 64 tokens, 28672 x 8192 49 -> 46.5 us, 512 tokens, 8192 x 8192 81 -> 78).
+    auto turn = [](uint32_t row) { return row * (4 / Q) & 15; };
     // a thread's pieces of a chunk: 16 bytes of a token (behind the last one: of the last one again; nobody looks at its results)
     const T *from[MINE];
     uint32_t to[MINE];
 #pragma unroll
     for (uint32_t i = 0; i < MINE; ++i) {
-        const uint32_t at = threadIdx.x + i * WG, m = at / (BYTES / 16) % TOKENS, c = at % (BYTES / 16), token = first + m < a.tokens ? first + m : a.tokens - 1;
+        const uint32_t at = threadIdx.x + i * WG, m = at / (STRIDE / 16) % TOKENS, c = at % (STRIDE / 16), token = first + m < a.tokens ? first + m : a.tokens - 1;
         from[i] = static_cast<const T *>(a.x) + token * a.x_stride + c * 8;
-        to[i] = m * STRIDE + c * 16;
+        to[i] = m * STRIDE + (c ^ turn(m)) * 16;
     }
     struct Pieces {
         w4u v[MINE];
@@ -597,8 +602,10 @@ __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductAr
         for (uint32_t i = 0; i < MINE; ++i)
             if ((LEAST == RW && PIECES % FEWEST == 0) || threadIdx.x + i * WG < PIECES) *reinterpret_cast<w4u *>(lds + buffer * TOKENS * STRIDE + to[i]) = p.v[i];
     };
-    const uint32_t x = n / (4 / Q) * STRIDE + kw * 2 * kTileCols + g * 16;
-    auto work = [&](const TileWords<GROUP, R> &t, uint32_t buffer) { add_tile<T, GROUP, MT, Q, R, 4 * Q * STRIDE>(lds + buffer * TOKENS * STRIDE + x, t, sum); };
+    uint32_t step[4];
+#pragma unroll
+    for (uint32_t s = 0; s < 4; ++s) step[s] = n / (4 / Q) * STRIDE + kw * 2 * kTileCols + ((4 * s + g) ^ turn(n / (4 / Q))) * 16;
+    auto work = [&](const TileWords<GROUP, R> &t, uint32_t buffer) { add_tile<T, GROUP, MT, Q, R, 4 * Q * STRIDE>(lds + buffer * TOKENS * STRIDE, step, t, sum); };
 
     TileWords<GROUP, R> t_rest = {};
     Pieces x_rest = {};
@@ -606,7 +613,7 @@ __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductAr
         if (whole * KW + kw < a.col_tiles) source.fetch(whole * KW + kw, lane, t_rest);
 #pragma unroll
         for (uint32_t i = 0; i < MINE; ++i) {
-            const uint32_t c = (threadIdx.x + i * WG) % (BYTES / 16) * 8;
+            const uint32_t c = (threadIdx.x + i * WG) % (STRIDE / 16) * 8;
             x_rest.v[i] = eight_of_rest(from[i] - c, (size_t)whole * COLS + c, a.cols);
         }
     }
