@@ -698,14 +698,9 @@ bool fresh(at::Tensor &made, at::IntArrayRef sizes, const at::Tensor &like, at::
     return !made.key_set().has_any(kTransformed);
 }
 
-// A contiguous array of one axis with n elements on `like`'s device: the one handed in or, where that is allowed, a new one.
-bool axis(PyObject *o, at::ScalarType type, size_t n, const at::Tensor &like, void *&ptr, at::Tensor *made = nullptr)
+// A contiguous array of one axis with n elements on `like`'s device.
+bool axis(PyObject *o, at::ScalarType type, size_t n, const at::Tensor &like, void *&ptr)
 {
-    if (made && o == Py_None) {
-        if (!fresh(*made, {(int64_t)n}, like, type)) return false;
-        ptr = made->data_ptr();
-        return true;
-    }
     Buffer b;
     if (!buffer(o, type, b) || b.t->dim() != 1 || b.n != n || b.t->get_device() != like.get_device()) return false;
     ptr = b.ptr;
@@ -935,9 +930,25 @@ PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, sta
     v.type = target.type, v.tokens = target.rows, v.vocab = target.cols, v.batch = sample.n;
     v.target = target.ptr, v.target_stride = target.stride, v.draft = draft.ptr, v.draft_stride = draft.stride;
     if (!axis(a[1], at::kLong, v.tokens, like, p[0]) || !axis(a[2], at::kFloat, v.tokens, like, p[1]) ||
-        (a[4] != Py_None && !axis(a[4], at::kInt, v.batch + 1, like, p[2])) || !axis(a[6], at::kLong, v.tokens, like, p[3], &made[0]) ||
-        !axis(a[7], at::kInt, v.batch, like, p[4], &made[1]) || !axis(a[8], at::kInt, v.batch, like, p[5], &made[2]))
+        (a[4] != Py_None && !axis(a[4], at::kInt, v.batch + 1, like, p[2])))
         return declined();
+    PyObject *const given[3] = {a[6], a[7], a[8]};
+    const size_t n[3] = {v.tokens, v.batch, v.batch};
+    size_t bytes = 0;
+    for (int i = 0; i < 3; ++i) {
+        const at::ScalarType type = i == 0 ? at::kLong : at::kInt;
+        if (given[i] == Py_None)
+            bytes += Outputs::padded(n[i] * at::elementSize(type));
+        else if (!axis(given[i], type, n[i], like, p[3 + i]))
+            return declined();
+    }
+    Outputs outputs;
+    if (!outputs.open(bytes, like)) return declined();
+    for (int i = 0; i < 3; ++i)
+        if (given[i] == Py_None) {
+            made[i] = outputs.next(n[i], i == 0 ? at::kLong : at::kInt);
+            p[3 + i] = made[i].data_ptr();
+        }
     v.ids = static_cast<int64_t *>(p[0]), v.uniform = static_cast<float *>(p[1]), v.sample = static_cast<float *>(sample.ptr);
     v.starts = static_cast<int32_t *>(p[2]), v.out = static_cast<int64_t *>(p[3]), v.accepted = static_cast<int32_t *>(p[4]), v.rejected = static_cast<int32_t *>(p[5]);
     Scratch scratch;
@@ -949,7 +960,6 @@ PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, sta
         scratch.bytes = space.n;
     }
     if (!enqueue("dq8_draft_verify", [&] { return g_lib.draft_verify(&v, scratch.ptr, scratch.bytes, stream); })) return nullptr;
-    PyObject *const given[3] = {a[6], a[7], a[8]};
     return tuple_of(given, made);
 }
 
