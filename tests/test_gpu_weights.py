@@ -150,6 +150,17 @@ def test_encode_and_decode_with_strides_and_guards(dtype):
     assert (band[:32] == 9).all() and (band[-32:] == 9).all() and (sband[:16] == 9).all() and (sband[-16:] == 9).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols,stride,offset", [(40, 128, 129, 0), (33, 128, 128, 1), (16, 256, 257, 1), (50, 127, 127, 0), (20, 8, 9, 1), (35, 131, 133, 3), (17, 391, 392, 5), (3, 1, 1, 1)])
+def test_encode_of_rows_that_start_between_words(rows, cols, stride, offset, dtype):
+    flat = torch.randn(offset + (rows - 1) * stride + cols, device="cuda").to(dtype)
+    view = flat[offset:].as_strided((rows, cols), (stride, 1))
+    for group in (32, 64, 128):
+        c, s = dq8.weights_encode(view, group)
+        codes, scales = ref.encode(array(view).astype(np.float32), group)
+        assert np.array_equal(c.cpu().numpy(), codes) and np.array_equal(array(s), scales)
+
+
 @pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5, 8, 13, 16, 17, 31, 32, 33, 48, 64, 65, 130])
 @pytest.mark.parametrize("rows,cols,group", [(16, 128, 32), (37, 300, 32), (130, 1025, 64), (200, 2048, 128), (5, 7, 64)])
 def test_products(tokens, rows, cols, group):
