@@ -55,11 +55,19 @@ void cut(const dq8_verify &v, uint32_t &chunk, uint32_t &chunks)
     chunks = (uint32_t)((v.vocab + chunk - 1) / chunk);
 }
 
-// Whether one workgroup reads a sequence's whole row, in one launch, or the whole chip and then a wavefront per sequence, in two.  What a compute unit needs for a row
-// grows with its numbers, what the chip needs with the batch.  us, in one | in two launches, binary32 with the draft's probabilities (bfloat16 without):
-//   1 sequence, 32768 probabilities 6.9 | 6.9 (6.0 | 6.7), 65536 10.4 | 7.3 (8.4 | 6.7);  16 of 65536 13.3 | 8.6 (8.7 | 7.1);  64 of 131072 21.9 | 15.9 (14.5 | 11.5);
-//   100 of 131072 22.2 | 19.4 (14.6 | 13.2), of 98304 bfloat16 (12.0 | 12.2);  256 of 131072 36.8 | 36.8 (15.6 | 30).
-bool alone(const dq8_verify &v, int cus) { return v.vocab <= 32768 + 768 * v.batch || v.batch >= (size_t)cus; }
+// Whether one workgroup reads a sequence's whole row, in one launch, or the whole chip and then a wavefront per sequence, in two: ns that each takes.  What a compute unit
+// needs for a row grows with its numbers, what the chip needs with all of them.  us from Python, in one | in two launches, four tokens of each sequence:
+//   binary32 with the draft's probabilities, 8 sequences of 32768 7.7 | 8.2, 50021 9.7 | 8.3, 65536 11.0 | 8.0; 64 of 100000 16.6 | 14.1, 131072 19.8 | 16.6; 128 of 131072
+//   22.9, bfloat16 20.7; binary32 without, 8 of 50021 7.6 | 8.3, 65536 8.5 | 8.1, 131072 12.8 | 8.0; 64 of 131072 13.8 | 11.2.  (In a graph two launches are a
+//   microsecond cheaper: one sequence of 32768 with draft 6.9 | 6.9, of 65536 bfloat16 without 8.4 | 6.7; 256 of 131072 bfloat16 without 15.6 | 30.)
+bool alone(const dq8_verify &v, int cus)
+{
+    uint32_t chunk, chunks;
+    cut(v, chunk, chunks);
+    const size_t bytes = (v.type == DQ8_FLOAT32 ? 4 : 2) * (v.draft ? 2 : 1), waves = v.batch * chunks;
+    const size_t one = (v.draft ? 4500 + v.vocab / 10 : 4200 + v.vocab * 13 / 200) + waves * bytes / 28, two = 8000 + (waves > 2048 ? (waves - 2048) * (bytes + 1) / 8 : 0);
+    return one <= two || v.batch >= (size_t)cus;
+}
 
 size_t workspace_of(const dq8_verify &v)
 {
