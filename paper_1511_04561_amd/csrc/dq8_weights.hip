@@ -100,9 +100,9 @@ int decode(const dq8_weights &o, void *w, size_t stride, hipStream_t stream)
 // What a product launches.  The number behind a name: row tiles of a workgroup; with 7 and 13 the most.
 enum Form {
     kFew16, kFew8, kFew4,          // one token or two, whole rows of activations staged; 16, 8, 4 wavefronts along the columns
-    kToken4x1, kToken4x2, kToken4x2Short, kToken4x7, kToken4x13,  // in chunks: up to 4 tokens; 8, 4, 2, 2, 1 wavefronts along the columns
-    kToken8x1, kToken8x2, kToken8x4, kToken8x7, kToken8x13,       // up to 8; 8, 4, 2, 2, 1
-    kToken16x1, kToken16x2, kToken16x4, kToken16x7, kToken16x13,  // up to 16; 8, 4, 2, 2, 1
+    kToken4x1, kToken4x2, kToken4x3, kToken4x2Short, kToken4x7, kToken4x13,  // in chunks: up to 4 tokens; 8, 4, 4, 2, 2, 1 wavefronts along the columns
+    kToken8x1, kToken8x2, kToken8x3, kToken8x4, kToken8x7, kToken8x13,       // up to 8; 8, 4, 4, 2, 2, 1
+    kToken16x1, kToken16x2, kToken16x3, kToken16x4, kToken16x7, kToken16x13,  // up to 16; 8, 4, 4, 2, 2, 1
     kToken32x2, kToken32x4, kToken32x4Deep, kToken32x8, kToken32x13,  // 32 a workgroup; 4, 2, 2 (with more loads ahead), 1, 1
     kToken64x4, kToken64x8, kToken64x16, kToken64x32              // 64 a workgroup; 2, 1, 1, 1
 };
@@ -127,10 +127,12 @@ constexpr size_t kFewBytes = 65536;  // of LDS, for whole rows; half of it where
 //   13 tokens, 4096 x 4096 kToken16x1 6.4 (kToken16x2 6.5), 8192 x 8192 kToken16x2 10.4 (kToken16x4 14), 14336 x 4096 kToken16x4 10.2 (kToken16x7 with 7 row tiles 11.8),
 //   20480 x 4096 kToken16x7 with 5 13.0 (kToken16x4 16.2), 32000 x 4096 with 4 15.7 (8 16.6), 50021 x 4096 kToken16x13 23.7 (workgroups of 8 row tiles 26.1);
 //   32 tokens, 8192 x 4096 kToken32x2 9.9 (kToken32x4 11.8), 16384 x 4096 kToken32x4Deep 13.1 (kToken32x8 22), 14336 x 8192 20.2 (kToken32x4 21.0), 50016 x 4096
-//   kToken32x13 28.3 (kToken32x8 32, kToken32x4Deep 42), 128256 x 4096 kToken32x8 67.5 (kToken32x13 73).
-// A workgroup of 7 or 13 row tiles at most gets as many as make all of a turn alike: some compute units with two and others with one cost what they idle.
+//   kToken32x13 28.3 (kToken32x8 32, kToken32x4Deep 42), 128256 x 4096 kToken32x8 67.5 (kToken32x13 73);
 //   64 tokens, 4096 x 4096 kToken32x2 9.3 (kToken32x4 11.5, kToken64x4 16.8), 8192 x 8192 kToken32x4 19.8 (kToken32x2 26.6, kToken64x4 28.7): two workgroups that
 //   read the same weights cost less than one whose chunks take twice as long; 96 tokens, 6144 x 8192 kToken64x4 28.8 (kToken32x4 29.4), 2048 columns 10.8 (11.1).
+// A workgroup of 7 or 13 row tiles at most gets as many as make all of a turn alike: some compute units with two and others with one cost what they idle.  (So do three
+// row tiles where there are up to three for each compute unit: 7 tokens, 9944 x 23552 kToken8x3 27.7 (kToken8x4 33, kToken8x2 35), 13 tokens 30.3 (38.6, 42), 4 tokens
+// 27.1 (kToken4x2Short 33.7); 7 tokens, 11008 x 4096 7.9 (8.5).)
 // Where kToken32x2 leaves half the compute units idle, columns from 6144 on are divided, and from 12288 on for kToken32x4: 32 tokens, 4096 x 8192 over two splits
 // 11.7 (one 13.3; kToken32x4 over four 11.4), 4096 x 4096 9.3 (8.6); 2048 x 8192 over four 9.7 (two 10.8, one 12.8); 4096 x 14336 kToken32x4 over four 15.3 (kToken32x2
 // over two 16.0), 2048 x 28672 over eight 15.6 (over four 16.4).  Of 9 to 16 tokens those from 12288 on, for kToken16x4: 4096 x 14336 over four 13.6 (kToken16x1 14.5),
@@ -158,12 +160,14 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_, bool split)
     else if (tokens <= 4)
         s = rows <= cus       ? Shape{kToken4x1, 1, 1024, 1}
             : rows <= 2 * cus ? Shape{kToken4x2, 2, 512, 1}
+            : rows <= 3 * cus ? Shape{kToken4x3, 3, 512, 1}
             : rows <= 4 * cus ? Shape{kToken4x2Short, 2, 256, 1}
             : rows <= 8 * cus ? Shape{kToken4x7, even(7), 256, 1}
                               : Shape{kToken4x13, even(13), 128, 1};
     else if (tokens <= 8)
         s = rows <= cus       ? Shape{kToken8x1, 1, 1024, 1}
             : rows <= 2 * cus ? Shape{kToken8x2, 2, 512, 1}
+            : rows <= 3 * cus ? Shape{kToken8x3, 3, 512, 1}
             : rows <= 4 * cus ? Shape{kToken8x4, 4, 256, 1}
             : rows <= 8 * cus ? Shape{kToken8x7, even(7), 256, 1}
                               : Shape{kToken8x13, even(13), 128, 1};
@@ -171,6 +175,7 @@ Shape shape_of(const dq8_weights &w, size_t tokens, int cus_, bool split)
         s = divide            ? Shape{kToken16x4, 4, 256, 1}
             : rows <= cus     ? Shape{kToken16x1, 1, 1024, 1}
             : rows <= 2 * cus ? Shape{kToken16x2, 2, 512, 1}
+            : rows <= 3 * cus ? Shape{kToken16x3, 3, 512, 1}
             : rows <= 4 * cus ? Shape{kToken16x4, 4, 256, 1}
             : rows <= 8 * cus ? Shape{kToken16x7, even(7), 256, 1}
                               : Shape{kToken16x13, even(13), 128, 1};
@@ -227,16 +232,19 @@ int product(const ProductArgs &k, const Shape &s, const SplitArgs &split, hipStr
     case kFew4: return few<T, GROUP, 1, 4, 4>(k, stream);
     case kToken4x1: return chunks<T, GROUP, 1, 1, 1, 1, 8, 2, 4>(k, n, split, stream);
     case kToken4x2: return chunks<T, GROUP, 1, 1, 1, 2, 4, 4, 4>(k, n, split, stream);
+    case kToken4x3: return chunks<T, GROUP, 1, 1, 1, 3, 4, 2, 4>(k, n, split, stream);
     case kToken4x2Short: return chunks<T, GROUP, 1, 1, 1, 2, 2, 4, 4>(k, n, split, stream);
     case kToken4x7: return chunks<T, GROUP, 1, 1, 1, 7, 2, 2, 4, 4>(k, n, split, stream);
     case kToken4x13: return chunks<T, GROUP, 1, 1, 1, 13, 1, 2, 4, 7>(k, n, split, stream);
     case kToken8x1: return chunks<T, GROUP, 1, 2, 1, 1, 8, 2, 4>(k, n, split, stream);
     case kToken8x2: return chunks<T, GROUP, 1, 2, 1, 2, 4, 4, 4>(k, n, split, stream);
+    case kToken8x3: return chunks<T, GROUP, 1, 2, 1, 3, 4, 2, 4>(k, n, split, stream);
     case kToken8x4: return chunks<T, GROUP, 1, 2, 1, 4, 2, 4, 4>(k, n, split, stream);
     case kToken8x7: return chunks<T, GROUP, 1, 2, 1, 7, 2, 2, 4, 4>(k, n, split, stream);
     case kToken8x13: return chunks<T, GROUP, 1, 2, 1, 13, 1, 2, 4, 7>(k, n, split, stream);
     case kToken16x1: return chunks<T, GROUP, 1, 4, 1, 1, 8, 2, 4>(k, n, split, stream);
     case kToken16x2: return chunks<T, GROUP, 1, 4, 1, 2, 4, 2, 4>(k, n, split, stream);
+    case kToken16x3: return chunks<T, GROUP, 1, 4, 1, 3, 4, 2, 4>(k, n, split, stream);
     case kToken16x4: return chunks<T, GROUP, 1, 4, 1, 4, 2, 4, 5>(k, n, split, stream);
     case kToken16x7: return chunks<T, GROUP, 1, 4, 1, 7, 2, 2, 4, 4>(k, n, split, stream);
     case kToken16x13: return chunks<T, GROUP, 1, 4, 1, 13, 1, 2, 4, 7>(k, n, split, stream);

@@ -216,10 +216,10 @@ def test_products_of_many_tokens(rows, tokens):
         within(array(dq8.weights_product(x, codes, scales, rows=rows)), want, size, group, cols, torch.bfloat16)
 
 
-@pytest.mark.parametrize("rows", [24600, 30001, 45000, 53300, 70001])
+@pytest.mark.parametrize("rows", [8300, 12287, 24600, 30001, 45000, 53300, 70001])
 def test_products_of_evenly_divided_rows(rows):
-    """Workgroups with any number of row tiles from 5 to 13, and behind the last row."""
-    cols = 330
+    """Workgroups with three row tiles or any number from 5 to 13, and behind the last row."""
+    cols = 1330 if rows < 20000 else 330
     codes, scales = dq8.weights_encode(torch.randn(rows, cols, device="cuda"), 32)
     w = dq8.weights_decode(codes, scales, rows, cols).double()
     bias = torch.randn(rows, device="cuda")
