@@ -442,6 +442,46 @@ __device__ __forceinline__ void store_result(const ProductArgs &a, uint32_t toke
         static_cast<T *>(a.out)[at] = (T)v;
 }
 
+// A wavefront's results, MT 16 tokens from `first` on and R row tiles, by way of `space` (MT 16 times 64 bytes of LDS that nobody else uses), so that a lane stores
+// 16 bytes of a token and not single results of 64 (500 x 22235 results of 128 columns: 18.5 us, without 23.6; 500 x 8192 of 4096 columns 40.4, without 42.2).
+template <typename T, typename O, int MT, int R>
+__device__ __forceinline__ void store_rows(const ProductArgs &a, char *space, uint32_t lane, uint32_t first, uint32_t row_tile, const float (&sum)[MT][R][4])
+{
+    typedef w4u WA __attribute__((aligned(2)));
+    constexpr int TILES = R * 16 * sizeof(O) < 64 ? R : 64 / (16 * sizeof(O));  // row tiles at a time
+    constexpr uint32_t ROWS = TILES * 16, PIECES = ROWS * sizeof(O) / 16, EACH = 16 / sizeof(O);
+    const uint32_t n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int r0 = 0; r0 < R; r0 += TILES) {
+#pragma unroll
+        for (int r = r0; r < r0 + TILES; ++r) {
+            const uint32_t row = (row_tile + r) * kTileRows + n;
+            const float more = a.bias && row < a.rows ? a.bias[row] : 0.0f;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v = sum[m][r][q] * Operand<T>::kLift;
+                    if (a.bias) v += more;
+                    reinterpret_cast<O *>(space)[(m * 16 + g * 4 + q) * ROWS + (r - r0) * 16 + n] = (O)v;
+                }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (uint32_t i = 0; i < MT * 16 * PIECES / 64; ++i) {
+            const uint32_t at = i * 64 + lane, token = first + at / PIECES, row = (row_tile + r0) * kTileRows + at % PIECES * EACH;
+            if (token >= a.tokens || row >= a.rows) continue;
+            O *to = static_cast<O *>(a.out) + token * a.out_stride + row;
+            if (row + EACH <= a.rows) {
+                *reinterpret_cast<WA *>(to) = reinterpret_cast<const w4u *>(space)[at];
+            } else {
+                for (uint32_t e = 0; row + e < a.rows; ++e) to[e] = reinterpret_cast<const O *>(space)[at * EACH + e];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
 // Sums of KW wavefronts that have the same rows, added up in LDS in their order and handed to `store` (token tile, row tile, sum of the lane, value).
 template <int MT, int R, int Q, int KW, typename F>
 __device__ __forceinline__ void join_sums(float *parts, uint32_t wave, uint32_t lane, const float (&sum)[MT][R][Q], F store)
@@ -556,7 +596,7 @@ __global__ __launch_bounds__(KW * 64, 4) void k_weights_product_few(ProductArgs 
 // compute unit gets from L2 is about 25 bytes a cycle, of HBM's weights 12: with few row tiles in a workgroup, activations cost more than weights.
 // With `parts` (workspace) the chunks are divided over the workgroups of grid z as well, and k_weights_join adds up their sums.
 // 50021 x 4096, 13 tokens: 22 us of 16.5 that its bytes take (weights' loads alone 18.8); 4096 x 14336, 20 tokens over four splits: 10.5 us
-// (chunks one after the other: a barrier, LDS, four dependent matrix instructions) and 3 of the join; 8192 x 4096, 500 tokens: 42 us, 800 TFLOP/s (matrix and
+// (chunks one after the other: a barrier, LDS, four dependent matrix instructions) and 3 of the join; 8192 x 4096, 500 tokens: 40.4 us, 830 TFLOP/s (matrix and
 // vector instructions of two wavefronts a SIMD in turn; 32 us without loads).
 struct SplitArgs {
     float *parts;  // [splits][tokens][rows]
@@ -654,6 +694,16 @@ __global__ __launch_bounds__(RW * KW * 64, OCC) void k_weights_product(ProductAr
         place_x(0, x_rest);
         __syncthreads();
         if (whole * KW + kw < a.col_tiles) work(t_rest, 0);
+    }
+    if constexpr (KW == 1 && MT == 4) {
+        static_assert(Q == 4 && RW * MT * 16 * 64 <= sizeof(lds), "LDS of a wavefront's results");
+        __syncthreads();
+        char *space = lds + wave * (MT * 16 * 64);
+        if (a.wide)
+            store_rows<T, float, MT, R>(a, space, lane, first, row_tile, sum);
+        else
+            store_rows<T, T, MT, R>(a, space, lane, first, row_tile, sum);
+        return;
     }
     join_sums<MT, R, Q, KW>(reinterpret_cast<float *>(lds), wave, lane, sum, [&](uint32_t m, uint32_t r, uint32_t q, float v) {
         const uint32_t token = first + m * (4 * Q) + g * Q + q, row = (row_tile + r) * kTileRows + n;
