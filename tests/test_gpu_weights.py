@@ -216,6 +216,22 @@ def test_products_of_many_tokens(rows, tokens):
         within(array(dq8.weights_product(x, codes, scales, rows=rows)), want, size, group, cols, torch.bfloat16)
 
 
+@pytest.mark.parametrize("rows,tokens", [(28401, 200), (8203, 301), (8203, 700)])
+@pytest.mark.parametrize("to", [torch.float32, torch.float16])
+def test_results_of_many_tokens_with_strides_and_guards(rows, tokens, to):
+    cols, group = 200, 64
+    codes, scales = dq8.weights_encode(torch.randn(rows, cols, device="cuda"), group)
+    w = dq8.weights_decode(codes, scales, rows, cols).double()
+    bias = torch.randn(rows, device="cuda")
+    x = torch.randn(tokens, cols + 3, device="cuda").half()[:, 1 : cols + 1]
+    want, size = array(x.double() @ w.T) + array(bias), array(x.double().abs() @ w.abs().T)
+    for left, right in ((0, 0), (1, 4), (8, 5)):
+        out = torch.full((tokens + 2, left + rows + right), 7.0, dtype=to, device="cuda")
+        dq8.weights_product(x, codes, scales, rows=rows, bias=bias, out=out[1 : tokens + 1, left : left + rows])
+        within(array(out[1 : tokens + 1, left : left + rows]), want, size, group, cols, to, array(bias))
+        assert (out[0] == 7).all() and (out[-1] == 7).all() and (out[:, :left] == 7).all() and (out[:, left + rows :] == 7).all()
+
+
 @pytest.mark.parametrize("rows", [8300, 12287, 24600, 30001, 45000, 53300, 70001])
 def test_products_of_evenly_divided_rows(rows):
     """Workgroups with three row tiles or any number from 5 to 13, and behind the last row."""
