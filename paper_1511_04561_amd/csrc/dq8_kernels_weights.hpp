@@ -246,18 +246,24 @@ __device__ __forceinline__ void two_values(uint32_t word, float &a, float &b)
     b = (float)v.y;
 }
 
-// The reverse, bound by its writes: 26 us.
+// The reverse, bound by its writes: 24.5 us.  The values go out by way of LDS (a wavefront's own; 16 bytes change places by the row, so that neither side meets bank
+// conflicts), so that 256 or 512 bytes of a row lie side by side in a store: rows that start anywhere cost 29 us (14336 x 4104 bfloat16), stores of 64 bytes of each of
+// sixteen rows 47, and 28 where they start at multiples of 64 bytes.
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void k_weights_decode(const uint8_t *__restrict__ codes, const uint16_t *__restrict__ scales, size_t rows, size_t cols,
                                                         uint32_t col_tiles, size_t tiles, T *__restrict__ w, size_t stride)
 {
     constexpr int PER = kTileCols / GROUP, RUNS = 4 / PER;
+    constexpr uint32_t EACH = 16 / sizeof(T), UNITS = kTileCols / EACH;  // values of 16 bytes, and such of a row
+    typedef T V __attribute__((ext_vector_type(EACH)));
+    typedef V VA __attribute__((aligned(sizeof(T))));
+    __shared__ V lds[4][kTileRows * UNITS];
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const size_t tile = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (tile >= tiles) return;
-    const size_t rt = tile / col_tiles, ct = tile - rt * col_tiles, row = rt * kTileRows + n;
+    V *mine = lds[threadIdx.x >> 6];
+    const size_t rt = tile / col_tiles, ct = tile - rt * col_tiles;
     const w4u word = *reinterpret_cast<const w4u *>(codes + tile * kTileBytes + lane * 16);
-    if (row >= rows) return;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const float s = bf16_value(scales[(tile * kTileRows + n) * PER + r / RUNS]);
@@ -266,18 +272,27 @@ __global__ __launch_bounds__(256) void k_weights_decode(const uint8_t *__restric
         two_values<1>(word[r], x[2], x[3]);
         two_values<2>(word[r], x[4], x[5]);
         two_values<3>(word[r], x[6], x[7]);
-        typedef T V __attribute__((ext_vector_type(8)));
-        typedef V VA __attribute__((aligned(sizeof(T))));
-        V v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (T)(x[e] * s);
-        const size_t k = ct * kTileCols + 32 * r + 8 * g;
+        for (uint32_t h = 0; h < 8 / EACH; ++h) {
+            V v;
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) v[e] = (T)(x[h * EACH + e] * s);
+            mine[n * UNITS + (((4 * r + g) * (8 / EACH) + h) ^ n)] = v;
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (uint32_t i = 0; i < kTileRows * UNITS / 64; ++i) {
+        const uint32_t at = i * 64 + lane, m = at / UNITS, u = at % UNITS;
+        const size_t row = rt * kTileRows + m, k = ct * kTileCols + u * EACH;
+        if (row >= rows || k >= cols) continue;
+        const V v = mine[m * UNITS + (u ^ m)];
         T *to = w + row * stride + k;
-        if (k + 8 <= cols) {
+        if (k + EACH <= cols) {
             *reinterpret_cast<VA *>(to) = v;
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (uint32_t e = 0; e < EACH; ++e)
                 if (k + e < cols) to[e] = v[e];
         }
     }
