@@ -41,6 +41,17 @@ __device__ __forceinline__ w4u last_eight(const T *row, size_t k, size_t cols)
     return w4u{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
 }
 
+// 16 bytes without their first `halves` times two, zeros behind them.
+__device__ __forceinline__ w4u moved_down(w4u v, size_t halves)
+{
+    uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+    const uint32_t bits = 16 * (uint32_t)(halves & 3);
+    if (halves & 4) lo = hi, hi = 0;
+    lo = lo >> bits | hi << 1 << (63 - bits), hi >>= bits;
+    if (halves >= 8) lo = hi = 0;
+    return w4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // The scale of a group whose largest absolute value has these bits as binary32: the nearest bfloat16 number to a sixth of it.
 __device__ __forceinline__ float scale_of(uint32_t most)
 {
@@ -65,28 +76,14 @@ template <typename T>
 struct Eight {
     float x[8];
 
-    template <bool>
-    __device__ __forceinline__ void load(const float *row, size_t k, size_t cols)
+    __device__ __forceinline__ void take(const w4u *row, uint32_t piece, uint32_t n)
     {
-        typedef float V __attribute__((ext_vector_type(8), aligned(4)));
-        if (k + 8 <= cols) {
-            const V v = *reinterpret_cast<const V *>(row + k);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = v[e];
-        } else if (k < cols) {
+        for (uint32_t h = 0; h < 2; ++h) {
+            const w4u v = row[(2 * piece + h) ^ n];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = row[k + e < cols ? k + e : cols - 1];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = k + e < cols ? x[e] : 0.0f;
-        } else {
-            clear();
+            for (int e = 0; e < 4; ++e) x[4 * h + e] = __uint_as_float(v[e]);
         }
-    }
-
-    __device__ __forceinline__ void clear()
-    {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
     }
 
     // The bits of the largest absolute value: infinities and NaN are above all others.
@@ -123,27 +120,7 @@ template <typename T>
 struct Eight16 {
     w4u raw;
 
-    // ODD: rows may start between two words; from such a one the words behind the first number are loaded, and that number by itself (14336 x 4097: 36.5 us; sixteen
-    // bytes from between two words 48.5).
-    template <bool ODD>
-    __device__ __forceinline__ void load(const T *row, size_t k, size_t cols)
-    {
-        typedef w4u WA __attribute__((aligned(2)));
-        const size_t past = ODD && ((uintptr_t)row & 2) != 0 ? 1 : 0;
-        if (k + 8 + past <= cols) {
-            raw = *reinterpret_cast<const WA *>(row + k + past);
-            if constexpr (ODD) {
-                const uint32_t first = *reinterpret_cast<const uint16_t *>(row + k);
-                if (past) raw = w4u{first | raw.x << 16, raw.x >> 16 | raw.y << 16, raw.y >> 16 | raw.z << 16, raw.z >> 16 | raw.w << 16};
-            }
-        } else if (k < cols) {
-            raw = last_eight(row, k, cols);
-        } else {
-            clear();
-        }
-    }
-
-    __device__ __forceinline__ void clear() { raw = w4u{0, 0, 0, 0}; }
+    __device__ __forceinline__ void take(const w4u *row, uint32_t piece, uint32_t n) { raw = row[piece ^ n]; }
 
     __device__ __forceinline__ float at(int e) const
     {
@@ -190,23 +167,59 @@ struct Eight<__bf16> : Eight16<__bf16> {};
 template <>
 struct Eight<_Float16> : Eight16<_Float16> {};
 
-// A wavefront per tile: lane 16 g + n has of row n the four runs of eight columns that its piece holds.
-// 14336 x 4096 bfloat16, groups of 32: 150 MB in 26 us (memory; 49 us with the bisection of binary32, which is bound by the vector unit).
-template <typename T, int GROUP, bool ODD>
+// A wavefront per tile: lane 16 g + n has of row n the four runs of eight columns that its piece holds.  The tile comes in by way of LDS (the wavefront's own; 16 bytes
+// change places by the row, so that neither side meets bank conflicts): 256 or 512 bytes of a row lie side by side in a load.
+// 14336 x 4096 bfloat16, groups of 32: 150 MB in 25.5 us (memory; 26 with loads of 64 bytes of each of sixteen rows, and 48 where they start between two words; 49 with the bisection of binary32, which is bound by the vector unit).
+template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void k_weights_encode(const T *__restrict__ w, size_t stride, size_t rows, size_t cols, uint32_t col_tiles, size_t tiles,
                                                         uint8_t *__restrict__ codes, uint16_t *__restrict__ scales)
 {
     constexpr int PER = kTileCols / GROUP, RUNS = 4 / PER;  // groups of a row in a tile; runs of a group
+    constexpr uint32_t EACH = 16 / sizeof(T), UNITS = kTileCols / EACH, LOADS = kTileRows * UNITS / 64;
+    __shared__ w4u lds[4][kTileRows * UNITS];
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const size_t tile = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (tile >= tiles) return;
-    const size_t rt = tile / col_tiles, ct = tile - rt * col_tiles, row = rt * kTileRows + n;
+    w4u *mine = lds[threadIdx.x >> 6];
+    const size_t rt = tile / col_tiles, ct = tile - rt * col_tiles;
+    const T *from = w + rt * kTileRows * stride + ct * kTileCols;
+    const uint32_t tall = rows - rt * kTileRows < kTileRows ? (uint32_t)(rows - rt * kTileRows) : kTileRows;
+    const uint32_t wide = cols - ct * kTileCols < kTileCols ? (uint32_t)(cols - ct * kTileCols) : kTileCols;
+    auto place = [&](uint32_t at, w4u v) { mine[at / UNITS * UNITS + (at % UNITS ^ at / UNITS)] = v; };
+    if (tall == kTileRows && wide == kTileCols) {  // (all its loads at once)
+        typedef w4u WA __attribute__((aligned(2)));
+        w4u unit[LOADS];
+#pragma unroll
+        for (uint32_t i = 0; i < LOADS; ++i) {
+            const uint32_t at = i * 64 + lane;
+            unit[i] = *reinterpret_cast<const WA *>(from + at / UNITS * stride + at % UNITS * EACH);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < LOADS; ++i) place(i * 64 + lane, unit[i]);
+    } else if (wide >= EACH) {  // (of a ragged end the row's last 16 bytes, moved down, so that these too go out together)
+        typedef w4u WA __attribute__((aligned(2)));
+        w4u unit[LOADS];
+#pragma unroll
+        for (uint32_t i = 0; i < LOADS; ++i) {
+            const uint32_t at = i * 64 + lane, m = at / UNITS, k = at % UNITS * EACH;
+            unit[i] = *reinterpret_cast<const WA *>(from + (m < tall ? m : tall - 1) * stride + (k + EACH <= wide ? k : wide - EACH));
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < LOADS; ++i) {
+            const uint32_t at = i * 64 + lane, k = at % UNITS * EACH;
+            if (wide % EACH != 0 && k + EACH > wide) unit[i] = moved_down(unit[i], (k + EACH - wide) * (sizeof(T) / 2));
+            place(at, at / UNITS < tall && k < wide ? unit[i] : w4u{0, 0, 0, 0});
+        }
+    } else {
+        for (uint32_t at = lane; at < kTileRows * UNITS; at += 64) place(at, w4u{0, 0, 0, 0});
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane < tall)
+            for (uint32_t k = 0; k < wide; ++k) reinterpret_cast<T *>(mine + lane * UNITS + lane)[k] = from[lane * stride + k];  // (the first 16 bytes of row `lane` are there)
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     Eight<T> x[4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        x[s].clear();
-        if (row < rows) x[s].template load<ODD>(w + row * stride, ct * kTileCols + 32 * s + 8 * g, cols);
-    }
+    for (uint32_t s = 0; s < 4; ++s) x[s].take(mine + n * UNITS, 4 * s + g, n);
     w4u word;
     uint32_t scale[PER];
 #pragma unroll
@@ -548,13 +561,7 @@ __device__ __forceinline__ w4u eight_of_rest(const T *row, size_t k, uint32_t co
     typedef w4u WA __attribute__((aligned(2)));
     if (cols < 8) return k < cols ? last_eight(row, k, cols) : w4u{0, 0, 0, 0};
     const size_t from = k + 8 <= cols ? k : cols - 8, past = k - from;
-    const w4u v = *reinterpret_cast<const WA *>(row + from);
-    uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
-    const uint32_t bits = 16 * (uint32_t)(past & 3);
-    if (past & 4) lo = hi, hi = 0;
-    lo = lo >> bits | hi << 1 << (63 - bits), hi >>= bits;
-    if (past >= 8) lo = hi = 0;
-    return w4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    return moved_down(*reinterpret_cast<const WA *>(row + from), past);
 }
 
 constexpr uint32_t kRowPad = 16;  // bytes between the rows of activations in LDS, so that 16 rows' pieces lie in different banks

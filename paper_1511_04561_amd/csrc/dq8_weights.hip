@@ -59,21 +59,13 @@ int check_matrix(const char *who, const char *what, const dq8_weights &w, int ty
 
 bool known(int type) { return type == DQ8_FLOAT32 || type == DQ8_BFLOAT16 || type == DQ8_FLOAT16; }
 
-template <typename T, int GROUP, bool ODD>
-int encode(const void *w, size_t stride, const dq8_weights &o, hipStream_t stream)
-{
-    const Tiles t = tiles_of(o);
-    hipLaunchKernelGGL((k_weights_encode<T, GROUP, ODD>), dim3((unsigned)((t.all + 3) / 4)), dim3(256), 0, stream, static_cast<const T *>(w), stride, o.rows, o.cols,
-                       (uint32_t)t.cols, t.all, o.codes, static_cast<uint16_t *>(o.scales));
-    return dq8::after_launch_of("k_weights_encode", stream);
-}
-
 template <typename T, int GROUP>
 int encode(const void *w, size_t stride, const dq8_weights &o, hipStream_t stream)
 {
-    if constexpr (sizeof(T) == 2)
-        if ((((uintptr_t)w | stride * 2) & 2) != 0) return encode<T, GROUP, true>(w, stride, o, stream);
-    return encode<T, GROUP, false>(w, stride, o, stream);
+    const Tiles t = tiles_of(o);
+    hipLaunchKernelGGL((k_weights_encode<T, GROUP>), dim3((unsigned)((t.all + 3) / 4)), dim3(256), 0, stream, static_cast<const T *>(w), stride, o.rows, o.cols,
+                       (uint32_t)t.cols, t.all, o.codes, static_cast<uint16_t *>(o.scales));
+    return dq8::after_launch_of("k_weights_encode", stream);
 }
 
 template <typename T, int GROUP>
