@@ -169,7 +169,8 @@ struct Eight<_Float16> : Eight16<_Float16> {};
 
 // A wavefront per tile: lane 16 g + n has of row n the four runs of eight columns that its piece holds.  The tile comes in by way of LDS (the wavefront's own; 16 bytes
 // change places by the row, so that neither side meets bank conflicts): 256 or 512 bytes of a row lie side by side in a load.
-// 14336 x 4096 bfloat16, groups of 32: 150 MB in 25.5 us (memory; 26 with loads of 64 bytes of each of sixteen rows, and 48 where they start between two words; 49 with the bisection of binary32, which is bound by the vector unit).
+// 14336 x 4096 bfloat16, groups of 32: 150 MB in 25.5 us (memory; 26 with loads of 64 bytes of each of sixteen rows, and 48 where these start between two words; 49
+// with the bisection of binary32, which is bound by the vector unit).
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void k_weights_encode(const T *__restrict__ w, size_t stride, size_t rows, size_t cols, uint32_t col_tiles, size_t tiles,
                                                         uint8_t *__restrict__ codes, uint16_t *__restrict__ scales)
