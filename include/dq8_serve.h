@@ -3,7 +3,9 @@
  *
  * dq8_cache_plan makes the slots and positions of dq8_cache_append and the page tables, lengths and starts of dq8_cache_attention from the
  * lengths of the requests; dq8_draft_verify judges drafted tokens by the target model's probabilities, and the number of those it
- * rejects is what the next plan takes back.  Neither waits for the host, and both can be captured into a graph.
+ * rejects is what the next plan takes back.  A sequence that the plan refuses has no tokens in the step, and the drop that it was refused with is
+ * still to come: dq8_draft_verify takes the plan's `granted` and `drop` and hands that drop on.  Neither waits for the host, and both can be
+ * captured into a graph.
  *
  * Conventions (streams, device pointers, error codes, DQ8_DEBUG, threads) are those of dq8.h.  The structs are HOST memory, read before the
  * call returns; the pointers in them are DEVICE pointers.  What the host cannot see is checked by the kernels as described below; nothing
@@ -30,7 +32,7 @@ extern "C" {
  * A sequence is granted all that it asks for or refused: where it would have more than max_pages pages, where its new tokens would end
  * behind `tokens`, or where the stack does not hold the pages that it and the sequences before it take.  (A refused sequence takes none, but
  * counts among those before the next: after one that found too few pages none that needs any gets them.)  For a refused sequence nothing
- * changes, its drop included.
+ * changes, its drop included, which a later plan has to be given again.
  * Written: starts[batch + 1], the sums of new tokens before each sequence, refused ones counted (at most `tokens`); granted[b]: new tokens
  * granted, -1 where refused; lens_out[b]: the length after the step; n_free_out[0]; and for tokens i = 0 .. `tokens` - 1 of the step, packed in the
  * order of the sequences, positions[i], the place in its sequence, and slots[i] = page * page_size + place in the page; both are -1 for tokens of
@@ -67,6 +69,9 @@ int dq8_cache_plan(const dq8_plan *p, void *hip_stream);
  * batch up to 65535, tokens below 2^31, vocab from 1 to below 2^31 - 4096.
  * starts outside 0 .. tokens count as the nearer end; they must not descend (a sequence whose do has no rows, and rows that two claim hold
  * tokens of either).
+ * granted [batch] (NULL: nobody was refused) and drop [batch] (NULL: 0 for all): those of the plan that gave the rows their places.  The rows of a sequence with granted[b]
+ * negative hold no tokens, whatever is in them: out is -1 there, accepted[b] is -1, and rejected[b] is what the plan did not take back, drop[b] (negative:
+ * 0).  So `rejected` is the next plan's drop for every sequence.  rejected may be drop; without granted, drop is not read.
  * workspace: dq8_draft_verify_workspace_bytes bytes at a multiple of 16, whose contents are of no meaning before and after; calls that
  * may run at the same time must not share it.  Without (NULL, or too few bytes) one workgroup reads a sequence's whole row.  Results do not depend on it.
  */
@@ -80,6 +85,7 @@ typedef struct {
     const int32_t *starts;
     int64_t *out;
     int32_t *accepted, *rejected;
+    const int32_t *granted, *drop;
 } dq8_verify;
 
 /* (Looks at sizes; the pointers may be anything.  0 after an error, or where none is of use.) */

@@ -916,11 +916,11 @@ PyObject *cache_plan(PyObject *const *a)  // lens, new, pages, free, n_free, pag
     return tuple_of(given, made);
 }
 
-PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace
+PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace, granted, drop
 {
     Matrix target, draft;
     Buffer sample, space;
-    void *stream, *p[6] = {};
+    void *stream, *p[6] = {}, *of_plan[2] = {};
     at::Tensor made[3];
     dq8_verify v = {};
     if (!target.take(a[0]) || !stream_for(*target.t, stream) || !buffer(a[3], at::kFloat, sample) || sample.t->dim() != 1 || sample.n == 0 ||
@@ -932,6 +932,8 @@ PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, sta
     if (!axis(a[1], at::kLong, v.tokens, like, p[0]) || !axis(a[2], at::kFloat, v.tokens, like, p[1]) ||
         (a[4] != Py_None && !axis(a[4], at::kInt, v.batch + 1, like, p[2])))
         return declined();
+    for (int i = 0; i < 2; ++i)
+        if (a[10 + i] != Py_None && !axis(a[10 + i], at::kInt, v.batch, like, of_plan[i])) return declined();
     PyObject *const given[3] = {a[6], a[7], a[8]};
     const size_t n[3] = {v.tokens, v.batch, v.batch};
     size_t bytes = 0;
@@ -951,6 +953,7 @@ PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, sta
         }
     v.ids = static_cast<int64_t *>(p[0]), v.uniform = static_cast<float *>(p[1]), v.sample = static_cast<float *>(sample.ptr);
     v.starts = static_cast<int32_t *>(p[2]), v.out = static_cast<int64_t *>(p[3]), v.accepted = static_cast<int32_t *>(p[4]), v.rejected = static_cast<int32_t *>(p[5]);
+    v.granted = static_cast<int32_t *>(of_plan[0]), v.drop = static_cast<int32_t *>(of_plan[1]);
     Scratch scratch;
     if (a[9] == Py_None) {
         if (!scratch.take(g_lib.workspace_verify(&v), like, stream)) return declined();
@@ -1032,7 +1035,7 @@ PyMethodDef g_methods[] = {
     method<weights_decode, 6>("weights_decode"),
     method<weights_product, 8>("weights_product"),
     method<cache_plan, 14>("cache_plan"),
-    method<draft_verify, 10>("draft_verify"),
+    method<draft_verify, 12>("draft_verify"),
     {nullptr, nullptr, 0, nullptr},
 };
 

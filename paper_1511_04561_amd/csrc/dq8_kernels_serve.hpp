@@ -276,6 +276,7 @@ struct VerifyArgs {
     uint32_t chunk, chunks;   // probabilities that a wavefront adds up at a time, and how many such
     struct Verdict *verdicts; // workspace [batch] (null: there is none)
     double *sums;             // workspace [batch][chunks]
+    const int32_t *granted, *drop;  // of the plan (null: nobody was refused, nothing was dropped)
 };
 
 // A probability: what is no positive number counts as none.
@@ -286,7 +287,10 @@ __device__ __forceinline__ float probability(T v)
     return __builtin_amdgcn_classf(f, 0x180) ? f : 0.0f;  // positive, subnormal or normal
 }
 
-// Where a sequence ends: rows first .. first + n - 1, `row` of them accepted; refused: whether row `row` refused its draft `token`.
+// Where a sequence ends: rows first .. first + n - 1, `row` of them accepted; refused: whether row `row` refused its draft `token`, or kNotGranted for a
+// sequence whose rows got no places from the plan.
+constexpr uint32_t kNotGranted = 2;
+
 struct Verdict {
     uint32_t first, n, row, refused;
     int64_t token;
@@ -310,9 +314,9 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
     }
     v.n = end - v.first;
     v.row = v.n ? v.n - 1 : 0;
-    v.refused = 0;
+    v.refused = a.granted && a.granted[b] < 0 ? kNotGranted : 0;
     v.token = -1;
-    for (uint32_t i0 = 0; i0 + 1 < v.n; i0 += 64) {
+    for (uint32_t i0 = 0; i0 + 1 < v.n && v.refused == 0; i0 += 64) {
         const uint32_t i = i0 + lane;
         bool no = false;
         int64_t d = -1;
@@ -333,7 +337,6 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
             v.row = i0 + (uint32_t)l;
             v.refused = 1;
             v.token = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(d >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)d, l));
-            break;
         }
     }
     v.first = (uint32_t)__builtin_amdgcn_readfirstlane((int)v.first);
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(kSumsWaves * 64) void k_verify_sums(VerifyArgs a)
     if (first >= a.chunks) return;
     const Verdict v = verdict_of<T>(a, b);
     if (first == 0 && lane == 0) a.verdicts[b] = v;
-    if (v.n == 0) return;
+    if (v.n == 0 || v.refused == kNotGranted) return;
     const Row<T> row(a, v);
     for (uint32_t c = first; c < a.chunks; c += gridDim.x * kSumsWaves) {
         const double s = sum_chunk(a, row, c);
@@ -489,6 +492,15 @@ __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(V
     const Verdict v = ALONE ? verdict_of<T>(a, b) : a.verdicts[b];
     if constexpr (!ALONE)
         for (uint32_t c = lane; c < a.chunks; c += 64) sums[c] = a.sums[(size_t)b * a.chunks + c];
+    if (v.refused == kNotGranted) {  // what the plan was asked to take back is still to be taken
+        if (threadIdx.x == 0) {
+            const int32_t owed = a.drop ? a.drop[b] : 0;
+            a.accepted[b] = -1;
+            a.rejected[b] = owed > 0 ? owed : 0;
+        }
+        for (uint32_t i = threadIdx.x; i < v.n; i += ALONE ? kAloneWaves * 64 : 64) a.out[v.first + i] = -1;
+        return;
+    }
     if (threadIdx.x == 0) {
         a.accepted[b] = v.n ? (int32_t)v.row : -1;
         a.rejected[b] = v.n ? (int32_t)(v.n - 1 - v.row) : 0;

@@ -154,16 +154,19 @@ int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_byt
     if (!v.accepted || !v.rejected || !v.sample || (v.tokens && (!v.target || !v.ids || !v.uniform || !v.out))) return failed(DQ8_ERR_NULL, "%s: NULL pointer", who);
     const size_t size = v.type == DQ8_FLOAT32 ? 4 : 2;
     if ((((uintptr_t)v.target | (uintptr_t)v.draft) & (size - 1)) != 0 || (((uintptr_t)v.ids | (uintptr_t)v.out) & 7) != 0 ||
-        (((uintptr_t)v.uniform | (uintptr_t)v.sample | (uintptr_t)v.starts | (uintptr_t)v.accepted | (uintptr_t)v.rejected) & 3) != 0 || ((uintptr_t)workspace & 15) != 0)
+        (((uintptr_t)v.uniform | (uintptr_t)v.sample | (uintptr_t)v.starts | (uintptr_t)v.accepted | (uintptr_t)v.rejected | (uintptr_t)v.granted |
+          (uintptr_t)v.drop) & 3) != 0 || ((uintptr_t)workspace & 15) != 0)
         return failed(DQ8_ERR_ARG, "%s: an array does not start at a multiple of its element's size (workspace: 16 bytes)", who);
     auto extent = [&](size_t stride) { return v.tokens ? ((v.tokens - 1) * stride + v.vocab) * size : 0; };
     const Array written[] = {{v.out, v.tokens * 8}, {v.accepted, v.batch * 4}, {v.rejected, v.batch * 4}, {workspace, workspace ? workspace_bytes : 0}};
     const Array read[] = {{v.target, extent(v.target_stride)}, {v.draft, v.draft ? extent(v.draft_stride) : 0}, {v.ids, v.tokens * 8}, {v.uniform, v.tokens * 4},
-                          {v.sample, v.batch * 4}, {v.starts, v.starts ? (v.batch + 1) * 4 : 0}};
+                          {v.sample, v.batch * 4}, {v.starts, v.starts ? (v.batch + 1) * 4 : 0}, {v.granted, v.granted ? v.batch * 4 : 0},
+                          {v.drop, v.granted && v.drop && v.drop != v.rejected ? v.batch * 4 : 0}};
     if (overlap(written, read)) return failed(DQ8_ERR_ARG, "%s: an output or the workspace overlaps another array", who);
     VerifyArgs k;
     k.target = v.target, k.draft = v.draft, k.target_stride = v.target_stride, k.draft_stride = v.draft_stride;
     k.ids = v.ids, k.uniform = v.uniform, k.sample = v.sample, k.starts = v.starts, k.out = v.out, k.accepted = v.accepted, k.rejected = v.rejected;
+    k.granted = v.granted, k.drop = v.drop;
     k.tokens = (uint32_t)v.tokens, k.batch = (uint32_t)v.batch, k.each = v.starts ? 0 : (uint32_t)(v.tokens / v.batch), k.vocab = (uint32_t)v.vocab;
     cut(v, k.chunk, k.chunks);
     dq8::DeviceTables dev;

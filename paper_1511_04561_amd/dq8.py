@@ -79,7 +79,7 @@ class _Plan(ctypes.Structure):  # dq8_plan of include/dq8_serve.h
 class _Verify(ctypes.Structure):  # dq8_verify
     _fields_ = ([("type", ctypes.c_int)] + [(f, ctypes.c_size_t) for f in ("tokens", "batch", "vocab")] + [(f, ctypes.c_void_p) for f in ("target", "draft")]
                 + [(f, ctypes.c_size_t) for f in ("target_stride", "draft_stride")]
-                + [(f, ctypes.c_void_p) for f in ("ids", "uniform", "sample", "starts", "out", "accepted", "rejected")])
+                + [(f, ctypes.c_void_p) for f in ("ids", "uniform", "sample", "starts", "out", "accepted", "rejected", "granted", "drop")])
 
 
 def lib():
@@ -773,7 +773,7 @@ def cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop=None, slo
     lens int32 [sequences]: cached tokens; drop int32 (None: none): how many of them are taken back first (rejected drafts; all of a
     sequence that has ended); new int32: how many are added.  pages int32 [sequences, n]: each sequence's page numbers, in place; free int32 and n_free
     int32 [1]: the stack of free pages, pages given back and taken in place.  A sequence gets all places that it needs or is refused and
-    stays as it was (granted -1).  tokens: rows of the step, padding among them.
+    stays as it was (granted -1, and its drop has to be given again: draft_verify hands it on).  tokens: rows of the step, padding among them.
 
     Returns (slots int64 [tokens], positions int64 [tokens], starts int32 [sequences + 1], lens_out, granted, n_free_out): -1 in slots and positions
     for padding and refused sequences; lens_out may be lens and n_free_out may be n_free.  (Those that are not handed in may share one allocation.)"""
@@ -831,7 +831,7 @@ def draft_verify_workspace(target, ids, uniform, sample, starts=None, draft=None
         return int(lib().dq8_draft_verify_workspace_bytes(ctypes.byref(v)))
 
 
-def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None, accepted=None, rejected=None, workspace=None):
+def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None, accepted=None, rejected=None, workspace=None, granted=None, drop=None):
     """Which drafted tokens stay, and the token behind them.
 
     Rows starts[b] .. starts[b + 1] - 1 of a step (None: every sequence has as many) are a sequence's last accepted token and its drafts, ids int64
@@ -839,10 +839,13 @@ def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None
     type: those that the token of the next row was drawn from (None: the draft was sure of it).  uniform float32 [tokens], sample float32
     [sequences]: random numbers from 0 to 1; row i's token of row i + 1 stays while uniform[i] * draft < target.
 
-    Returns (out int64 [tokens]: accepted tokens, the one drawn behind them, -1; accepted int32 [sequences]; rejected int32 [sequences]: what
-    cache_plan takes back as ``drop``).  workspace: a uint8 tensor of draft_verify_workspace() bytes; None: taken from torch's allocator, and not while the
+    granted, drop: those of the cache_plan that gave the rows their places (None: it refused nobody; it had none).  A sequence that it refused gets -1 in out and
+    accepted, and in rejected the drop that is still to come (``rejected`` may be ``drop``).
+
+    Returns (out int64 [tokens]: accepted tokens, the one drawn behind them, -1; accepted int32 [sequences]; rejected int32 [sequences]: what the
+    next cache_plan takes back as ``drop``).  workspace: a uint8 tensor of draft_verify_workspace() bytes; None: taken from torch's allocator, and not while the
     stream is captured into a graph (hand one in there: without it one workgroup reads a sequence's whole row)."""
-    done = _native.draft_verify(target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace)
+    done = _native.draft_verify(target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace, granted, drop)
     if done is not None:
         return done
     v = _draft(target, ids, uniform, sample, starts, draft)
@@ -850,6 +853,7 @@ def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None
     out = _given(out, dev, torch.int64, (v.tokens,), "out")
     accepted, rejected = _given(accepted, dev, torch.int32, (v.batch,), "accepted"), _given(rejected, dev, torch.int32, (v.batch,), "rejected")
     v.out, v.accepted, v.rejected = out.data_ptr(), accepted.data_ptr(), rejected.data_ptr()
+    v.granted, v.drop = (None if t is None else _given(t, dev, torch.int32, (v.batch,), what).data_ptr() for t, what in ((granted, "granted"), (drop, "drop")))
     if workspace is None:
         with torch.cuda.device(dev):
             if not torch.cuda.is_current_stream_capturing():
