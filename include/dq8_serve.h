@@ -65,10 +65,11 @@ int dq8_cache_plan(const dq8_plan *p, void *hip_stream);
  * none was with the target's of the last row.  It is the first t whose weights 0 .. t add up to more than sample[b] times the sum of all, or the last with
  * a weight where none does (sample[b] of 1 and more; NaN and negative count as 0).  Differences and sums in binary64.
  * Written: out, for each row of a sequence: the accepted tokens, the drawn one, then -1 (the drawn one is -1 too if all its weights are 0); accepted[b]: how
- * many drafts were accepted, -1 for a sequence without rows; rejected[b]: how many were not.  Rows behind the last sequence stay as they were.
+ * many drafts were accepted, -1 for a sequence without rows; rejected[b]: how many were not.  Rows of no sequence, before the first and behind the last,
+ * stay as they were, or are -1 where `fill` is not 0.  (Without sequences nothing is written.)
  * batch up to 65535, tokens below 2^31, vocab from 1 to below 2^31 - 4096.
  * starts outside 0 .. tokens count as the nearer end; they must not descend (a sequence whose do has no rows, and rows that two claim hold
- * tokens of either).
+ * tokens of either, with `fill` perhaps -1).
  * granted [batch] (NULL: nobody was refused) and drop [batch] (NULL: 0 for all): those of the plan that gave the rows their places.  The rows of a sequence with granted[b]
  * negative hold no tokens, whatever is in them: out is -1 there, accepted[b] is -1, and rejected[b] is what the plan did not take back, drop[b] (negative:
  * 0).  So `rejected` is the next plan's drop for every sequence.  rejected may be drop; without granted, drop is not read.
@@ -86,6 +87,7 @@ typedef struct {
     int64_t *out;
     int32_t *accepted, *rejected;
     const int32_t *granted, *drop;
+    int fill;
 } dq8_verify;
 
 /* (Looks at sizes; the pointers may be anything.  0 after an error, or where none is of use.) */

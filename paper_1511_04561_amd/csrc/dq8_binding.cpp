@@ -953,6 +953,7 @@ PyObject *draft_verify(PyObject *const *a)  // target, ids, uniform, sample, sta
         }
     v.ids = static_cast<int64_t *>(p[0]), v.uniform = static_cast<float *>(p[1]), v.sample = static_cast<float *>(sample.ptr);
     v.starts = static_cast<int32_t *>(p[2]), v.out = static_cast<int64_t *>(p[3]), v.accepted = static_cast<int32_t *>(p[4]), v.rejected = static_cast<int32_t *>(p[5]);
+    v.fill = given[0] == Py_None;
     v.granted = static_cast<int32_t *>(of_plan[0]), v.drop = static_cast<int32_t *>(of_plan[1]);
     Scratch scratch;
     if (a[9] == Py_None) {

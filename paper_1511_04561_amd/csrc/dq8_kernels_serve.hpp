@@ -277,6 +277,7 @@ struct VerifyArgs {
     struct Verdict *verdicts; // workspace [batch] (null: there is none)
     double *sums;             // workspace [batch][chunks]
     const int32_t *granted, *drop;  // of the plan (null: nobody was refused, nothing was dropped)
+    int fill;                 // whether rows of no sequence get -1
 };
 
 // A probability: what is no positive number counts as none.
@@ -296,6 +297,12 @@ struct Verdict {
     int64_t token;
 };
 
+__device__ __forceinline__ uint32_t start_of(const VerifyArgs &a, uint32_t b)
+{
+    const int32_t s = a.starts[b];
+    return s < 0 ? 0 : (uint32_t)s < a.tokens ? (uint32_t)s : a.tokens;
+}
+
 // Every wavefront finds it by itself: a lane per draft.
 template <typename T>
 __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
@@ -304,9 +311,8 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
     Verdict v;
     uint32_t end;
     if (a.starts) {
-        const int32_t s0 = a.starts[b], s1 = a.starts[b + 1];
-        v.first = s0 < 0 ? 0 : (uint32_t)s0 < a.tokens ? (uint32_t)s0 : a.tokens;
-        end = s1 < 0 ? 0 : (uint32_t)s1 < a.tokens ? (uint32_t)s1 : a.tokens;
+        v.first = start_of(a, b);
+        end = start_of(a, b + 1);
         if (end < v.first) end = v.first;
     } else {
         v.first = b * a.each;
@@ -487,18 +493,24 @@ template <typename T, bool ALONE>
 __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(VerifyArgs a)
 {
     __shared__ double sums[kChunksMost];
+    constexpr uint32_t WG = ALONE ? kAloneWaves * 64 : 64;
     const uint32_t b = blockIdx.x, lane = threadIdx.x & 63, wave = wave_of(threadIdx.x);
     const float r = a.sample[b];
     const Verdict v = ALONE ? verdict_of<T>(a, b) : a.verdicts[b];
     if constexpr (!ALONE)
         for (uint32_t c = lane; c < a.chunks; c += 64) sums[c] = a.sums[(size_t)b * a.chunks + c];
+    if (a.fill) {  // all workgroups have a part of the rows of no sequence
+        const uint32_t s0 = start_of(a, 0), s1 = start_of(a, a.batch), mine = b * WG + threadIdx.x;
+        for (uint32_t i = mine; i < s0; i += a.batch * WG) a.out[i] = -1;
+        for (uint32_t i = s1 + mine; i < a.tokens; i += a.batch * WG) a.out[i] = -1;
+    }
     if (v.refused == kNotGranted) {  // what the plan was asked to take back is still to be taken
         if (threadIdx.x == 0) {
             const int32_t owed = a.drop ? a.drop[b] : 0;
             a.accepted[b] = -1;
             a.rejected[b] = owed > 0 ? owed : 0;
         }
-        for (uint32_t i = threadIdx.x; i < v.n; i += ALONE ? kAloneWaves * 64 : 64) a.out[v.first + i] = -1;
+        for (uint32_t i = threadIdx.x; i < v.n; i += WG) a.out[v.first + i] = -1;
         return;
     }
     if (threadIdx.x == 0) {

@@ -166,7 +166,7 @@ int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_byt
     VerifyArgs k;
     k.target = v.target, k.draft = v.draft, k.target_stride = v.target_stride, k.draft_stride = v.draft_stride;
     k.ids = v.ids, k.uniform = v.uniform, k.sample = v.sample, k.starts = v.starts, k.out = v.out, k.accepted = v.accepted, k.rejected = v.rejected;
-    k.granted = v.granted, k.drop = v.drop;
+    k.granted = v.granted, k.drop = v.drop, k.fill = v.fill && v.starts;
     k.tokens = (uint32_t)v.tokens, k.batch = (uint32_t)v.batch, k.each = v.starts ? 0 : (uint32_t)(v.tokens / v.batch), k.vocab = (uint32_t)v.vocab;
     cut(v, k.chunk, k.chunks);
     dq8::DeviceTables dev;

@@ -79,7 +79,7 @@ class _Plan(ctypes.Structure):  # dq8_plan of include/dq8_serve.h
 class _Verify(ctypes.Structure):  # dq8_verify
     _fields_ = ([("type", ctypes.c_int)] + [(f, ctypes.c_size_t) for f in ("tokens", "batch", "vocab")] + [(f, ctypes.c_void_p) for f in ("target", "draft")]
                 + [(f, ctypes.c_size_t) for f in ("target_stride", "draft_stride")]
-                + [(f, ctypes.c_void_p) for f in ("ids", "uniform", "sample", "starts", "out", "accepted", "rejected", "granted", "drop")])
+                + [(f, ctypes.c_void_p) for f in ("ids", "uniform", "sample", "starts", "out", "accepted", "rejected", "granted", "drop")] + [("fill", ctypes.c_int)])
 
 
 def lib():
@@ -842,15 +842,19 @@ def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None
     granted, drop: those of the cache_plan that gave the rows their places (None: it refused nobody; it had none).  A sequence that it refused gets -1 in out and
     accepted, and in rejected the drop that is still to come (``rejected`` may be ``drop``).
 
-    Returns (out int64 [tokens]: accepted tokens, the one drawn behind them, -1; accepted int32 [sequences]; rejected int32 [sequences]: what the
-    next cache_plan takes back as ``drop``).  workspace: a uint8 tensor of draft_verify_workspace() bytes; None: taken from torch's allocator, and not while the
-    stream is captured into a graph (hand one in there: without it one workgroup reads a sequence's whole row)."""
+    Returns (out int64 [tokens]: accepted tokens, the one drawn behind them, -1, and -1 in rows of no sequence, which an ``out`` that is handed in keeps
+    as they were; accepted int32 [sequences]; rejected int32 [sequences]: what the next cache_plan takes back as ``drop``).  workspace: a uint8 tensor of
+    draft_verify_workspace() bytes; None: taken from torch's allocator, and not while the stream is captured into a graph (hand one in there: without it one
+    workgroup reads a sequence's whole row)."""
     done = _native.draft_verify(target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace, granted, drop)
     if done is not None:
         return done
     v = _draft(target, ids, uniform, sample, starts, draft)
     dev = target.device
+    v.fill = out is None
     out = _given(out, dev, torch.int64, (v.tokens,), "out")
+    if v.fill and v.batch == 0:
+        out.fill_(-1)
     accepted, rejected = _given(accepted, dev, torch.int32, (v.batch,), "accepted"), _given(rejected, dev, torch.int32, (v.batch,), "rejected")
     v.out, v.accepted, v.rejected = out.data_ptr(), accepted.data_ptr(), rejected.data_ptr()
     v.granted, v.drop = (None if t is None else _given(t, dev, torch.int32, (v.batch,), what).data_ptr() for t, what in ((granted, "granted"), (drop, "drop")))
