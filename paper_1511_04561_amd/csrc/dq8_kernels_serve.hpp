@@ -261,8 +261,11 @@ __global__ __launch_bounds__(kPlaceWg) void k_cache_place(PlanArgs a)
 //
 // A sequence's drafts are judged by single numbers; only the row behind the accepted ones is read as a whole, the draft's too where one was
 // refused.  A row is cut into chunks; a wavefront adds up one at a time.  The chunk in which the sum passes its mark is found from the
-// chunks' sums and read once more by one wavefront, which finds the token in it.  All sums are binary64: their rounding, 2^-53 of the whole, moves no token's
-// border by as much as 2^-28 of the smallest step between two random numbers of 24 bits.
+// chunks' sums and read once more by one wavefront, which finds the token in it.  All sums are binary64: each addition is off
+// by 2^-53 of the whole at most.  A number is in 10 of them on its way into a chunk's sum (4 of a lane, 6 of lanes), 37 more into the whole's (31 of a lane's chunks at most,
+// 6 of lanes), or 68 into the sum before a chunk (31 again) and 17 to a token's border in it; with the mark's product and the differences fewer than 150, so that no border
+// moves by 2^-45 of the whole, 2^-21 of the step between two random numbers of 24 bits.  (Up to a vocabulary of 2^21; then chunks have more than 1024 numbers, one addition for
+// each 1024 more.)
 
 struct VerifyArgs {
     const void *target, *draft;
@@ -541,7 +544,8 @@ __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(V
     }
     int64_t token = -1;
     if (total > 0.0) {
-        const double mark = (r > 0.0f ? (double)r : 0.0) * total;
+        // (of one and more: above all sums, for a running one may round to more than the whole's, which is taken in another order)
+        const double mark = r >= 1.0f ? __builtin_inf() : (r > 0.0f ? (double)r : 0.0) * total;
         const uint32_t c = first_above(run, mark, sum, chunk_sum);
         const uint32_t begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
         for (uint32_t i0 = begin; i0 < end; i0 += kChunk) {
