@@ -162,9 +162,16 @@ def n_blocks(n, block):
     return (n + b - 1) // b
 
 
-def _dev(t, dtype, what):
+def _cuda(t, what):
+    """A tensor in device memory that holds its elements, and not their negatives (as the imaginary part of a conjugate does)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % what)
+    if t.is_neg():
+        raise ValueError("%s is a view of negated elements (resolve_neg() gives a tensor of its own)" % what)
+
+
+def _dev(t, dtype, what):
+    _cuda(t, what)
     if t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
     if not t.is_contiguous():
@@ -495,8 +502,7 @@ def _on(device, t, dtype, shape, what):
 
 def _rows(t, what, device, dtype, tokens, heads, dim):
     """[tokens, heads, dim] with the elements of a row side by side, any other strides: (address, token stride, head stride)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor" % what)
+    _cuda(t, what)
     if t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
     if t.dim() != 3 or (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
@@ -625,8 +631,7 @@ def cache_attention(kind, q, codes, scales, pages, lens, starts=None, max_new=No
 
 def _matrix(t, what, device, dtypes, rows, cols):
     """[rows, cols] (None: any) with the elements of a row side by side: (address, stride)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor" % what)
+    _cuda(t, what)
     if t.dtype not in dtypes:
         raise TypeError("%s must be %s, got %s" % (what, " or ".join(str(d) for d in dtypes), t.dtype))
     if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
