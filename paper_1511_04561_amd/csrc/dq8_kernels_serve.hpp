@@ -267,21 +267,32 @@ __global__ __launch_bounds__(kPlaceWg) void k_cache_place(PlanArgs a)
 // moves by 2^-45 of the whole, 2^-21 of the step between two random numbers of 24 bits.  (Up to a vocabulary of 2^21; then chunks have more than 1024 numbers, one addition for
 // each 1024 more.)
 
+struct Verdict;
+
+// 128 bytes, two cache lines of a launch's arguments: with 152 a row of 32000 took 6.40 us in a graph, so 6.33.
 struct VerifyArgs {
     const void *target, *draft;
     size_t target_stride, draft_stride;
     const int64_t *ids;
     const float *uniform, *sample;
-    const int32_t *starts;
+    union {
+        const int32_t *starts;
+        uint64_t each;  // rows of every sequence, with kEven
+    };
     int64_t *out;
     int32_t *accepted, *rejected;
-    uint32_t tokens, batch, each, vocab;
-    uint32_t chunk, chunks;   // probabilities that a wavefront adds up at a time, and how many such
-    struct Verdict *verdicts; // workspace [batch] (null: there is none)
-    double *sums;             // workspace [batch][chunks]
     const int32_t *granted, *drop;  // of the plan (null: nobody was refused, nothing was dropped)
-    int fill;                 // whether rows of no sequence get -1
+    double *sums;                   // workspace [batch][chunks], and behind it [batch] verdicts
+    uint32_t tokens, batch, vocab;
+    uint32_t flags;                 // the logarithm of a chunk's probabilities, kEven, kFill
+
+    static constexpr uint32_t kEven = 256, kFill = 512;  // kFill: rows of no sequence get -1
+
+    __host__ __device__ uint32_t chunk() const { return 1u << (flags & 31); }  // probabilities that a wavefront adds up at a time
+    __host__ __device__ uint32_t chunks() const { return (vocab + chunk() - 1) >> (flags & 31); }
+    __host__ __device__ Verdict *verdicts() const { return reinterpret_cast<Verdict *>(sums + (size_t)batch * chunks()); }
 };
+static_assert(sizeof(VerifyArgs) == 128, "two cache lines");
 
 // A probability: what is no positive number counts as none.
 template <typename T>
@@ -291,10 +302,7 @@ __device__ __forceinline__ float probability(T v)
     return __builtin_amdgcn_classf(f, 0x180) ? f : 0.0f;  // positive, subnormal or normal
 }
 
-// Where a sequence ends: rows first .. first + n - 1, `row` of them accepted; refused: whether row `row` refused its draft `token`, or kNotGranted for a
-// sequence whose rows got no places from the plan.
-constexpr uint32_t kNotGranted = 2;
-
+// Where a sequence ends: rows first .. first + n - 1, `row` of them accepted; refused: whether row `row` refused its draft `token`.
 struct Verdict {
     uint32_t first, n, row, refused;
     int64_t token;
@@ -306,6 +314,9 @@ __device__ __forceinline__ uint32_t start_of(const VerifyArgs &a, uint32_t b)
     return s < 0 ? 0 : (uint32_t)s < a.tokens ? (uint32_t)s : a.tokens;
 }
 
+// Whether the plan refused a sequence: its rows hold no tokens.
+__device__ __forceinline__ bool without_places(const VerifyArgs &a, uint32_t b) { return a.granted && a.granted[b] < 0; }
+
 // Every wavefront finds it by itself: a lane per draft.
 template <typename T>
 __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
@@ -313,19 +324,19 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
     const uint32_t lane = threadIdx.x & 63;
     Verdict v;
     uint32_t end;
-    if (a.starts) {
+    if (!(a.flags & VerifyArgs::kEven)) {
         v.first = start_of(a, b);
         end = start_of(a, b + 1);
         if (end < v.first) end = v.first;
     } else {
-        v.first = b * a.each;
-        end = v.first + a.each;
+        v.first = b * (uint32_t)a.each;
+        end = v.first + (uint32_t)a.each;
     }
     v.n = end - v.first;
     v.row = v.n ? v.n - 1 : 0;
-    v.refused = a.granted && a.granted[b] < 0 ? kNotGranted : 0;
+    v.refused = 0;
     v.token = -1;
-    for (uint32_t i0 = 0; i0 + 1 < v.n && v.refused == 0; i0 += 64) {
+    for (uint32_t i0 = 0; i0 + 1 < v.n; i0 += 64) {
         const uint32_t i = i0 + lane;
         bool no = false;
         int64_t d = -1;
@@ -346,6 +357,7 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
             v.row = i0 + (uint32_t)l;
             v.refused = 1;
             v.token = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(d >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)d, l));
+            break;
         }
     }
     v.first = (uint32_t)__builtin_amdgcn_readfirstlane((int)v.first);
@@ -354,7 +366,16 @@ __device__ __forceinline__ Verdict verdict_of(const VerifyArgs &a, uint32_t b)
     return v;
 }
 
-constexpr uint32_t kSumsWaves = 4, kAloneWaves = 16, kChunksMost = 2048, kChunk = 1024;
+// Wavefront `mine` of `all` writes its part of the rows of no sequence.  Wavefronts do it that nobody waits for (0.08 of 6.3 us).
+__device__ __forceinline__ void fill_others(const VerifyArgs &a, uint32_t mine, uint32_t all)
+{
+    if (!(a.flags & VerifyArgs::kFill)) return;
+    const uint32_t s0 = start_of(a, 0), s1 = start_of(a, a.batch), at = mine * 64 + (threadIdx.x & 63);
+    for (uint32_t i = at; i < s0; i += all * 64) a.out[i] = -1;
+    for (uint32_t i = s1 + at; i < a.tokens; i += all * 64) a.out[i] = -1;
+}
+
+constexpr uint32_t kSumsWaves = 4, kAloneWaves = 16, kPickWaves = 2, kChunksMost = 2048, kChunk = 1024;
 constexpr int kPer = kChunk / 64;  // numbers of a lane: neighbours
 
 // The row from which a sequence's token is drawn.
@@ -424,7 +445,7 @@ struct Row {
 template <typename T>
 __device__ __forceinline__ double sum_chunk(const VerifyArgs &a, const Row<T> &row, uint32_t c)
 {
-    const uint32_t begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
+    const uint32_t begin = c * a.chunk(), end = a.vocab - begin < a.chunk() ? a.vocab : begin + a.chunk();
     double sum = 0.0;
     for (uint32_t i = begin; i < end; i += kChunk) {
         double w[kPer];
@@ -442,14 +463,14 @@ template <typename T>
 __global__ __launch_bounds__(kSumsWaves * 64) void k_verify_sums(VerifyArgs a)
 {
     const uint32_t b = blockIdx.y, first = blockIdx.x * kSumsWaves + wave_of(threadIdx.x), lane = threadIdx.x & 63;
-    if (first >= a.chunks) return;
+    if (first >= a.chunks()) return;
     const Verdict v = verdict_of<T>(a, b);
-    if (first == 0 && lane == 0) a.verdicts[b] = v;
-    if (v.n == 0 || v.refused == kNotGranted) return;
+    if (first == 0 && lane == 0) a.verdicts()[b] = v;
+    if (v.n == 0 || without_places(a, b)) return;
     const Row<T> row(a, v);
-    for (uint32_t c = first; c < a.chunks; c += gridDim.x * kSumsWaves) {
+    for (uint32_t c = first; c < a.chunks(); c += gridDim.x * kSumsWaves) {
         const double s = sum_chunk(a, row, c);
-        if (lane == 63) a.sums[(size_t)b * a.chunks + c] = s;
+        if (lane == 63) a.sums[(size_t)b * a.chunks() + c] = s;
     }
 }
 
@@ -489,53 +510,56 @@ __device__ __forceinline__ uint32_t first_above(uint32_t run, double mark, doubl
     return (uint32_t)l * run + (uint32_t)__builtin_amdgcn_readlane((int)(votes ? at : last), l);
 }
 
-// One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums.
+// One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums, and a
+// second one for the rows of no sequence.
 // 32000 probabilities, ALONE: 6.0 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
 // needs), then 4.5.
 template <typename T, bool ALONE>
-__global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(VerifyArgs a)
+__global__ __launch_bounds__((ALONE ? kAloneWaves : kPickWaves) * 64) void k_verify_pick(VerifyArgs a)
 {
     __shared__ double sums[kChunksMost];
-    constexpr uint32_t WG = ALONE ? kAloneWaves * 64 : 64;
+    constexpr uint32_t OTHERS = (ALONE ? kAloneWaves : kPickWaves) - 1;
     const uint32_t b = blockIdx.x, lane = threadIdx.x & 63, wave = wave_of(threadIdx.x);
     const float r = a.sample[b];
-    const Verdict v = ALONE ? verdict_of<T>(a, b) : a.verdicts[b];
+    const bool no_places = without_places(a, b);
+    const Verdict v = ALONE ? verdict_of<T>(a, b) : a.verdicts()[b];
     if constexpr (!ALONE)
-        for (uint32_t c = lane; c < a.chunks; c += 64) sums[c] = a.sums[(size_t)b * a.chunks + c];
-    if (a.fill) {  // all workgroups have a part of the rows of no sequence
-        const uint32_t s0 = start_of(a, 0), s1 = start_of(a, a.batch), mine = b * WG + threadIdx.x;
-        for (uint32_t i = mine; i < s0; i += a.batch * WG) a.out[i] = -1;
-        for (uint32_t i = s1 + mine; i < a.tokens; i += a.batch * WG) a.out[i] = -1;
-    }
-    if (v.refused == kNotGranted) {  // what the plan was asked to take back is still to be taken
-        if (threadIdx.x == 0) {
-            const int32_t owed = a.drop ? a.drop[b] : 0;
+        for (uint32_t c = threadIdx.x; c < a.chunks(); c += kPickWaves * 64) sums[c] = a.sums[(size_t)b * a.chunks() + c];
+    if (v.n == 0 || no_places) {
+        if (wave != 0) {
+            fill_others(a, b * OTHERS + wave - 1, a.batch * OTHERS);
+            return;
+        }
+        if (lane == 0) {
+            const int32_t owed = no_places && a.drop ? a.drop[b] : 0;  // what the plan was asked to take back is still to be taken
             a.accepted[b] = -1;
             a.rejected[b] = owed > 0 ? owed : 0;
         }
-        for (uint32_t i = threadIdx.x; i < v.n; i += WG) a.out[v.first + i] = -1;
+        for (uint32_t i = lane; i < v.n; i += 64) a.out[v.first + i] = -1;
         return;
     }
     if (threadIdx.x == 0) {
-        a.accepted[b] = v.n ? (int32_t)v.row : -1;
-        a.rejected[b] = v.n ? (int32_t)(v.n - 1 - v.row) : 0;
+        a.accepted[b] = (int32_t)v.row;
+        a.rejected[b] = (int32_t)(v.n - 1 - v.row);
     }
-    if (v.n == 0) return;
     Row<T> row(a, v);
     if constexpr (ALONE)
-        for (uint32_t c = wave; c < a.chunks; c += kAloneWaves) {
+        for (uint32_t c = wave; c < a.chunks(); c += kAloneWaves) {
             const double s = sum_chunk(a, row, c);
             if (lane == 63) sums[c] = s;
         }
     __syncthreads();
-    if (wave != 0) return;
-    const uint32_t run = (a.chunks + 63) / 64;
-    auto chunk_sum = [&](uint32_t i) { return lane * run + i < a.chunks ? sums[lane * run + i] : 0.0; };
+    if (wave != 0) {
+        fill_others(a, b * OTHERS + wave - 1, a.batch * OTHERS);
+        return;
+    }
+    const uint32_t run = (a.chunks() + 63) / 64;
+    auto chunk_sum = [&](uint32_t i) { return lane * run + i < a.chunks() ? sums[lane * run + i] : 0.0; };
     double total, sum = sums_of(run, total, chunk_sum);
     if (!(total > 0.0)) {  // nothing is left of the difference: the target's own
         row.q = nullptr;
         row.less = -1;
-        for (uint32_t c = 0; c < a.chunks; ++c) {
+        for (uint32_t c = 0; c < a.chunks(); ++c) {
             const double s = sum_chunk(a, row, c);
             if (lane == 63) sums[c] = s;
         }
@@ -547,7 +571,7 @@ __global__ __launch_bounds__(ALONE ? kAloneWaves * 64 : 64) void k_verify_pick(V
         // (of one and more: above all sums, for a running one may round to more than the whole's, which is taken in another order)
         const double mark = r >= 1.0f ? __builtin_inf() : (r > 0.0f ? (double)r : 0.0) * total;
         const uint32_t c = first_above(run, mark, sum, chunk_sum);
-        const uint32_t begin = c * a.chunk, end = a.vocab - begin < a.chunk ? a.vocab : begin + a.chunk;
+        const uint32_t begin = c * a.chunk(), end = a.vocab - begin < a.chunk() ? a.vocab : begin + a.chunk();
         for (uint32_t i0 = begin; i0 < end; i0 += kChunk) {
             double x[kPer], mine = 0.0;
             row.template weights<false>(i0, end, x);

@@ -84,13 +84,13 @@ int verify(const VerifyArgs &k, int cus, hipStream_t stream)
         return dq8::after_launch_of("k_verify_pick", stream);
     }
     // wavefronts for the whole chip, a chunk at least for each
-    unsigned groups = (k.chunks + kSumsWaves - 1) / kSumsWaves;
+    unsigned groups = (k.chunks() + kSumsWaves - 1) / kSumsWaves;
     const unsigned most = (unsigned)cus * 32 / (kSumsWaves * k.batch) + 1;
     if (groups > most) groups = most;
     hipLaunchKernelGGL(k_verify_sums<T>, dim3(groups, k.batch), dim3(kSumsWaves * 64), 0, stream, k);
     const int rc = dq8::after_launch_of("k_verify_sums", stream);
     if (rc) return rc;
-    hipLaunchKernelGGL((k_verify_pick<T, false>), dim3(k.batch), dim3(64), 0, stream, k);
+    hipLaunchKernelGGL((k_verify_pick<T, false>), dim3(k.batch), dim3(kPickWaves * 64), 0, stream, k);
     return dq8::after_launch_of("k_verify_pick", stream);
 }
 
@@ -166,15 +166,17 @@ int dq8_draft_verify(const dq8_verify *in, void *workspace, size_t workspace_byt
     VerifyArgs k;
     k.target = v.target, k.draft = v.draft, k.target_stride = v.target_stride, k.draft_stride = v.draft_stride;
     k.ids = v.ids, k.uniform = v.uniform, k.sample = v.sample, k.starts = v.starts, k.out = v.out, k.accepted = v.accepted, k.rejected = v.rejected;
-    k.granted = v.granted, k.drop = v.drop, k.fill = v.fill && v.starts;
-    k.tokens = (uint32_t)v.tokens, k.batch = (uint32_t)v.batch, k.each = v.starts ? 0 : (uint32_t)(v.tokens / v.batch), k.vocab = (uint32_t)v.vocab;
-    cut(v, k.chunk, k.chunks);
+    k.granted = v.granted, k.drop = v.drop;
+    k.tokens = (uint32_t)v.tokens, k.batch = (uint32_t)v.batch, k.vocab = (uint32_t)v.vocab;
+    uint32_t chunk, chunks;
+    cut(v, chunk, chunks);
+    k.flags = (uint32_t)__builtin_ctz(chunk) | (v.starts ? 0 : VerifyArgs::kEven) | (v.fill && v.starts ? VerifyArgs::kFill : 0);
+    if (!v.starts) k.each = v.tokens / v.batch;
     dq8::DeviceTables dev;
     const int found = dq8::device_tables(0, &dev);
     if (found) return found;
     const bool some = v.tokens && workspace && !alone(v, dev.cus) && workspace_bytes >= workspace_of(v);
     k.sums = some ? static_cast<double *>(workspace) : nullptr;
-    k.verdicts = some ? reinterpret_cast<Verdict *>(k.sums + v.batch * k.chunks) : nullptr;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (v.type == DQ8_FLOAT32) return verify<float>(k, dev.cus, stream);
     return v.type == DQ8_BFLOAT16 ? verify<__bf16>(k, dev.cus, stream) : verify<_Float16>(k, dev.cus, stream);
