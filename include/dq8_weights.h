@@ -55,7 +55,7 @@ int dq8_weights_decode(const dq8_weights *in, int type, void *w, size_t row_stri
  * Products are exact, sums are held in binary32 (of 32 .. 128 products in the matrix instructions, then times the group's scale; of bfloat16 activations
  * at 2^-10 of their size, so that no sum of a group leaves binary32, and results below 2^-115 have fewer bits), the result is rounded once.  Their order depends on rows, cols, tokens and group and on whether there is a workspace: equal calls give equal bits.  An
  * infinity or NaN in a row of x makes that row of out what it makes the sum; other rows do not depend on it.
- * workspace: dq8_weights_product_workspace_bytes bytes at a multiple of 16 (0: none is of use, as for up to 8 tokens), whose contents are of no meaning before
+ * workspace: dq8_weights_product_workspace_bytes bytes at a multiple of 16 (0: none is used, as for up to 8 tokens), whose contents are of no meaning before
  * and after; calls that may run at the same time must not share it.  Without (NULL, or too few bytes) a workgroup has all columns of its rows:
  * slower where there are few rows.
  */

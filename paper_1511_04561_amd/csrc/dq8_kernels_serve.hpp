@@ -512,8 +512,8 @@ __device__ __forceinline__ uint32_t first_above(uint32_t run, double mark, doubl
 
 // One workgroup per sequence.  ALONE: its wavefronts add up the chunks themselves; otherwise it is one wavefront behind k_verify_sums, and a
 // second one for the rows of no sequence.
-// 32000 probabilities, ALONE: 6.0 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
-// needs), then 4.5.
+// 32000 probabilities, ALONE: 6.3 us, of which binary64 instructions of one compute unit are half; 64 sequences of 131072: k_verify_sums 11.5 us (4.7 TB/s of what it
+// needs), then 4.
 template <typename T, bool ALONE>
 __global__ __launch_bounds__((ALONE ? kAloneWaves : kPickWaves) * 64) void k_verify_pick(VerifyArgs a)
 {

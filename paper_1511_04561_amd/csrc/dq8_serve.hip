@@ -57,9 +57,9 @@ void cut(const dq8_verify &v, uint32_t &chunk, uint32_t &chunks)
 
 // Whether one workgroup reads a sequence's whole row, in one launch, or the whole chip and then a wavefront per sequence, in two: ns that each takes.  What a compute unit
 // needs for a row grows with its numbers, what the chip needs with all of them.  us from Python, in one | in two launches, four tokens of each sequence:
-//   binary32 with the draft's probabilities, 8 sequences of 32768 7.7 | 8.2, 50021 9.7 | 8.3, 65536 11.0 | 8.0; 64 of 100000 16.6 | 14.1, 131072 19.8 | 16.6; 128 of 131072
-//   22.9, bfloat16 20.7; binary32 without, 8 of 50021 7.6 | 8.3, 65536 8.5 | 8.1, 131072 12.8 | 8.0; 64 of 131072 13.8 | 11.2.  (In a graph two launches are a
-//   microsecond cheaper: one sequence of 32768 with draft 6.9 | 6.9, of 65536 bfloat16 without 8.4 | 6.7; 256 of 131072 bfloat16 without 15.6 | 30.)
+//   binary32 with the draft's probabilities, 8 sequences of 32768 7.8 | 7.9, 50021 9.8 | 7.9, 65536 11.0 | 8.1; 64 of 100000 16.7 | 12.9, 131072 19.9 | 15.8; 128 of 131072
+//   22.7 | 23.0, bfloat16 20.7 | 17.2; binary32 without, 8 of 50021 7.7 | 7.8, 65536 8.5 | 8.0, 131072 12.9 | 8.0; 64 of 131072 14.0 | 11.2.  (In a graph two launches of few
+//   sequences are a microsecond cheaper: one of 32768 with draft 6.2 | 6.2, of 65536 bfloat16 without 8.4 | 6.4; 256 of 131072 bfloat16 without 16.0 | 19.7.)
 bool alone(const dq8_verify &v, int cus)
 {
     uint32_t chunk, chunks;

@@ -781,7 +781,8 @@ def cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop=None, slo
     stays as it was (granted -1, and its drop has to be given again: draft_verify hands it on).  tokens: rows of the step, padding among them.
 
     Returns (slots int64 [tokens], positions int64 [tokens], starts int32 [sequences + 1], lens_out, granted, n_free_out): -1 in slots and positions
-    for padding and refused sequences; lens_out may be lens and n_free_out may be n_free.  (Those that are not handed in may share one allocation.)"""
+    for padding and refused sequences; lens_out may be lens and n_free_out may be n_free.  (Those that are not handed in share one
+    allocation, as draft_verify's do.)"""
     done = _native.cache_plan(lens, new, pages, free, n_free, page_size, tokens, drop, slots, positions, starts, lens_out, granted, n_free_out)
     if done is not None:
         return done
@@ -850,7 +851,8 @@ def draft_verify(target, ids, uniform, sample, starts=None, draft=None, out=None
     Returns (out int64 [tokens]: accepted tokens, the one drawn behind them, -1, and -1 in rows of no sequence, which an ``out`` that is handed in keeps
     as they were; accepted int32 [sequences]; rejected int32 [sequences]: what the next cache_plan takes back as ``drop``).  workspace: a uint8 tensor of
     draft_verify_workspace() bytes; None: taken from torch's allocator, and not while the stream is captured into a graph (hand one in there: without it one
-    workgroup reads a sequence's whole row)."""
+    workgroup reads a sequence's whole row).  Results that are not handed in share one allocation: what keeps one keeps all, and resize_ of one may reach
+    into the next."""
     done = _native.draft_verify(target, ids, uniform, sample, starts, draft, out, accepted, rejected, workspace, granted, drop)
     if done is not None:
         return done
