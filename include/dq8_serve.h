@@ -8,7 +8,7 @@
  * captured into a graph.
  *
  * Conventions (streams, device pointers, error codes, DQ8_DEBUG, threads) are those of dq8.h.  The structs are HOST memory, read before the
- * call returns; the pointers in them are DEVICE pointers.  What the host cannot see is checked by the kernels as described below; nothing
+ * call returns; the pointers in them are DEVICE pointers; fields that a caller does not use are 0.  What the host cannot see is checked by the kernels as described below; nothing
  * outside the given arrays is read or written.
  */
 #ifndef DQ8_SERVE_H
